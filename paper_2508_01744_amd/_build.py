@@ -7,7 +7,7 @@ ROOT = os.path.dirname(PKG)
 CSRC = os.path.join(PKG, "csrc")
 INCLUDE = os.path.join(ROOT, "include")
 LIB = os.path.join(PKG, "libagft.so")
-SOURCES = [os.path.join(CSRC, "agft_step.hip"), os.path.join(CSRC, "agft_env.hip")]
+SOURCES = [os.path.join(CSRC, name) for name in ("agft_step.hip", "agft_env.hip", "agft_kv.hip", "agft_kv_attend.hip")]
 
 HIPCC_FLAGS = [
     "--offload-arch=gfx950", "-O3", "-std=c++17", "-fPIC", "-shared",

@@ -1,6 +1,6 @@
 """ctypes binding of libagft.so: argument marshalling only.
 
-The names mirror include/agft.h and include/agft_sim.h.  Loading fails loudly
+The names mirror include/agft.h, include/agft_sim.h and include/agft_kv.h.  Loading fails loudly
 when the library has not been built: there is no other implementation to
 fall back to.
 """
@@ -56,11 +56,36 @@ class agft_launch_shape(ctypes.Structure):
                 ("cu_workgroups", _i32)]
 
 
+class agft_kv_config(ctypes.Structure):
+    _fields_ = [("requests", _i32), ("row_pages", _i32), ("pages", _i32), ("page", _i32),
+                ("heads", _i32), ("group", _i32), ("dim", _i32), ("form", _i32)]
+
+
+class agft_kv_tables_view(ctypes.Structure):
+    _fields_ = [("counters", _vp), ("lengths", _vp), ("table", _vp), ("ring", _vp)]
+
+
+class agft_kv_step_view(ctypes.Structure):
+    _fields_ = [("counters", _vp), ("lengths", _vp), ("granted", _vp), ("starts", _vp), ("slots", _vp)]
+
+
+class agft_kv_dense(ctypes.Structure):
+    _fields_ = [("data", _vp), ("token_stride", _i64), ("head_stride", _i64), ("type", _i32)]
+
+
+AGFT_KV_E4M3, AGFT_KV_INT8 = 0, 1
+AGFT_KV_BF16, AGFT_KV_FP16, AGFT_KV_FP32 = 0, 1, 2
+
 ABI_VERSION = 6   # AGFT_ABI_VERSION of the agft_config layout declared here
 
 EXPORTED = ["agft_state_bytes", "agft_create", "agft_step", "agft_get_state", "agft_export",
             "agft_set_stream", "agft_destroy", "agft_strerror", "agft_abi_version", "agft_launch_shape_for",
             "agft_env_state_bytes", "agft_env_reset", "agft_env_step", "agft_sim_step"]
+
+# of agft_kv.h
+KV_EXPORTED = ["agft_kv_tables_bytes", "agft_kv_step_bytes", "agft_kv_cache_bytes", "agft_kv_attend_bytes",
+               "agft_kv_tables_at", "agft_kv_step_at", "agft_kv_reset", "agft_kv_plan", "agft_kv_commit",
+               "agft_kv_append", "agft_kv_attend", "agft_kv_export"]
 
 _lib = None
 
@@ -103,6 +128,21 @@ def _declare(lib):
     lib.agft_env_step.argtypes = [envp, _vp, _sz, _i32, _vp, _vp, _vp, _vp, _vp, _vp]
     lib.agft_sim_step.restype = ctypes.c_int
     lib.agft_sim_step.argtypes = [_vp, envp, _vp, _sz, _vp, _vp, _vp, _vp, _vp, _vp]
+    kvp, densep = ctypes.POINTER(agft_kv_config), ctypes.POINTER(agft_kv_dense)
+    for name, restype, args in (
+            ("tables_bytes", _sz, []), ("step_bytes", _sz, [_i32]), ("cache_bytes", _sz, []),
+            ("attend_bytes", _sz, [_i32]),
+            ("tables_at", ctypes.c_int, [_vp, _sz, ctypes.POINTER(agft_kv_tables_view)]),
+            ("step_at", ctypes.c_int, [_i32, _vp, _sz, ctypes.POINTER(agft_kv_step_view)]),
+            ("reset", ctypes.c_int, [_vp, _sz, _vp]),
+            ("plan", ctypes.c_int, [_vp, _sz, _vp, _vp, _sz, _i32, _vp]),
+            ("commit", ctypes.c_int, [_vp, _sz, _vp, _sz, _i32, _vp]),
+            ("append", ctypes.c_int, [_vp, _sz, _vp, _sz, _i32, densep, densep, _vp]),
+            ("attend", ctypes.c_int, [_vp, _sz, _vp, _sz, _vp, _sz, _i32, _i32, densep, densep, _vp, _f32, _vp, _sz,
+                                      _vp]),
+            ("export", ctypes.c_int, [_vp, _sz, _vp, _i64, densep, densep, _vp])):
+        fn = getattr(lib, "agft_kv_" + name)
+        fn.restype, fn.argtypes = restype, [kvp, *args]
     return lib
 
 

@@ -1,0 +1,173 @@
+// agft_kv_common.h -- what the cache's kernels share: the configuration's
+// checks, where the parts of the caller's buffers lie, and the 8-bit codes.
+#ifndef AGFT_KV_COMMON_H
+#define AGFT_KV_COMMON_H
+
+#include <hip/hip_runtime.h>
+
+#include <cstddef>
+#include <cstdint>
+
+#include "agft.h"
+#include "agft_kv.h"
+
+namespace agft_kv_detail {
+
+constexpr size_t kAlign = 256;
+constexpr int kBlockTokens = 16;   // tokens of a layout block
+constexpr int kBlockDims = 64;     // numbers of a layout block
+constexpr int kBlockBytes = kBlockTokens * kBlockDims;
+constexpr int kUnit = 64;          // tokens of a unit of attention work
+constexpr int kFewRows = 16;       // query rows (tokens x group) of a request that one matrix tile holds
+constexpr int kTileRows = 128;     // query rows of a tile of the attention over many rows
+constexpr int kMinExp = -64;
+
+inline size_t align_up(size_t n) { return (n + kAlign - 1) / kAlign * kAlign; }
+
+// AGFT_OK, or what is wrong with the configuration
+inline int config_status(const agft_kv_config *c) {
+    if (c == nullptr) return AGFT_E_INVAL;
+    if (c->requests < 1 || c->requests > 65536 || c->row_pages < 1) return AGFT_E_INVAL;
+    if (c->page != 16 && c->page != 32 && c->page != 64 && c->page != 128) return AGFT_E_INVAL;
+    if ((int64_t)c->row_pages * c->page >= (int64_t)1 << 30) return AGFT_E_INVAL;
+    if (c->pages < 1 || c->pages > 1 << 28) return AGFT_E_INVAL;
+    if (c->heads < 1 || c->heads > 256 || c->group < 1 || c->group > 128) return AGFT_E_INVAL;
+    if (c->form != AGFT_KV_E4M3 && c->form != AGFT_KV_INT8) return AGFT_E_INVAL;
+    if (c->dim != 64 && c->dim != 128 && c->dim != 256)
+        return c->dim >= 1 ? AGFT_E_UNSUPPORTED : AGFT_E_INVAL;
+    return AGFT_OK;
+}
+
+inline bool tokens_ok(int32_t max_tokens) { return max_tokens >= 1 && max_tokens <= 1 << 30; }
+
+struct TablesLayout {
+    size_t counters, lengths, table, ring, total;
+};
+
+inline TablesLayout tables_layout(const agft_kv_config *c) {
+    TablesLayout L;
+    size_t at = 0;
+    L.counters = at, at += align_up(8 * 4);
+    L.lengths = at, at += align_up((size_t)c->requests * 4);
+    L.table = at, at += align_up((size_t)c->requests * c->row_pages * 4);
+    L.ring = at, at += align_up((size_t)c->pages * 4);
+    L.total = at;
+    return L;
+}
+
+struct StepLayout {
+    size_t counters, starts, granted, lengths, work, tiles, need, touched, back, runs, slots, total;
+};
+
+// Runs of one page's tokens in a window: a request's n tokens touch at most
+// 2 + (n - 2) / page pages.
+inline int64_t run_cap(const agft_kv_config *c, int32_t max_tokens) {
+    const int64_t by_page = 2 * (int64_t)c->requests + max_tokens / c->page;
+    return by_page < max_tokens ? by_page : max_tokens;
+}
+
+inline StepLayout step_layout(const agft_kv_config *c, int32_t max_tokens) {
+    StepLayout L;
+    size_t at = 0;
+    const size_t row = align_up(((size_t)c->requests + 1) * 4);
+    L.counters = at, at += align_up(8 * 4);
+    L.starts = at, at += row;
+    L.granted = at, at += row;
+    L.lengths = at, at += row;
+    L.work = at, at += row;
+    L.tiles = at, at += row;
+    L.need = at, at += row;
+    L.touched = at, at += row;
+    L.back = at, at += row;
+    L.runs = at, at += align_up(((size_t)run_cap(c, max_tokens) + 1) * 4);
+    L.slots = at, at += align_up((size_t)max_tokens * 8);
+    L.total = at;
+    return L;
+}
+
+struct CacheLayout {
+    size_t codes, exps, total;
+};
+
+inline CacheLayout cache_layout(const agft_kv_config *c) {
+    CacheLayout L;
+    L.codes = 0;
+    L.exps = align_up((size_t)c->pages * c->heads * 2 * c->page * c->dim);
+    L.total = L.exps + align_up((size_t)c->pages * c->heads * 2 * 4);
+    return L;
+}
+
+inline bool buffer_ok(const void *p, size_t have, size_t need) {
+    return p != nullptr && reinterpret_cast<uintptr_t>(p) % kAlign == 0 && have >= need;
+}
+
+inline size_t type_bytes(int32_t type) { return type == AGFT_KV_FP32 ? 4 : 2; }
+
+// rows of numbers that can be moved 16 bytes at a time
+inline bool dense_ok(const agft_kv_dense *t) {
+    if (t == nullptr || t->data == nullptr) return false;
+    if (t->type != AGFT_KV_BF16 && t->type != AGFT_KV_FP16 && t->type != AGFT_KV_FP32) return false;
+    const int64_t per = 16 / (int64_t)type_bytes(t->type);
+    return reinterpret_cast<uintptr_t>(t->data) % 16 == 0 && t->token_stride >= 0 && t->head_stride >= 0 &&
+           t->token_stride % per == 0 && t->head_stride % per == 0;
+}
+
+inline int launched() { return hipGetLastError() == hipSuccess ? AGFT_OK : AGFT_E_HIP; }
+
+// ---- device side ----
+
+// 2^e for e in -126..127
+__device__ __forceinline__ float pow2(int e) { return __uint_as_float((uint32_t)(e + 127) << 23); }
+
+template <int FORM>
+struct Code;
+
+template <>
+struct Code<AGFT_KV_E4M3> {
+    static constexpr float kMax = 448.0f;
+    // four numbers within the range to four codes, to nearest even
+    static __device__ __forceinline__ uint32_t pack4(float a, float b, float c, float d) {
+        int w = __builtin_amdgcn_cvt_pk_fp8_f32(a, b, 0, false);
+        return (uint32_t)__builtin_amdgcn_cvt_pk_fp8_f32(c, d, w, true);
+    }
+    static __device__ __forceinline__ void unpack4(uint32_t w, float *x) {
+        x[0] = __builtin_amdgcn_cvt_f32_fp8((int)w, 0);
+        x[1] = __builtin_amdgcn_cvt_f32_fp8((int)w, 1);
+        x[2] = __builtin_amdgcn_cvt_f32_fp8((int)w, 2);
+        x[3] = __builtin_amdgcn_cvt_f32_fp8((int)w, 3);
+    }
+    // smallest e with top <= 448 * 2^e = 1.75 * 2^(e + 8)
+    static __device__ __forceinline__ int need(uint32_t bits) {
+        return (int)(bits >> 23) - 127 - ((bits & 0x7fffffu) <= 0x600000u ? 8 : 7);
+    }
+};
+
+template <>
+struct Code<AGFT_KV_INT8> {
+    static constexpr float kMax = 127.0f;
+    static __device__ __forceinline__ uint32_t pack4(float a, float b, float c, float d) {
+        return ((uint32_t)(int)rintf(a) & 255u) | ((uint32_t)(int)rintf(b) & 255u) << 8 |
+               ((uint32_t)(int)rintf(c) & 255u) << 16 | (uint32_t)(int)rintf(d) << 24;
+    }
+    static __device__ __forceinline__ void unpack4(uint32_t w, float *x) {
+        x[0] = (float)(int8_t)w;
+        x[1] = (float)(int8_t)(w >> 8);
+        x[2] = (float)(int8_t)(w >> 16);
+        x[3] = (float)(int8_t)(w >> 24);
+    }
+    // smallest e with top <= 127 * 2^e = 1.984375 * 2^(e + 6)
+    static __device__ __forceinline__ int need(uint32_t bits) {
+        return (int)(bits >> 23) - 127 - ((bits & 0x7fffffu) <= 0x7e0000u ? 6 : 5);
+    }
+};
+
+// The exponent that holds top (finite, >= 0).
+template <int FORM>
+__device__ __forceinline__ int exponent(float top) {
+    const int e = Code<FORM>::need(__float_as_uint(top));
+    return e < kMinExp ? kMinExp : e;
+}
+
+}  // namespace agft_kv_detail
+
+#endif

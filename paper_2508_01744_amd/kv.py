@@ -1,0 +1,301 @@
+"""Python front end of the serving node's paged cache (agft_kv.h): torch
+supplies device memory and streams, the work runs in the HIP kernels behind
+libagft.so.
+
+One window of a node with a KvTables `tables` and, per layer, a KvCache `cache`:
+
+    step = tables.plan(add, max_tokens)        # pages and slots of the new tokens
+    cache.append(step, k, v)                   # per layer
+    out = cache.attend(tables, step, q)        # per layer
+    tables.commit(step)                        # the new lengths become the tables'
+
+Calls enqueue on the stream given to the object, or else on the stream that is
+current when they are called; nothing here waits for the GPU except load().
+"""
+import ctypes
+import math
+
+import torch
+
+from . import _lib as L
+
+FORMS = {"e4m3": L.AGFT_KV_E4M3, "int8": L.AGFT_KV_INT8}
+TYPES = {torch.bfloat16: L.AGFT_KV_BF16, torch.float16: L.AGFT_KV_FP16, torch.float32: L.AGFT_KV_FP32}
+
+
+def kv_config(requests, row_tokens, pages, page=16, heads=8, group=4, dim=128, form="e4m3"):
+    """The agft_kv_config of a node: rows of the block table, tokens a request
+    can hold, pages of the pool, tokens of a page, key/value heads, query heads
+    per key/value head, numbers of a head, and how the cache holds them
+    ("e4m3" or "int8").  No device work."""
+    if form not in FORMS:
+        raise ValueError(f"form must be one of {sorted(FORMS)}, not {form!r}")
+    page = int(page)
+    if page < 1:
+        raise ValueError("a page holds at least one token")
+    return L.agft_kv_config(int(requests), -(-int(row_tokens) // page), int(pages), page, int(heads), int(group),
+                            int(dim), FORMS[form])
+
+
+def _device(device):
+    device = torch.device(device)
+    if device.type == "cuda" and device.index is None:
+        device = torch.device("cuda", torch.cuda.current_device())
+    return device
+
+
+class _OnStream:
+    """What the front ends share: a configuration, a device, a stream."""
+
+    def _init(self, cfg, device, stream):
+        self.cfg, self.device, self.stream = cfg, _device(device), stream
+        self._cfg = ctypes.byref(cfg)
+        self._lib = L.lib()
+
+    def set_stream(self, stream):
+        """Enqueue on `stream` from now on (None: on the stream current at each call)."""
+        self.stream = stream
+
+    def _s(self):
+        return (self.stream if self.stream is not None else torch.cuda.current_stream(self.device)).cuda_stream
+
+    def _buffer(self, nbytes, what):
+        if nbytes == 0:
+            raise ValueError(f"invalid {what} configuration")
+        return torch.empty(nbytes, dtype=torch.uint8, device=self.device)
+
+    def _ints(self, t, shape, what):
+        if t.device != self.device or t.dtype != torch.int32 or not t.is_contiguous() or tuple(t.shape) != shape:
+            raise ValueError(f"{what} must be a contiguous int32 tensor {list(shape)} on {self.device}")
+
+
+def _view(buf, ptr, dtype, shape):
+    off = ptr - buf.data_ptr()
+    count = math.prod(shape) * dtype.itemsize
+    return buf[off:off + count].view(dtype).view(shape)
+
+
+class KvStep(_OnStream):
+    """A planned window, on the GPU:
+
+    counters [8]  after the window: ring's head, free pages; the window's
+                  tokens, requests refused, pages taken, pages given back
+    lengths [R]   after the window, granted [R] new tokens that got slots
+    starts [R+1]  first row of each request in the window's tensors
+    slots [max_tokens] int64, -1 where nothing is stored
+    """
+
+    def __init__(self, cfg, max_tokens, max_new=None, device="cuda"):
+        self._init(cfg, device, None)
+        self.max_tokens = int(max_tokens)
+        if not 1 <= self.max_tokens <= 1 << 30:
+            raise ValueError("max_tokens must be in 1..2^30")
+        self.set_max_new(max_new)
+        self.nbytes = self._lib.agft_kv_step_bytes(self._cfg, self.max_tokens)
+        self.buffer = self._buffer(self.nbytes, "cache")
+        self.ptr = self.buffer.data_ptr()
+        v = L.agft_kv_step_view()
+        L.check("agft_kv_step_at", self._lib.agft_kv_step_at(self._cfg, self.max_tokens, self.ptr, self.nbytes,
+                                                             ctypes.byref(v)))
+        R = cfg.requests
+        self.counters = _view(self.buffer, v.counters, torch.int32, (8,))
+        self.lengths = _view(self.buffer, v.lengths, torch.int32, (R,))
+        self.granted = _view(self.buffer, v.granted, torch.int32, (R,))
+        self.starts = _view(self.buffer, v.starts, torch.int32, (R + 1,))
+        self.slots = _view(self.buffer, v.slots, torch.int64, (self.max_tokens,))
+        self._work = None
+
+    def set_max_new(self, max_new):
+        """No request brings more new tokens than this (None: max_tokens)."""
+        self.max_new = self.max_tokens if max_new is None else int(max_new)
+        if not 1 <= self.max_new <= self.max_tokens:
+            raise ValueError("max_new must be in 1..max_tokens")
+
+    def work(self):
+        """The attention's workspace, shared by the layers, which run one after another."""
+        if self._work is None:
+            self._work = self._buffer(self._lib.agft_kv_attend_bytes(self._cfg, self.max_tokens), "cache")
+        return self._work
+
+
+class KvTables(_OnStream):
+    """Block tables, lengths and the ring of free pages of a node's requests:
+    counters [8], lengths [R], table [R][row_pages], ring [pages] (int32)."""
+
+    def __init__(self, cfg, device="cuda", stream=None):
+        self._init(cfg, device, stream)
+        self.nbytes = self._lib.agft_kv_tables_bytes(self._cfg)
+        self.buffer = self._buffer(self.nbytes, "cache")
+        self.ptr = self.buffer.data_ptr()
+        v = L.agft_kv_tables_view()
+        L.check("agft_kv_tables_at", self._lib.agft_kv_tables_at(self._cfg, self.ptr, self.nbytes, ctypes.byref(v)))
+        self.counters = _view(self.buffer, v.counters, torch.int32, (8,))
+        self.lengths = _view(self.buffer, v.lengths, torch.int32, (cfg.requests,))
+        self.table = _view(self.buffer, v.table, torch.int32, (cfg.requests, cfg.row_pages))
+        self.ring = _view(self.buffer, v.ring, torch.int32, (cfg.pages,))
+        self.reset()
+
+    def reset(self):
+        """No request holds a token, every page is free."""
+        L.check("agft_kv_reset", self._lib.agft_kv_reset(self._cfg, self.ptr, self.nbytes, self._s()))
+
+    def load(self, lengths, table, free):
+        """Take over the tables of a running node: lengths [R], table
+        [R][row_pages] and the free pages in the order of their use (int32).
+        Set-up: checks the values, which waits for the GPU."""
+        cfg = self.cfg
+        self._ints(lengths, (cfg.requests,), "lengths")
+        self._ints(table, (cfg.requests, cfg.row_pages), "table")
+        if free.dim() != 1 or free.numel() > cfg.pages:
+            raise ValueError("free must list at most the pool's pages")
+        self._ints(free, (free.numel(),), "free")
+        for t, top, what in ((lengths, cfg.row_pages * cfg.page + 1, "lengths"), (table, cfg.pages, "table"),
+                             (free, cfg.pages, "free")):
+            if t.numel() and (int(t.min()) < 0 or int(t.max()) >= top):
+                raise ValueError(f"{what} out of range")
+        stream = self.stream if self.stream is not None else torch.cuda.current_stream(self.device)
+        torch.cuda.current_stream(self.device).synchronize()
+        with torch.cuda.stream(stream):
+            self.lengths.copy_(lengths)
+            self.table.copy_(table)
+            self.ring.zero_()
+            self.ring[:free.numel()].copy_(free)
+            self.counters.zero_()
+            self.counters[1:2].fill_(free.numel())
+        stream.synchronize()
+
+    def plan(self, add, max_tokens, max_new=None, step=None):
+        """Plan a window: add [R] int32 new tokens per request (0: none, < 0: it
+        ends), at most max_tokens in all and max_new per request (bounds the
+        host knows).  step: a KvStep of the same max_tokens to write again."""
+        self._ints(add, (self.cfg.requests,), "add")
+        if step is None:
+            step = KvStep(self.cfg, max_tokens, max_new, self.device)
+        elif step.max_tokens != max_tokens:
+            raise ValueError(f"step is for {step.max_tokens} tokens, not {max_tokens}")
+        else:
+            step.set_max_new(max_new)
+        code = self._lib.agft_kv_plan(self._cfg, self.ptr, self.nbytes, add.data_ptr(), step.ptr, step.nbytes,
+                                      step.max_tokens, self._s())
+        if code != L.AGFT_OK:
+            L.check("agft_kv_plan", code)
+        return step
+
+    def commit(self, step):
+        """The planned window's lengths and free pages become the tables'."""
+        L.check("agft_kv_commit", self._lib.agft_kv_commit(self._cfg, self.ptr, self.nbytes, step.ptr, step.nbytes,
+                                                           step.max_tokens, self._s()))
+
+
+class KvCache(_OnStream):
+    """One layer's pages: 8-bit codes and an exponent per page, head and side."""
+
+    def __init__(self, cfg, device="cuda", stream=None):
+        self._init(cfg, device, stream)
+        self.nbytes = self._lib.agft_kv_cache_bytes(self._cfg)
+        self.buffer = self._buffer(self.nbytes, "cache")
+        self.ptr = self.buffer.data_ptr()
+        count = cfg.pages * cfg.heads * 2
+        # codes by blocks (agft_kv.h), exponents behind them
+        self.codes = self.buffer[:count * cfg.page * cfg.dim].view(cfg.pages, cfg.heads, 2, cfg.page * cfg.dim)
+        at = -(-count * cfg.page * cfg.dim // 256) * 256
+        self.exps = self.buffer[at:at + 4 * count].view(torch.int32).view(cfg.pages, cfg.heads, 2)
+
+    def load(self, codes, exps):
+        """Take over codes uint8 [pages][heads][2][page][dim] (keys, values) and
+        exponents int32 [pages][heads][2].  Set-up: waits for the GPU."""
+        c = self.cfg
+        if codes.dtype != torch.uint8 or tuple(codes.shape) != (c.pages, c.heads, 2, c.page, c.dim):
+            raise ValueError("codes must be uint8 [pages][heads][2][page][dim]")
+        if exps.dtype != torch.int32 or tuple(exps.shape) != (c.pages, c.heads, 2):
+            raise ValueError("exps must be int32 [pages][heads][2]")
+        self._dev(codes), self._dev(exps)
+        stream = self.stream if self.stream is not None else torch.cuda.current_stream(self.device)
+        torch.cuda.current_stream(self.device).synchronize()
+        with torch.cuda.stream(stream):
+            self.exps.copy_(exps)
+            part = max(1, (1 << 28) // (c.heads * 2 * c.page * c.dim))
+            for p in range(0, c.pages, part):
+                q = min(c.pages, p + part)
+                lead = (q - p, c.heads, c.page // 16)
+                k = codes[p:q, :, 0].reshape(*lead, 16, c.dim // 64, 4, 16)
+                self.codes[p:q, :, 0] = k.permute(0, 1, 2, 4, 5, 3, 6).reshape(q - p, c.heads, -1)
+                v = codes[p:q, :, 1].reshape(*lead, 4, 4, c.dim // 64, 4, 16)
+                self.codes[p:q, :, 1] = v.permute(0, 1, 2, 5, 3, 7, 6, 4).reshape(q - p, c.heads, -1)
+        stream.synchronize()
+
+    def _dev(self, t):
+        if t.device != self.device:
+            raise ValueError(f"expected a tensor on {self.device}")
+
+    def _dense(self, t, heads, rows, what, types=TYPES):
+        """The agft_kv_dense of a [tokens][heads][dim] tensor of at least `rows` tokens."""
+        shape, strides = t.shape, t.stride()
+        if (t.device != self.device or t.dtype not in types or len(shape) != 3 or shape[0] < rows or
+                shape[1] != heads or shape[2] != self.cfg.dim or strides[2] != 1):
+            raise ValueError(f"{what} must be [{rows} or more][{heads}][{self.cfg.dim}] on {self.device}, "
+                             f"{' or '.join(str(d) for d in types)}, with contiguous numbers of a head")
+        per = 16 // t.element_size()
+        if t.data_ptr() % 16 or strides[0] % per or strides[1] % per:
+            raise ValueError(f"{what}: rows must start at multiples of 16 bytes")
+        return L.agft_kv_dense(t.data_ptr(), strides[0], strides[1], types[t.dtype])
+
+    def append(self, step, k, v):
+        """Store the window's keys and values, [max_tokens][heads][dim] each
+        (bf16, fp16 or fp32), rows as in step.starts."""
+        H, n = self.cfg.heads, step.max_tokens
+        if k.dtype != v.dtype:
+            raise ValueError("k and v must have one type")
+        dk, dv = self._dense(k, H, n, "k"), self._dense(v, H, n, "v")
+        code = self._lib.agft_kv_append(self._cfg, self.ptr, self.nbytes, step.ptr, step.nbytes, n, ctypes.byref(dk),
+                                        ctypes.byref(dv), self._s())
+        if code != L.AGFT_OK:
+            L.check("agft_kv_append", code)
+
+    def attend(self, tables, step, q, out=None, lse=None, scale=None):
+        """softmax(scale q K^T) V of the window's tokens over their requests'
+        tokens up to themselves.  q, out [max_tokens][heads * group][dim], bf16
+        or fp16 (out is allocated if None); lse float32
+        [max_tokens][heads * group] or None receives the logarithms of the sums;
+        scale: 1 / sqrt(dim) if None."""
+        c, n = self.cfg, step.max_tokens
+        hq = c.heads * c.group
+        if out is None:
+            out = torch.empty(n, hq, c.dim, dtype=q.dtype, device=self.device)
+        elif out.dtype != q.dtype:
+            raise ValueError("q and out must have one type")
+        dq, do = self._dense(q, hq, n, "q", HALVES), self._dense(out, hq, n, "out", HALVES)
+        if lse is not None and (lse.device != self.device or lse.dtype != torch.float32 or
+                                lse.shape != (n, hq) or not lse.is_contiguous()):
+            raise ValueError(f"lse must be a contiguous float32 tensor [{n}][{hq}] on {self.device}")
+        work = step.work()
+        code = self._lib.agft_kv_attend(self._cfg, self.ptr, self.nbytes, tables.ptr, tables.nbytes, step.ptr,
+                                        step.nbytes, n, step.max_new, ctypes.byref(dq), ctypes.byref(do),
+                                        None if lse is None else lse.data_ptr(),
+                                        1.0 / math.sqrt(c.dim) if scale is None else float(scale), work.data_ptr(),
+                                        work.numel(), self._s())
+        if code != L.AGFT_OK:
+            L.check("agft_kv_attend", code)
+        return out
+
+    def export(self, slots, dtype=torch.bfloat16):
+        """Keys and values of the slots [n] (int64; -1 gives zeros) as two
+        tensors [n][heads][dim] of dtype."""
+        if slots.device != self.device or slots.dtype != torch.int64 or slots.dim() != 1 or not slots.is_contiguous():
+            raise ValueError(f"slots must be a contiguous int64 tensor [n] on {self.device}")
+        if dtype not in TYPES:
+            raise ValueError(f"no exports in {dtype}")
+        n, H, D = slots.numel(), self.cfg.heads, self.cfg.dim
+        k = torch.empty(n, H, D, dtype=dtype, device=self.device)
+        v = torch.empty(n, H, D, dtype=dtype, device=self.device)
+        if n:
+            dk = L.agft_kv_dense(k.data_ptr(), H * D, D, TYPES[dtype])
+            dv = L.agft_kv_dense(v.data_ptr(), H * D, D, TYPES[dtype])
+            code = self._lib.agft_kv_export(self._cfg, self.ptr, self.nbytes, slots.data_ptr(), n, ctypes.byref(dk),
+                                            ctypes.byref(dv), self._s())
+            if code != L.AGFT_OK:
+                L.check("agft_kv_export", code)
+        return k, v
+
+
+HALVES = {t: c for t, c in TYPES.items() if t != torch.float32}
