@@ -89,7 +89,9 @@ __global__ __launch_bounds__(kScanThreads) void agft_kv_scan_kernel(PlanArgs p) 
         const bool few = (int64_t)rows * p.group <= kFewRows;
         int32_t v[6];
         v[0] = ok ? pages_of(after, p.page, p.shift) - (a.past >> p.shift) : 0;            // pages written to
-        v[1] = rows == 0 || !few ? 0 : ok ? (after + kUnit - 1) / kUnit : 1;               // units of few rows
+        // units of few rows: every 16 rows read the request's tokens (one unit where there are none)
+        v[1] = rows == 0 || !few ? 0
+                                 : (ok ? (after + kUnit - 1) / kUnit : 1) * ((rows * p.group + kRowTile - 1) / kRowTile);
         v[2] = rows == 0 || few ? 0 : (int32_t)(((int64_t)rows * p.group + kTileRows - 1) / kTileRows);
         v[3] = a.ends ? a.held : 0;
         v[4] = live && a.add > 0 && !ok ? 1 : 0;

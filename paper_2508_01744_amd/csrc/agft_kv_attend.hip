@@ -14,7 +14,7 @@ namespace agft_kv_detail {
 struct AttendArgs {
     const char *codes;
     const int32_t *exps, *table;
-    const int32_t *starts, *granted, *lengths, *work;
+    const int32_t *starts, *granted, *lengths, *work, *tiles;
     const char *q;
     char *out;
     float *lse, *partial;
@@ -139,12 +139,13 @@ __device__ __forceinline__ float across_sum(float x) {
 
 // ---- few query rows: shared out over the cached tokens ----
 //
-// The work is the list of units (64 tokens of one request and head) of the
-// requests with at most 16 query rows, requests outermost; every workgroup
+// The work is the list of units (64 tokens of one request, for one head's 16
+// query rows) of the requests with at most 64 query rows per head, requests
+// outermost, then heads, then rows; every workgroup
 // takes an equal stretch of it, so the split does not depend on how the lengths
-// are spread.  A stretch's part of one request and head (a segment) is cut among
-// the wavefronts, each keeping its own maximum and sums, and joined in LDS; a
-// request and head that several workgroups share leaves partial sums, joined by
+// are spread.  A stretch's part of one request's 16 rows (a segment) is cut among
+// the wavefronts, each keeping its own maximum and sums, and joined in LDS; rows
+// that several workgroups share leave partial sums, joined by
 // agft_kv_join_kernel in the order of the workgroups.
 //
 // Scores are made transposed, S^T = K Q^T (16 tokens x 16 rows per matrix
@@ -173,9 +174,34 @@ __device__ __forceinline__ Stretch stretch_of(const AttendArgs &p) {
     return s;
 }
 
+// The rows that unit x of the work belongs to, and its place among their units.
+struct Segment {
+    int request, head, row, first, rows, units, at;
+};
+__device__ __forceinline__ Segment segment_of(const AttendArgs &p, int32_t x) {
+    Segment s;
+    s.request = find_last(p.work, p.requests, x / p.heads);
+    const int32_t base = p.work[s.request], all = p.work[s.request + 1] - base;
+    s.first = p.starts[s.request];
+    const int rows = (p.starts[s.request + 1] - s.first) * p.group;
+    const int tiles = (rows + kRowTile - 1) / kRowTile;
+    if (all <= 0 || tiles <= 0 || all < tiles) {
+        s.units = 0;
+        return s;
+    }
+    s.units = all / tiles;
+    const int32_t rest = x - base * p.heads;
+    s.head = rest / all;
+    const int32_t in = rest - s.head * all, tile = in / s.units;
+    s.row = tile * kRowTile;
+    s.rows = rows - s.row < kRowTile ? rows - s.row : kRowTile;
+    s.at = in - tile * s.units;
+    return s;
+}
+
 template <int DIM>
 constexpr int partial_floats() {
-    return kFewRows * (DIM + 2);
+    return kRowTile * (DIM + 2);
 }
 
 template <int TYPE, int DIM>
@@ -198,8 +224,8 @@ __global__ __launch_bounds__(64 * kFewWaves, 2) void agft_kv_few_kernel(AttendAr
     constexpr int ROW = DIM + 4;                  // LDS row, off the banks
     using H = Half<TYPE>;
     using F = Half<AGFT_KV_FP16>;
-    __shared__ float s_o[kFewWaves][kFewRows * ROW];
-    __shared__ float s_m[kFewWaves][kFewRows], s_l[kFewWaves][kFewRows];
+    __shared__ float s_o[kFewWaves][kRowTile * ROW];
+    __shared__ float s_m[kFewWaves][kRowTile], s_l[kFewWaves][kRowTile];
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     const int g = lane >> 4, n = lane & 15;
     const Stretch st = stretch_of(p);
@@ -210,21 +236,19 @@ __global__ __launch_bounds__(64 * kFewWaves, 2) void agft_kv_few_kernel(AttendAr
     const float scale2 = p.scale * kLog2e;
     int32_t x = (int32_t)x_first;
     while (x < x1) {
-        const int i = find_last(p.work, p.requests, x / p.heads);
-        const int32_t base = p.work[i], units = p.work[i + 1] - base;
-        if (units <= 0) break;
-        const int32_t rest = x - base * p.heads;
-        const int head = rest / units, u0 = rest % units;
+        const Segment seg = segment_of(p, x);
+        if (seg.units <= 0) break;
+        const int i = seg.request, head = seg.head, units = seg.units, u0 = seg.at, row0 = seg.row, rows = seg.rows;
+        const int first = seg.first;
         const int count = units - u0 < x1 - x ? units - u0 : x1 - x;
         x += count;
-        const int first = p.starts[i], rows = (p.starts[i + 1] - first) * p.group;
         const int granted = p.granted[i], len = p.lengths[i];
         if (granted <= 0) {
             // no slots, no keys
             for (int c = threadIdx.x; c < rows * DIM / 4; c += blockDim.x) {
                 const int r = c / (DIM / 4), d = c % (DIM / 4) * 4;
-                store_row4<TYPE, DIM>(p, first, head, r, d, (float4v){0, 0, 0, 0}, 0.0f);
-                if (d == 0) store_lse(p, first, head, r, -INFINITY, 0.0f);
+                store_row4<TYPE, DIM>(p, first, head, row0 + r, d, (float4v){0, 0, 0, 0}, 0.0f);
+                if (d == 0) store_lse(p, first, head, row0 + r, -INFINITY, 0.0f);
             }
             continue;
         }
@@ -232,7 +256,7 @@ __global__ __launch_bounds__(64 * kFewWaves, 2) void agft_kv_few_kernel(AttendAr
         typename H::x8 q[DG * 2];
         const bool row_here = n < rows;
         {
-            const int tk = n / p.group, hq = head * p.group + n % p.group;
+            const int tk = (row0 + n) / p.group, hq = head * p.group + (row0 + n) % p.group;
             const char *src = p.q + ((int64_t)(first + tk) * p.q_token + hq * p.q_head) * 2;
 #pragma unroll
             for (int c = 0; c < DG * 2; ++c) {
@@ -241,8 +265,8 @@ __global__ __launch_bounds__(64 * kFewWaves, 2) void agft_kv_few_kernel(AttendAr
                 q[c] = __builtin_bit_cast(typename H::x8, v);
             }
         }
-        const int limit = row_here ? len - granted + n / p.group + 1 : len;     // keys that row n sees
-        const int least = len - granted + 1;                                    // keys that every row sees
+        const int limit = row_here ? len - granted + (row0 + n) / p.group + 1 : len;   // keys that row n sees
+        const int least = len - granted + row0 / p.group + 1;                          // keys that every row sees
         const int blocks = (len + kBlockTokens - 1) / kBlockTokens;
         const char *codes = p.codes + (int64_t)head * 2 * p.page * DIM;
         const int sub_mask = (p.page >> 4) - 1;
@@ -380,34 +404,32 @@ __global__ __launch_bounds__(64 * kFewWaves, 2) void agft_kv_few_kernel(AttendAr
                 ll = fmaf(s_l[w][r], f, ll);
             }
             if (whole) {
-                store_row4<TYPE, DIM>(p, first, head, r, d, oo, ll);
-                if (d == 0) store_lse(p, first, head, r, mm, ll);
+                store_row4<TYPE, DIM>(p, first, head, row0 + r, d, oo, ll);
+                if (d == 0) store_lse(p, first, head, row0 + r, mm, ll);
             } else {
                 *reinterpret_cast<float4v *>(part + r * DIM + d) = oo;
-                if (d == 0) part[kFewRows * DIM + r] = mm, part[kFewRows * (DIM + 1) + r] = ll;
+                if (d == 0) part[kRowTile * DIM + r] = mm, part[kRowTile * (DIM + 1) + r] = ll;
             }
         }
         __syncthreads();
     }
 }
 
-// Partial sums of the request and head whose first unit lies in this
-// workgroup's stretch and whose last does not; a wavefront per row.
+// Partial sums of the rows whose first unit lies in this workgroup's stretch
+// and whose last does not; a wavefront per row.
 template <int TYPE, int DIM>
 __global__ __launch_bounds__(256) void agft_kv_join_kernel(AttendArgs p) {
     const Stretch st = stretch_of(p);
     const int64_t x_first = (int64_t)blockIdx.x * st.share;
     if (x_first + st.share >= st.total) return;
     const int32_t x1 = (int32_t)x_first + st.share;               // the next stretch's first unit
-    const int i = find_last(p.work, p.requests, (x1 - 1) / p.heads);
-    const int32_t base = p.work[i], units = p.work[i + 1] - base;
-    if (units <= 0) return;
-    const int head = (x1 - 1 - base * p.heads) / units;
-    const int32_t from = base * p.heads + head * units;
-    if (from < x_first || from + units <= x1) return;
-    if (p.granted[i] <= 0) return;
-    const int first = p.starts[i], rows = (p.starts[i + 1] - first) * p.group;
-    const int last = (from + units - 1) / st.share;               // the workgroup with the last unit
+    const Segment seg = segment_of(p, x1 - 1);
+    if (seg.units <= 0) return;
+    const int32_t from = x1 - 1 - seg.at;
+    if (from < x_first || from + seg.units <= x1) return;
+    if (p.granted[seg.request] <= 0) return;
+    const int head = seg.head, first = seg.first, row0 = seg.row, rows = seg.rows;
+    const int last = (from + seg.units - 1) / st.share;           // the workgroup with the last unit
     const int lane = threadIdx.x & 63;
     const int r = blockIdx.y * 4 + (threadIdx.x >> 6);
     if (r >= rows) return;
@@ -421,7 +443,7 @@ __global__ __launch_bounds__(256) void agft_kv_join_kernel(AttendArgs p) {
     float4v oo = {0, 0, 0, 0};
     for (int w = blockIdx.x + ph; w <= last; w += STEP) {
         const float *a = piece(w);
-        const float m = a[kFewRows * DIM + r], l = a[kFewRows * (DIM + 1) + r];
+        const float m = a[kRowTile * DIM + r], l = a[kRowTile * (DIM + 1) + r];
         const float4v o = *reinterpret_cast<const float4v *>(a + r * DIM + d);
         const float m1 = fmaxf(mm, m);
         const float f0 = mm == -INFINITY ? 0.0f : exp2f(mm - m1), f1 = m == -INFINITY ? 0.0f : exp2f(m - m1);
@@ -444,79 +466,212 @@ __global__ __launch_bounds__(256) void agft_kv_join_kernel(AttendArgs p) {
         mm = m1;
     }
     if (ph == 0) {
-        store_row4<TYPE, DIM>(p, first, head, r, d, oo, ll);
-        if (d == 0) store_lse(p, first, head, r, mm, ll);
+        store_row4<TYPE, DIM>(p, first, head, row0 + r, d, oo, ll);
+        if (d == 0) store_lse(p, first, head, row0 + r, mm, ll);
     }
 }
 
-// One wavefront per token and query head, 64 keys at a time: a lane per key for
-// the scores, a lane per number for the sums.
+// ---- many query rows: tiles of 128 ----
+//
+// A workgroup takes 128 rows (tokens x group) of one request and head, 32 per
+// wavefront, and goes over the tokens 64 at a time.  The codes come from HBM
+// straight to LDS, one tile ahead, each wavefront fetching one block of 16
+// tokens; the wavefronts turn them into 16 bits on the way to the matrix
+// instructions (32 x 32 x 16).  As above, S^T = K Q^T and O^T = V^T P^T, so a
+// row's probabilities stay in the lanes that made them.  The longest tiles
+// start first, and consecutive workgroups take consecutive heads, so that (with
+// 8 heads) an XCD's L2 holds one head's tokens.
+typedef float float16v __attribute__((ext_vector_type(16)));
+
+template <int TYPE>
+__device__ __forceinline__ float16v mfma32(typename Half<TYPE>::x8 a, typename Half<TYPE>::x8 b, float16v c) {
+    if constexpr (TYPE == AGFT_KV_BF16) return __builtin_amdgcn_mfma_f32_32x32x16_bf16(a, b, c, 0, 0, 0);
+    else return __builtin_amdgcn_mfma_f32_32x32x16_f16(a, b, c, 0, 0, 0);
+}
+
+constexpr int kTileWaves = 4;
+constexpr int kTileKeys = 64;
+constexpr float kSlack = 8.0f;    // powers of two that a maximum may grow before the sums are rescaled
+
 template <int FORM, int TYPE, int DIM>
-__global__ __launch_bounds__(64) void agft_kv_attend_kernel(AttendArgs p) {
-    __shared__ float s_q[DIM], s_p[64];
-    const int lane = threadIdx.x;
-    const int t = blockIdx.x, hq = blockIdx.y, head = hq / p.group;
-    if (t >= p.starts[p.requests]) return;
-    int lo = 0, hi = p.requests;
-    while (hi - lo > 1) {
-        const int mid = (lo + hi) >> 1;
-        if (p.starts[mid] <= t) lo = mid;
-        else hi = mid;
+__global__ __launch_bounds__(64 * kTileWaves, DIM > 128 ? 1 : 2) void agft_kv_tile_kernel(AttendArgs p) {
+    constexpr int DG = DIM / kBlockDims;
+    constexpr int SIDE = kBlockBytes * DG;                 // one block's keys (or values)
+    using H = Half<TYPE>;
+    using F = Half<AGFT_KV_FP16>;
+    __shared__ __attribute__((aligned(16))) char s_codes[2][4][2][SIDE];   // buffer, block, side
+    __shared__ int2 s_exps[2][4];
+    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    const int h = lane >> 5, n = lane & 31, m16 = lane & 15, b16 = (lane >> 4) & 1;
+    const int head = blockIdx.x % p.heads;
+    const int back = blockIdx.x / p.heads, total = p.tiles[p.requests];
+    if (back >= total) return;
+    const int tile = total - 1 - back;
+    const int i = find_last(p.tiles, p.requests, tile);
+    const int first = p.starts[i], all_rows = (p.starts[i + 1] - first) * p.group;
+    const int granted = p.granted[i], len = p.lengths[i];
+    const int row0 = (tile - p.tiles[i]) * kTileRows;
+    const int rows = all_rows - row0 < kTileRows ? all_rows - row0 : kTileRows;
+    if (rows <= 0) return;
+    if (granted <= 0) {
+        for (int c = threadIdx.x; c < rows * DIM / 4; c += blockDim.x) {
+            const int r = c / (DIM / 4), d = c % (DIM / 4) * 4;
+            store_row4<TYPE, DIM>(p, first, head, row0 + r, d, (float4v){0, 0, 0, 0}, 0.0f);
+            if (d == 0) store_lse(p, first, head, row0 + r, -INFINITY, 0.0f);
+        }
+        return;
     }
-    const int i = lo, n = p.granted[i];
-    if ((p.starts[i + 1] - p.starts[i]) * p.group <= kFewRows) return;
-    const int keys = n > 0 ? p.lengths[i] - n + (t - p.starts[i]) + 1 : 0;
-    for (int d = lane; d < DIM; d += 64) s_q[d] = Half<TYPE>::load(p.q, t * p.q_token + hq * p.q_head + d);
-    __syncthreads();
-    float m = -INFINITY, l = 0.0f, acc[DIM / 64] = {};
-    for (int j0 = 0; j0 < keys; j0 += 64) {
-        const int j = j0 + lane;
-        float s = -INFINITY;
-        if (j < keys) {
-            const int64_t page_id = (uint32_t)p.table[(int64_t)i * p.row_pages + (j >> p.shift)] % (uint32_t)p.pages;
-            const int pos = j & (p.page - 1);
-            const char *block = p.codes + (page_id * p.heads + head) * 2 * p.page * DIM + (pos >> 4) * 16 * DIM;
-            float dot = 0.0f;
-            for (int c = 0; c < DIM / 16; ++c) {
-                const uint32_t *w = reinterpret_cast<const uint32_t *>(block + c / 4 * kBlockBytes + ((c % 4) * 16 + (pos & 15)) * 16);
-                for (int b = 0; b < 4; ++b) {
-                    float x[4];
-                    Code<FORM>::unpack4(w[b], x);
-                    for (int z = 0; z < 4; ++z) dot += x[z] * s_q[c * 16 + b * 4 + z];
+    const int past = len - granted;
+    const int wrow = row0 + 32 * wave;                     // this wavefront's rows
+    const bool busy = 32 * wave < rows, row_here = 32 * wave + n < rows;
+    const int row = row_here ? wrow + n : row0 + rows - 1;
+    const int limit = past + row / p.group + 1;            // keys that this lane's row sees
+    const int least = past + wrow / p.group + 1;           // keys that every row of the wavefront sees
+    const int wlast = 32 * wave + 31 < rows ? wrow + 31 : row0 + rows - 1;
+    const int most = busy ? past + wlast / p.group + 1 : 0;
+    const int keys = past + (row0 + rows - 1) / p.group + 1;
+    const int tiles = (keys + kTileKeys - 1) / kTileKeys;
+    const int blocks = (len + kBlockTokens - 1) / kBlockTokens;
+
+    typename H::x8 q[DG * 4];
+    {
+        const int tk = row / p.group, hq = head * p.group + row % p.group;
+        const char *src = p.q + ((int64_t)(first + tk) * p.q_token + hq * p.q_head) * 2;
+#pragma unroll
+        for (int c = 0; c < DG * 4; ++c)                   // numbers 64 dg + 16 (2 c + h) + 8 e.. + 7
+            q[c] = __builtin_bit_cast(typename H::x8, *reinterpret_cast<const uint4v *>(
+                       src + ((c >> 2) * kBlockDims + 16 * (2 * ((c >> 1) & 1) + h) + 8 * (c & 1)) * 2));
+    }
+    const float scale2 = p.scale * kLog2e;
+    const int64_t page_bytes = (int64_t)p.heads * 2 * p.page * DIM;
+    const char *codes = p.codes + (int64_t)head * 2 * p.page * DIM;
+    const int sub_mask = (p.page >> 4) - 1;
+
+    // a lane per tile: the page and exponents of this wavefront's block of it
+    int id = 0;
+    int2 ee = make_int2(0, 0);
+    const auto look_up = [&](int t0) {
+        int b = (t0 + lane) * 4 + wave;
+        if (b >= blocks) b = blocks - 1;
+        uint32_t z = (uint32_t)p.table[(int64_t)i * p.row_pages + ((b << 4) >> p.shift)];
+        if (z >= (uint32_t)p.pages) z = (uint32_t)p.pages - 1;
+        id = (int)z;
+        ee = *reinterpret_cast<const int2 *>(p.exps + ((int64_t)id * p.heads + head) * 2);
+    };
+    const auto fetch = [&](int t, int buf) {
+        if ((t & 63) == 0) look_up(t);
+        int b = t * 4 + wave;
+        if (b >= blocks) b = blocks - 1;
+        const int64_t page_id = __builtin_amdgcn_readlane(id, t & 63);
+        const char *src = codes + page_id * page_bytes + (b & sub_mask) * (16 * DIM) + lane * 16;
+#pragma unroll
+        for (int side = 0; side < 2; ++side)
+#pragma unroll
+            for (int dg = 0; dg < DG; ++dg)
+                __builtin_amdgcn_global_load_lds(
+                    (const __attribute__((address_space(1))) void *)(src + side * p.page * DIM + dg * kBlockBytes),
+                    (__attribute__((address_space(3))) void *)&s_codes[buf][wave][side][dg * kBlockBytes],
+                    16, 0, 0);
+        if (lane == (t & 63)) s_exps[buf][wave] = ee;
+    };
+
+    float m = -INFINITY, l = 0.0f;
+    float16v o[DG * 2];
+#pragma unroll
+    for (int c = 0; c < DG * 2; ++c)
+#pragma unroll
+        for (int j = 0; j < 16; ++j) o[c][j] = 0.0f;
+
+    fetch(0, 0);
+    for (int t = 0; t < tiles; ++t) {
+        const int buf = t & 1;
+        __builtin_amdgcn_s_waitcnt(0x0f70);                // this wavefront's codes have landed: vmcnt(0)
+        __syncthreads();                                   // everybody's have, and the other buffer is read
+        if (t + 1 < tiles) fetch(t + 1, buf ^ 1);
+        const int key0 = t * kTileKeys;
+        if (key0 >= most) continue;
+        float16v s[2];
+#pragma unroll
+        for (int half = 0; half < 2; ++half) {
+#pragma unroll
+            for (int j = 0; j < 16; ++j) s[half][j] = 0.0f;
+#pragma unroll
+            for (int c = 0; c < DG * 2; ++c) {             // 16-byte entry 16 (2 (c % 2) + h) + m16 of block 2 half + b16
+                const uint4v k = *reinterpret_cast<const uint4v *>(
+                    &s_codes[buf][2 * half + b16][0][(c >> 1) * kBlockBytes + (16 * (2 * (c & 1) + h) + m16) * 16]);
+                s[half] = mfma32<TYPE>(H::template decode<FORM>(k[0], k[1]), q[2 * c], s[half]);
+                s[half] = mfma32<TYPE>(H::template decode<FORM>(k[2], k[3]), q[2 * c + 1], s[half]);
+            }
+        }
+        float pow_back[4];
+#pragma unroll
+        for (int b = 0; b < 4; ++b) {
+            const int2 e = s_exps[buf][b];
+            const float ks = scale2 * pow2(e.x), ev = (float)e.y;
+            pow_back[b] = pow2(-e.y);
+#pragma unroll
+            for (int j = 0; j < 8; ++j) s[b >> 1][8 * (b & 1) + j] = fmaf(s[b >> 1][8 * (b & 1) + j], ks, ev);
+        }
+        if (key0 + kTileKeys > least) {
+#pragma unroll
+            for (int half = 0; half < 2; ++half)
+#pragma unroll
+                for (int j = 0; j < 16; ++j)
+                    if (key0 + 32 * half + 8 * (j >> 2) + 4 * h + (j & 3) >= limit) s[half][j] = -INFINITY;
+        }
+        float top = s[0][0];
+#pragma unroll
+        for (int half = 0; half < 2; ++half)
+#pragma unroll
+            for (int j = 0; j < 16; ++j) top = fmaxf(top, s[half][j]);
+        top = fmaxf(top, __shfl_xor(top, 32, 64));
+        if (__any(top > m + kSlack || m == -INFINITY)) {
+            const float m1 = fmaxf(m, top);
+            const float fall = m == -INFINITY ? 0.0f : exp2f(m - m1);
+            m = m1;
+            l *= fall;
+#pragma unroll
+            for (int c = 0; c < DG * 2; ++c) o[c] *= fall;
+        }
+        const float off = m == -INFINITY ? 0.0f : m;
+        const bool tail = key0 + kTileKeys > len;
+#pragma unroll
+        for (int b = 0; b < 4; ++b) {
+            float e[8];
+#pragma unroll
+            for (int j = 0; j < 8; ++j) e[j] = __builtin_amdgcn_exp2f(s[b >> 1][8 * (b & 1) + j] - off);
+            l = fmaf(((e[0] + e[1]) + (e[2] + e[3])) + ((e[4] + e[5]) + (e[6] + e[7])), pow_back[b], l);
+            fp16x8 pr;
+#pragma unroll
+            for (int j = 0; j < 8; ++j) pr[j] = (_Float16)e[j];
+            uint32_t keep[2] = {~0u, ~0u};
+            if (tail) {
+                // codes past the request's tokens may be anything, NaN too
+#pragma unroll
+                for (int z = 0; z < 2; ++z) {
+                    const int valid = len - (key0 + 16 * b + 8 * z + 4 * h);
+                    keep[z] = valid >= 4 ? ~0u : valid <= 0 ? 0u : (1u << (8 * valid)) - 1u;
                 }
             }
-            s = dot * p.scale * pow2(p.exps[(page_id * p.heads + head) * 2]);
-        }
-        float top = s;
-        for (int z = 1; z < 64; z *= 2) top = fmaxf(top, __shfl_xor(top, z, 64));
-        const float m1 = fmaxf(m, top), keep = expf(m - m1);
-        const float w = j < keys ? expf(s - m1) : 0.0f;
-        float sum = w;
-        for (int z = 1; z < 64; z *= 2) sum += __shfl_xor(sum, z, 64);
-        l = l * keep + sum;
-        m = m1;
-        s_p[lane] = w;
-        __syncthreads();
-        for (int dg = 0; dg < DIM / 64; ++dg) acc[dg] *= keep;
-        for (int k = 0; k < 64 && j0 + k < keys; ++k) {
-            const int jj = j0 + k;
-            const int64_t page_id = (uint32_t)p.table[(int64_t)i * p.row_pages + (jj >> p.shift)] % (uint32_t)p.pages;
-            const int pos = jj & (p.page - 1), mm = pos & 15;
-            const int64_t base = (page_id * p.heads + head) * 2 + 1;
-            const char *block = p.codes + base * p.page * DIM + (pos >> 4) * 16 * DIM;
-            const float f = s_p[k] * pow2(p.exps[base]);
-            for (int dg = 0; dg < DIM / 64; ++dg) {
-                float x[4];
-                Code<FORM>::unpack4((uint8_t)block[dg * kBlockBytes + ((mm >> 2) * 16 + (lane & 15)) * 16 + (lane >> 4) * 4 + (mm & 3)], x);
-                acc[dg] += f * x[0];
+#pragma unroll
+            for (int dg = 0; dg < DG; ++dg) {              // words 2 b16, 2 b16 + 1 of entries 16 h + m16, 16 (h + 2) + m16
+                const char *src = &s_codes[buf][b][1][dg * kBlockBytes + (16 * h + m16) * 16 + 8 * b16];
+                uint2 v0 = *reinterpret_cast<const uint2 *>(src), v1 = *reinterpret_cast<const uint2 *>(src + 512);
+                if (tail) v0.x &= keep[0], v0.y &= keep[0], v1.x &= keep[1], v1.y &= keep[1];
+                o[2 * dg] = mfma32<AGFT_KV_FP16>(F::template decode<FORM>(v0.x, v1.x), pr, o[2 * dg]);
+                o[2 * dg + 1] = mfma32<AGFT_KV_FP16>(F::template decode<FORM>(v0.y, v1.y), pr, o[2 * dg + 1]);
             }
         }
-        __syncthreads();
     }
-    for (int dg = 0; dg < DIM / 64; ++dg)
-        Half<TYPE>::store(p.out, t * p.out_token + hq * p.out_head + dg * 64 + lane, keys > 0 ? acc[dg] / l : 0.0f);
-    if (p.lse != nullptr && lane == 0)
-        p.lse[(int64_t)t * p.heads * p.group + hq] = keys > 0 ? m + logf(l) : -INFINITY;
+    l += __shfl_xor(l, 32, 64);
+    if (!row_here) return;
+#pragma unroll
+    for (int c = 0; c < DG * 2; ++c)
+#pragma unroll
+        for (int z = 0; z < 4; ++z)                        // rows 8 z + 4 h.. of O^T: numbers 64 dg + 32 (z / 2) + 16 T + ..
+            store_row4<TYPE, DIM>(p, first, head, row, 64 * (c >> 1) + 32 * (z >> 1) + 16 * (c & 1) + 8 * (z & 1) + 4 * h,
+                                  (float4v){o[c][4 * z], o[c][4 * z + 1], o[c][4 * z + 2], o[c][4 * z + 3]}, l);
+    if (h == 0) store_lse(p, first, head, row, m, l);
 }
 
 inline int log2_of(int32_t page) { return page == 16 ? 4 : page == 32 ? 5 : page == 64 ? 6 : 7; }
@@ -529,7 +684,7 @@ extern "C" {
 
 size_t agft_kv_attend_bytes(const agft_kv_config *cfg, int32_t max_tokens) {
     if (config_status(cfg) != AGFT_OK || !tokens_ok(max_tokens)) return 0;
-    return align_up((size_t)kFewGroups * 2 * kFewRows * (cfg->dim + 2) * sizeof(float));
+    return align_up((size_t)kFewGroups * 2 * kRowTile * (cfg->dim + 2) * sizeof(float));
 }
 
 int agft_kv_attend(const agft_kv_config *cfg, const void *d_cache, size_t cache_bytes, const void *d_tables,
@@ -554,6 +709,7 @@ int agft_kv_attend(const agft_kv_config *cfg, const void *d_cache, size_t cache_
     p.table = tv.table;
     p.starts = sv.starts, p.granted = sv.granted, p.lengths = sv.lengths;
     p.work = reinterpret_cast<const int32_t *>(static_cast<const char *>(d_step) + step_layout(cfg, max_tokens).work);
+    p.tiles = reinterpret_cast<const int32_t *>(static_cast<const char *>(d_step) + step_layout(cfg, max_tokens).tiles);
     p.partial = static_cast<float *>(d_work);
     p.q = static_cast<const char *>(q->data), p.out = static_cast<char *>(out->data), p.lse = d_lse;
     p.q_token = q->token_stride, p.q_head = q->head_stride;
@@ -561,16 +717,20 @@ int agft_kv_attend(const agft_kv_config *cfg, const void *d_cache, size_t cache_
     p.scale = scale;
     p.requests = cfg->requests, p.row_pages = cfg->row_pages, p.pages = cfg->pages;
     p.page = cfg->page, p.shift = log2_of(cfg->page), p.heads = cfg->heads, p.group = cfg->group;
-    const dim3 grid((unsigned)max_tokens, (unsigned)(cfg->heads * cfg->group));
+    // tiles of many rows: the rows' own and a last one of each request that has more than kFewRows
+    const int64_t all_rows = (int64_t)max_tokens * cfg->group;
+    const int64_t many = all_rows / (kFewRows + 1) < cfg->requests ? all_rows / (kFewRows + 1) : cfg->requests;
+    const int64_t tile_groups = (all_rows / kTileRows + many) * cfg->heads;
+    if (tile_groups > INT32_MAX) return AGFT_E_INVAL;
     const auto go = [&](auto form, auto type, auto dim) {
         const hipStream_t hs = static_cast<hipStream_t>(stream);
         agft_kv_few_kernel<form(), type(), dim()><<<kFewGroups, 64 * kFewWaves, 0, hs>>>(p);
         int code = launched();
         if (code != AGFT_OK) return code;
-        agft_kv_join_kernel<type(), dim()><<<dim3(kFewGroups, kFewRows / 4), 256, 0, hs>>>(p);
+        agft_kv_join_kernel<type(), dim()><<<dim3(kFewGroups, kRowTile / 4), 256, 0, hs>>>(p);
         code = launched();
         if (code != AGFT_OK || (int64_t)max_new * cfg->group <= kFewRows) return code;
-        agft_kv_attend_kernel<form(), type(), dim()><<<grid, 64, 0, hs>>>(p);
+        agft_kv_tile_kernel<form(), type(), dim()><<<(unsigned)tile_groups, 64 * kTileWaves, 0, hs>>>(p);
         return launched();
     };
     const auto dims = [&](auto form, auto type) {

@@ -18,7 +18,8 @@ constexpr int kBlockTokens = 16;   // tokens of a layout block
 constexpr int kBlockDims = 64;     // numbers of a layout block
 constexpr int kBlockBytes = kBlockTokens * kBlockDims;
 constexpr int kUnit = 64;          // tokens of a unit of attention work
-constexpr int kFewRows = 16;       // query rows (tokens x group) of a request that one matrix tile holds
+constexpr int kRowTile = 16;       // query rows (tokens x group) of a tile of the attention over few rows
+constexpr int kFewRows = 64;       // query rows of a request up to which that takes it
 constexpr int kTileRows = 128;     // query rows of a tile of the attention over many rows
 constexpr int kMinExp = -64;
 
