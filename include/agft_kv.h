@@ -109,7 +109,7 @@ typedef struct agft_kv_step_view {
 size_t agft_kv_tables_bytes(const agft_kv_config *cfg);
 size_t agft_kv_step_bytes(const agft_kv_config *cfg, int32_t max_tokens);
 size_t agft_kv_cache_bytes(const agft_kv_config *cfg);
-/* workspace of agft_kv_attend (may be shared by calls that run one after another) */
+/* workspace of agft_kv_attend, whatever it holds */
 size_t agft_kv_attend_bytes(const agft_kv_config *cfg, int32_t max_tokens);
 
 int agft_kv_tables_at(const agft_kv_config *cfg, void *d_tables, size_t nbytes, agft_kv_tables_view *out);
@@ -157,11 +157,13 @@ int agft_kv_append(const agft_kv_config *cfg, void *d_cache, size_t cache_bytes,
  * -infinity.  Rows past the window's tokens are left alone.
  * max_new: no request has more new tokens than this (1..max_tokens); short
  * bounds save launches, a bound that is too low leaves rows unwritten.
- * Products and sums are kept in fp32; probabilities meet the values in q's
- * type (relative to the largest, at most 1).
+ * Products and sums are kept in fp32; probabilities meet the values in fp16,
+ * relative to about the largest one's.
+ * Calls that share a step or a workspace run one after another: partial sums
+ * meet there.  The step's other parts stay as they are.
  */
 int agft_kv_attend(const agft_kv_config *cfg, const void *d_cache, size_t cache_bytes, const void *d_tables,
-                   size_t tables_bytes, const void *d_step, size_t step_bytes, int32_t max_tokens,
+                   size_t tables_bytes, void *d_step, size_t step_bytes, int32_t max_tokens,
                    int32_t max_new, const agft_kv_dense *q, const agft_kv_dense *out, float *d_lse, float scale,
                    void *d_work, size_t work_bytes, void *stream);
 

@@ -17,133 +17,225 @@ struct PlanArgs {
     const int32_t *add;
     const int32_t *counters, *lengths;
     int32_t *table, *ring;
-    int32_t *out_counters, *starts, *granted, *out_lengths, *work, *tiles, *need, *touched, *back, *runs;
+    int32_t *out_counters, *starts, *granted, *out_lengths, *need, *touched, *back, *sums, *arrived, *runs;
+    Work *works;
     int64_t *slots;
     int32_t requests, row_pages, pages, page, shift, group, max_tokens;
 };
 
 __device__ __forceinline__ int32_t pages_of(int32_t n, int32_t page, int32_t shift) { return (n + page - 1) >> shift; }
 
+// ---- tables ----
+//
+// A window's table work is prefix sums over the requests and a search for every
+// token's request: a few hundred KB at most, so latency is all of it.  Up to
+// 1,024 requests every workgroup makes all the prefix sums for itself, in LDS,
+// and then its own 1,024 tokens' slots: one launch, no workgroup waits for
+// another.  Beyond that one launch makes the sums of 1,024 requests per
+// workgroup, and a second adds the other chunks' totals while it makes the
+// slots.
+constexpr int kPlanThreads = 256;
+constexpr int kPlanPer = kPlanChunk / kPlanThreads;    // requests of a thread
+constexpr int kPlanTokens = 1024;                      // tokens of a workgroup
+
 // What a request asks of the window, from its own lengths alone.
 struct Ask {
-    int32_t past, add, held, tokens, need;
-    bool ends;
+    int32_t past, held, need;
+    uint32_t tokens;
+    bool wants, ends;
 };
 
 __device__ __forceinline__ Ask ask_of(const PlanArgs &p, int32_t past, int32_t add) {
     Ask a;
     const int32_t cap = p.row_pages << p.shift;
     a.past = past < 0 ? 0 : past > cap ? cap : past;
-    a.add = add;
+    a.wants = add > 0;
     a.ends = add < 0;
     a.held = pages_of(a.past, p.page, p.shift);
     a.tokens = add > 0 && add <= cap - a.past ? add : 0;
-    a.need = pages_of(a.past + a.tokens, p.page, p.shift) - a.held;
+    a.need = pages_of(a.past + (int32_t)a.tokens, p.page, p.shift) - a.held;
     return a;
 }
 
-template <typename T>
-__device__ __forceinline__ T wave_inclusive(T x) {
-    const int lane = threadIdx.x & 63;
+// Sums of what is asked may pass 32 bits; saturated ones compare alike (every
+// limit is below 2^31), and a saturated sum less one request's share is still
+// above every limit.
+__device__ __forceinline__ uint32_t add_sat(uint32_t a, uint32_t b) { return __builtin_elementwise_add_sat(a, b); }
+
+struct PlanLds {
+    uint32_t asked[2][kPlanThreads / 64];
+    int32_t sums[kPlanSums][kPlanThreads / 64];
+};
+
+// The requests [r0 + kPlanPer * thread, ..) of one thread.
+struct PlanPart {
+    int32_t past[kPlanPer], held[kPlanPer], granted[kPlanPer], after[kPlanPer], first[kPlanPer], need[kPlanPer];
+    int32_t sums[kPlanSums][kPlanPer];      // sums over the chunk's earlier requests
+    int32_t all[kPlanSums];                 // over the chunk
+    uint32_t tokens;                        // asked by the chunk and all before it
+};
+
+// Prefix sums over a chunk, behind requests that ask for need0 pages and tok0 tokens.
+__device__ __forceinline__ void plan_chunk(const PlanArgs &p, int r0, uint32_t need0, uint32_t tok0, int32_t free_pages,
+                                           PlanLds &lds, PlanPart &o) {
+    constexpr int W = kPlanThreads / 64;
+    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+    const int i0 = r0 + threadIdx.x * kPlanPer;
+    Ask a[kPlanPer];
+    uint32_t need = 0, tok = 0;
+#pragma unroll
+    for (int j = 0; j < kPlanPer; ++j) {
+        const bool live = i0 + j < p.requests;
+        a[j] = ask_of(p, live ? p.lengths[i0 + j] : 0, live ? p.add[i0 + j] : 0);
+        need = add_sat(need, a[j].need), tok = add_sat(tok, a[j].tokens);
+    }
+    uint32_t need_in = need, tok_in = tok;
 #pragma unroll
     for (int s = 1; s < 64; s *= 2) {
-        const T y = __shfl_up(x, s, 64);
-        if (lane >= s) x += y;
+        const uint32_t x = __shfl_up(need_in, s, 64), y = __shfl_up(tok_in, s, 64);
+        if (lane >= s) need_in = add_sat(need_in, x), tok_in = add_sat(tok_in, y);
     }
-    return x;
-}
-
-// Prefix sums over the requests, by one workgroup.
-constexpr int kScanThreads = 1024;
-
-__global__ __launch_bounds__(kScanThreads) void agft_kv_scan_kernel(PlanArgs p) {
-    constexpr int W = kScanThreads / 64;
-    __shared__ int64_t s64[2][W];
-    __shared__ int32_t s32[6][W];
-    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
-    const int32_t head = p.counters[0], free_pages = p.counters[1];
-    int64_t need0 = 0, tok0 = 0;                                        // sums of the requests before this round's
-    int32_t touched0 = 0, work0 = 0, tiles0 = 0, back0 = 0, refused0 = 0, taken0 = 0;
-    for (int r0 = 0; r0 < p.requests; r0 += kScanThreads) {
-        const int i = r0 + threadIdx.x;
-        const bool live = i < p.requests;
-        const Ask a = ask_of(p, live ? p.lengths[i] : 0, live ? p.add[i] : 0);
-        int64_t need = wave_inclusive((int64_t)a.need), tok = wave_inclusive((int64_t)a.tokens);
-        if (lane == 63) s64[0][wave] = need, s64[1][wave] = tok;
-        __syncthreads();
-        int64_t need_all = 0, tok_all = 0;
-        for (int w = 0; w < W; ++w) {
-            if (w == wave) need += need_all, tok += tok_all;
-            need_all += s64[0][w], tok_all += s64[1][w];
-        }
-        need += need0, tok += tok0;
-        need0 += need_all, tok0 += tok_all;
-        const bool ok = a.tokens > 0 && (a.need == 0 || need <= free_pages) && tok <= p.max_tokens;
-        const int32_t granted = ok ? a.tokens : 0;
-        const int64_t first64 = tok - a.tokens;
-        const int32_t first = first64 < p.max_tokens ? (int32_t)first64 : p.max_tokens;
-        const int32_t last = tok < p.max_tokens ? (int32_t)tok : p.max_tokens;
-        const int32_t after = a.ends ? 0 : a.past + granted;
+    if (lane == 63) lds.asked[0][wave] = need_in, lds.asked[1][wave] = tok_in;
+    uint32_t need_at = __shfl_up(need_in, 1, 64), tok_at = __shfl_up(tok_in, 1, 64);
+    if (lane == 0) need_at = 0, tok_at = 0;
+    __syncthreads();
+    need_at = add_sat(need_at, need0), tok_at = add_sat(tok_at, tok0);
+    o.tokens = tok0;
+#pragma unroll
+    for (int w = 0; w < W; ++w) {
+        if (w < wave) need_at = add_sat(need_at, lds.asked[0][w]), tok_at = add_sat(tok_at, lds.asked[1][w]);
+        o.tokens = add_sat(o.tokens, lds.asked[1][w]);
+    }
+    int32_t mine[kPlanSums] = {};
+#pragma unroll
+    for (int j = 0; j < kPlanPer; ++j) {
+        const uint32_t need_to = add_sat(need_at, a[j].need), tok_to = add_sat(tok_at, a[j].tokens);
+        const bool ok = a[j].tokens > 0 && (a[j].need == 0 || need_to <= (uint32_t)free_pages) &&
+                        tok_to <= (uint32_t)p.max_tokens;
+        const int32_t limit = p.max_tokens;
+        o.past[j] = a[j].past, o.held[j] = a[j].held;
+        o.granted[j] = ok ? (int32_t)a[j].tokens : 0;
+        o.after[j] = a[j].ends ? 0 : a[j].past + o.granted[j];
+        o.first[j] = tok_at < (uint32_t)limit ? (int32_t)tok_at : limit;
+        o.need[j] = need_at < (uint32_t)free_pages ? (int32_t)need_at : free_pages;
+        const int32_t last = tok_to < (uint32_t)limit ? (int32_t)tok_to : limit;
         // what the window's kernels have to do for it
-        const int32_t rows = last - first;                              // rows of the window's tensors
-        const bool few = (int64_t)rows * p.group <= kFewRows;
-        int32_t v[6];
-        v[0] = ok ? pages_of(after, p.page, p.shift) - (a.past >> p.shift) : 0;            // pages written to
-        // units of few rows: every 16 rows read the request's tokens (one unit where there are none)
-        v[1] = rows == 0 || !few ? 0
-                                 : (ok ? (after + kUnit - 1) / kUnit : 1) * ((rows * p.group + kRowTile - 1) / kRowTile);
-        v[2] = rows == 0 || few ? 0 : (int32_t)(((int64_t)rows * p.group + kTileRows - 1) / kTileRows);
-        v[3] = a.ends ? a.held : 0;
-        v[4] = live && a.add > 0 && !ok ? 1 : 0;
-        v[5] = ok ? a.need : 0;
-        int32_t own[6];
-        for (int k = 0; k < 6; ++k) {
-            own[k] = v[k];
-            v[k] = wave_inclusive(v[k]);
-            if (lane == 63) s32[k][wave] = v[k];
+        const int32_t rows = last - o.first[j];                         // rows of the window's tensors
+        const int64_t wide = (int64_t)rows * p.group;
+        const bool few = wide <= kFewRows;
+        const int32_t v[kPlanSums] = {
+            ok ? pages_of(o.after[j], p.page, p.shift) - (a[j].past >> p.shift) : 0,    // pages written to
+            // units of few rows: every 16 rows read the request's tokens (one unit where there are none)
+            rows == 0 || !few ? 0 : (ok ? (o.after[j] + kUnit - 1) / kUnit : 1) * (((int32_t)wide + kRowTile - 1) / kRowTile),
+            rows == 0 || few ? 0 : (int32_t)((wide + kTileRows - 1) / kTileRows),       // tiles of many rows
+            a[j].ends ? a[j].held : 0,                                                  // pages given back
+            a[j].wants && !ok ? 1 : 0,
+            ok ? a[j].need : 0,
+        };
+#pragma unroll
+        for (int k = 0; k < kPlanSums; ++k) {
+            o.sums[k][j] = mine[k];
+            mine[k] += v[k];
         }
-        __syncthreads();
-        int32_t all[6] = {};
-        for (int w = 0; w < W; ++w)
-            for (int k = 0; k < 6; ++k) {
-                if (w == wave) v[k] += all[k];
-                all[k] += s32[k][w];
-            }
-        if (live) {
-            p.starts[i] = first;
-            p.granted[i] = granted;
-            p.out_lengths[i] = after;
-            p.need[i] = (int32_t)(need - a.need < free_pages ? need - a.need : free_pages);
-            p.touched[i] = touched0 + v[0] - own[0];
-            p.work[i] = work0 + v[1] - own[1];
-            p.tiles[i] = tiles0 + v[2] - own[2];
-            p.back[i] = back0 + v[3] - own[3];
-        }
-        touched0 += all[0], work0 += all[1], tiles0 += all[2], back0 += all[3], refused0 += all[4], taken0 += all[5];
-        __syncthreads();
+        need_at = need_to, tok_at = tok_to;
     }
-    if (threadIdx.x == 0) {
-        const int32_t total = tok0 < p.max_tokens ? (int32_t)tok0 : p.max_tokens;
-        p.starts[p.requests] = total;
-        p.touched[p.requests] = touched0;
-        p.work[p.requests] = work0;
-        p.tiles[p.requests] = tiles0;
-        p.back[p.requests] = back0;
-        p.runs[0] = touched0;
-        int32_t *c = p.out_counters;
-        c[0] = (int32_t)(((int64_t)head + taken0) % p.pages);
-        c[1] = free_pages - taken0 + back0;
-        c[2] = total;
-        c[3] = refused0;
-        c[4] = taken0;
-        c[5] = back0;
-        c[6] = c[7] = 0;
+    int32_t in[kPlanSums];
+#pragma unroll
+    for (int k = 0; k < kPlanSums; ++k) in[k] = mine[k];
+#pragma unroll
+    for (int s = 1; s < 64; s *= 2)
+#pragma unroll
+        for (int k = 0; k < kPlanSums; ++k) {
+            const int32_t x = __shfl_up(in[k], s, 64);
+            if (lane >= s) in[k] += x;
+        }
+#pragma unroll
+    for (int k = 0; k < kPlanSums; ++k)
+        if (lane == 63) lds.sums[k][wave] = in[k];
+    __syncthreads();
+#pragma unroll
+    for (int k = 0; k < kPlanSums; ++k) {
+        int32_t before = in[k] - mine[k];
+        o.all[k] = 0;
+#pragma unroll
+        for (int w = 0; w < W; ++w) {
+            if (w < wave) before += lds.sums[k][w];
+            o.all[k] += lds.sums[k][w];
+        }
+#pragma unroll
+        for (int j = 0; j < kPlanPer; ++j) o.sums[k][j] += before;
     }
 }
 
-// the last i with a[i] <= x (a[0] <= x, a ascending, n entries)
-__device__ __forceinline__ int32_t last_at_most(const int32_t *a, int32_t n, int32_t x) {
-    int32_t lo = 0, hi = n;
+// The window's totals: ends of the prefix sums, and the counters.
+__device__ __forceinline__ void plan_totals(const PlanArgs &p, uint32_t tokens, const int32_t *all, int32_t head,
+                                            int32_t free_pages) {
+    const int32_t total = tokens < (uint32_t)p.max_tokens ? (int32_t)tokens : p.max_tokens;
+    p.starts[p.requests] = total;
+    p.works[p.requests] = Work{all[1], all[2], total, 0, 0, {0, 0, 0}};
+    p.runs[0] = all[0];
+    int32_t *c = p.out_counters;
+    c[0] = (int32_t)(((int64_t)head + all[5]) % p.pages);
+    c[1] = free_pages - all[5] + all[3];
+    c[2] = total;
+    c[3] = all[4];
+    c[4] = all[5];
+    c[5] = all[3];
+    c[6] = c[7] = 0;
+}
+
+// Nobody has arrived yet at the joins of the window's attention.
+__device__ __forceinline__ void plan_arrived(const PlanArgs &p) {
+    for (int k = threadIdx.x; k < kFewGroups; k += kPlanThreads) p.arrived[k] = 0;
+}
+
+// place k of the ring from its head on
+__device__ __forceinline__ int32_t ring_at(const PlanArgs &p, int32_t head, int64_t k) {
+    const int64_t at = head + k;
+    return (int32_t)(at < p.pages ? at : at - p.pages < p.pages ? at - p.pages : at % p.pages);
+}
+
+// Token t's slot, its run's place where it starts one, and its page's entry in
+// the table where it is the page's first.  base: pages taken before its
+// request's, run: runs before its request's.
+__device__ __forceinline__ void plan_token(const PlanArgs &p, int64_t t, int32_t i, int32_t past, int32_t k, int32_t base,
+                                           int32_t run, int32_t head) {
+    const int32_t pos = past + k, n = pos >> p.shift, held = pages_of(past, p.page, p.shift), off = pos & (p.page - 1);
+    int32_t id;
+    if (n >= held) {
+        id = p.ring[ring_at(p, head, (int64_t)base + n - held)];
+        if (off == 0) p.table[(int64_t)i * p.row_pages + n] = id;
+    } else {
+        id = p.table[(int64_t)i * p.row_pages + n];
+    }
+    if (k == 0 || off == 0) p.runs[1 + run + n - (past >> p.shift)] = (int32_t)t;
+    p.slots[t] = ((int64_t)id << p.shift) + off;
+}
+
+// Pages of the requests of this wavefront that end (a lane per request) go
+// behind the ring's tail.
+__device__ __forceinline__ void plan_give_back(const PlanArgs &p, bool ends, int32_t i, int32_t held, int32_t before,
+                                               int32_t head, int32_t free_pages) {
+    constexpr int AHEAD = 4;    // entries of a lane on their way at once
+    const int lane = threadIdx.x & 63;
+    for (uint64_t left = __ballot(ends && held > 0); left != 0; left &= left - 1) {
+        const int l = __ffsll((unsigned long long)left) - 1;
+        const int32_t r = __shfl(i, l, 64), n = __shfl(held, l, 64), b = __shfl(before, l, 64);
+        const int32_t *row = p.table + (int64_t)r * p.row_pages;
+        for (int32_t k0 = lane; k0 < n; k0 += 64 * AHEAD) {
+            int32_t id[AHEAD];
+#pragma unroll
+            for (int z = 0; z < AHEAD; ++z)
+                if (k0 + 64 * z < n) id[z] = row[k0 + 64 * z];
+#pragma unroll
+            for (int z = 0; z < AHEAD; ++z)
+                if (k0 + 64 * z < n) p.ring[ring_at(p, head, (int64_t)free_pages + b + k0 + 64 * z)] = id[z];
+        }
+    }
+}
+
+// the last i in [lo, hi) with a[i] <= x (a[lo] <= x, a ascending)
+__device__ __forceinline__ int32_t last_at_most(const int32_t *a, int32_t lo, int32_t hi, int32_t x) {
     while (hi - lo > 1) {
         const int32_t mid = (lo + hi) >> 1;
         if (a[mid] <= x) lo = mid;
@@ -152,37 +244,146 @@ __device__ __forceinline__ int32_t last_at_most(const int32_t *a, int32_t n, int
     return lo;
 }
 
-// Slots, runs and new table entries by tokens; the pages that come back by pages.
-__global__ __launch_bounds__(256) void agft_kv_slots_kernel(PlanArgs p) {
+__global__ __launch_bounds__(kPlanThreads) void agft_kv_plan_kernel(PlanArgs p) {
+    __shared__ PlanLds lds;
+    __shared__ int32_t s_first[kPlanChunk], s_past[kPlanChunk], s_granted[kPlanChunk], s_need[kPlanChunk],
+        s_touched[kPlanChunk], s_back[kPlanChunk];
     const int32_t head = p.counters[0], free_pages = p.counters[1];
-    const int32_t total = p.starts[p.requests];
-    const int64_t stride = (int64_t)gridDim.x * blockDim.x;
-    const int64_t id = (int64_t)blockIdx.x * blockDim.x + threadIdx.x;
-    for (int64_t t = id; t < p.max_tokens; t += stride) {
-        int64_t slot = -1;
-        if (t < total) {
-            const int32_t i = last_at_most(p.starts, p.requests, (int32_t)t);
-            if (p.granted[i] > 0) {
-                const int32_t past = p.lengths[i], k = (int32_t)t - p.starts[i], pos = past + k;
-                const int32_t n = pos >> p.shift, held = pages_of(past, p.page, p.shift), off = pos & (p.page - 1);
-                int32_t id_of;
-                if (n >= held) {
-                    id_of = p.ring[((int64_t)head + p.need[i] + n - held) % p.pages];
-                    if (off == 0) p.table[(int64_t)i * p.row_pages + n] = id_of;
-                } else {
-                    id_of = p.table[(int64_t)i * p.row_pages + n];
-                }
-                slot = ((int64_t)id_of << p.shift) + off;
-                if (k == 0 || off == 0) p.runs[1 + p.touched[i] + n - (past >> p.shift)] = (int32_t)t;
-            }
-        }
-        p.slots[t] = slot;
+    PlanPart o;
+    plan_chunk(p, 0, 0, 0, free_pages, lds, o);
+    const int i0 = threadIdx.x * kPlanPer;
+#pragma unroll
+    for (int j = 0; j < kPlanPer; ++j) {
+        s_first[i0 + j] = o.first[j], s_past[i0 + j] = o.past[j], s_granted[i0 + j] = o.granted[j];
+        s_need[i0 + j] = o.need[j], s_touched[i0 + j] = o.sums[0][j], s_back[i0 + j] = o.sums[3][j];
     }
-    const int32_t gone = p.back[p.requests];
-    for (int64_t g = id; g < gone; g += stride) {
-        const int32_t i = last_at_most(p.back, p.requests, (int32_t)g);
-        const int32_t page_id = p.table[(int64_t)i * p.row_pages + (g - p.back[i])];
-        p.ring[((int64_t)head + free_pages + g) % p.pages] = page_id;
+    if (blockIdx.x == 0) {
+#pragma unroll
+        for (int j = 0; j < kPlanPer; ++j) {
+            const int i = i0 + j;
+            if (i >= p.requests) continue;
+            p.starts[i] = o.first[j], p.granted[i] = o.granted[j], p.out_lengths[i] = o.after[j];
+            p.works[i] = Work{o.sums[1][j], o.sums[2][j], o.first[j], o.granted[j], o.after[j], {0, 0, 0}};
+        }
+        if (threadIdx.x == 0) plan_totals(p, o.tokens, o.all, head, free_pages);
+        plan_arrived(p);
+    }
+    __syncthreads();
+    const int32_t total = o.tokens < (uint32_t)p.max_tokens ? (int32_t)o.tokens : p.max_tokens;
+    for (int64_t t0 = (int64_t)blockIdx.x * kPlanTokens; t0 < p.max_tokens; t0 += (int64_t)gridDim.x * kPlanTokens)
+        for (int64_t t = t0 + threadIdx.x; t < t0 + kPlanTokens && t < p.max_tokens; t += kPlanThreads) {
+            const int32_t i = t < total ? last_at_most(s_first, 0, p.requests, (int32_t)t) : 0;
+            if (t < total && s_granted[i] > 0)
+                plan_token(p, t, i, s_past[i], (int32_t)t - s_first[i], s_need[i], s_touched[i], head);
+            else
+                p.slots[t] = -1;
+        }
+    // pages given back, one after another over all threads
+    for (int32_t k = blockIdx.x * kPlanThreads + threadIdx.x; k < o.all[3]; k += gridDim.x * kPlanThreads) {
+        const int32_t i = last_at_most(s_back, 0, p.requests, k);
+        p.ring[ring_at(p, head, (int64_t)free_pages + k)] = p.table[(int64_t)i * p.row_pages + k - s_back[i]];
+    }
+}
+
+// More than kPlanChunk requests, first launch: a workgroup per chunk.
+__global__ __launch_bounds__(kPlanThreads) void agft_kv_plan_sums_kernel(PlanArgs p) {
+    __shared__ PlanLds lds;
+    __shared__ uint32_t s_before[2][kPlanThreads / 64];
+    const int32_t free_pages = p.counters[1];
+    const int r0 = blockIdx.x * kPlanChunk, lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+    uint32_t need0 = 0, tok0 = 0;
+#pragma unroll 4
+    for (int i = threadIdx.x; i < r0; i += kPlanThreads) {
+        const Ask a = ask_of(p, p.lengths[i], p.add[i]);
+        need0 = add_sat(need0, a.need), tok0 = add_sat(tok0, a.tokens);
+    }
+#pragma unroll
+    for (int s = 1; s < 64; s *= 2) {
+        need0 = add_sat(need0, __shfl_xor(need0, s, 64));
+        tok0 = add_sat(tok0, __shfl_xor(tok0, s, 64));
+    }
+    if (lane == 0) s_before[0][wave] = need0, s_before[1][wave] = tok0;
+    __syncthreads();
+    need0 = tok0 = 0;
+    for (int w = 0; w < kPlanThreads / 64; ++w) need0 = add_sat(need0, s_before[0][w]), tok0 = add_sat(tok0, s_before[1][w]);
+    PlanPart o;
+    plan_chunk(p, r0, need0, tok0, free_pages, lds, o);
+#pragma unroll
+    for (int j = 0; j < kPlanPer; ++j) {
+        const int i = r0 + threadIdx.x * kPlanPer + j;
+        if (i >= p.requests) continue;
+        p.starts[i] = o.first[j], p.granted[i] = o.granted[j], p.out_lengths[i] = o.after[j], p.need[i] = o.need[j];
+        p.touched[i] = o.sums[0][j], p.back[i] = o.sums[3][j];
+        p.works[i] = Work{o.sums[1][j], o.sums[2][j], o.first[j], o.granted[j], o.after[j], {0, 0, 0}};
+    }
+    if (threadIdx.x == 0) {
+        for (int k = 0; k < kPlanSums; ++k) p.sums[blockIdx.x * kPlanSums + k] = o.all[k];
+        if (blockIdx.x == gridDim.x - 1)
+            p.starts[p.requests] = o.tokens < (uint32_t)p.max_tokens ? (int32_t)o.tokens : p.max_tokens;
+    }
+}
+
+// Second launch: slots, with the chunks' totals added where they are needed.
+__global__ __launch_bounds__(kPlanThreads) void agft_kv_plan_slots_kernel(PlanArgs p) {
+    constexpr int kMaxChunks = 65536 / kPlanChunk;
+    static_assert(kMaxChunks <= 64, "a wavefront's lanes hold the chunks' totals");
+    __shared__ int32_t s_off[kPlanSums][kMaxChunks], s_all[kPlanSums], s_first[kPlanTokens], s_range[2];
+    const int32_t head = p.counters[0], free_pages = p.counters[1];
+    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+    const int chunks = (p.requests + kPlanChunk - 1) / kPlanChunk;
+    for (int k = wave; k < kPlanSums; k += kPlanThreads / 64) {
+        const int32_t v = lane < chunks ? p.sums[lane * kPlanSums + k] : 0;
+        int32_t in = v;
+#pragma unroll
+        for (int s = 1; s < 64; s *= 2) {
+            const int32_t x = __shfl_up(in, s, 64);
+            if (lane >= s) in += x;
+        }
+        s_off[k][lane] = in - v;
+        if (lane == 63) s_all[k] = in;
+    }
+    __syncthreads();
+    const int32_t total = p.starts[p.requests];
+    if (blockIdx.x == 0) plan_arrived(p);
+    if (blockIdx.x == 0 && threadIdx.x == 0) {
+        int32_t all[kPlanSums];
+        for (int k = 0; k < kPlanSums; ++k) all[k] = s_all[k];
+        plan_totals(p, (uint32_t)total, all, head, free_pages);
+    }
+    // sums that other kernels read become sums over all requests
+    for (int i = blockIdx.x * kPlanThreads + threadIdx.x; (i & ~63) < p.requests; i += gridDim.x * kPlanThreads) {
+        const bool live = i < p.requests;
+        if (live) {
+            p.works[i].few += s_off[1][i / kPlanChunk];
+            p.works[i].many += s_off[2][i / kPlanChunk];
+        }
+        const bool ends = live && p.add[i] < 0;
+        const Ask a = ask_of(p, ends ? p.lengths[i] : 0, 0);
+        plan_give_back(p, ends, i, a.held, ends ? p.back[i] + s_off[3][i / kPlanChunk] : 0, head, free_pages);
+    }
+    for (int64_t t0 = (int64_t)blockIdx.x * kPlanTokens; t0 < p.max_tokens; t0 += (int64_t)gridDim.x * kPlanTokens) {
+        // the requests of these tokens
+        __syncthreads();
+        if (wave < 2) {
+            const int64_t t = wave == 0 ? t0 : t0 + kPlanTokens - 1;
+            const int32_t i = total == 0 ? 0 : find_last([&](int k) { return p.starts[k]; }, p.requests, t < total ? (int32_t)t : total - 1);
+            if (lane == 0) s_range[wave] = i;
+        }
+        __syncthreads();
+        const int32_t lo = s_range[0], hi = s_range[1] + 1;
+        const bool near = hi - lo <= kPlanTokens;      // (requests without tokens may lie between)
+        for (int i = lo + threadIdx.x; near && i < hi; i += kPlanThreads) s_first[i - lo] = p.starts[i];
+        __syncthreads();
+        for (int64_t t = t0 + threadIdx.x; t < t0 + kPlanTokens && t < p.max_tokens; t += kPlanThreads) {
+            int32_t i = 0;
+            if (t < total)
+                i = near ? lo + last_at_most(s_first, 0, hi - lo, (int32_t)t) : last_at_most(p.starts, lo, hi, (int32_t)t);
+            if (t < total && p.granted[i] > 0)
+                plan_token(p, t, i, ask_of(p, p.lengths[i], 0).past, (int32_t)t - p.starts[i], p.need[i],
+                           p.touched[i] + s_off[0][i / kPlanChunk], head);
+            else
+                p.slots[t] = -1;
+        }
     }
 }
 
@@ -507,16 +708,22 @@ int agft_kv_plan(const agft_kv_config *cfg, void *d_tables, size_t tables_bytes,
     p.add = d_add;
     p.counters = tv.counters, p.lengths = tv.lengths, p.table = tv.table, p.ring = tv.ring;
     p.out_counters = sv.counters, p.starts = sv.starts, p.granted = sv.granted, p.out_lengths = sv.lengths;
-    p.work = part(L.work), p.tiles = part(L.tiles), p.need = part(L.need), p.touched = part(L.touched);
-    p.back = part(L.back), p.runs = part(L.runs), p.slots = sv.slots;
+    p.works = reinterpret_cast<Work *>(base + L.works), p.need = part(L.need), p.touched = part(L.touched);
+    p.back = part(L.back), p.sums = part(L.sums), p.arrived = part(L.arrived), p.runs = part(L.runs), p.slots = sv.slots;
     p.requests = cfg->requests, p.row_pages = cfg->row_pages, p.pages = cfg->pages, p.page = cfg->page;
     p.shift = log2_of(cfg->page), p.group = cfg->group, p.max_tokens = max_tokens;
-    hipLaunchKernelGGL(agft_kv_scan_kernel, dim3(1), dim3(kScanThreads), 0, static_cast<hipStream_t>(stream), p);
+    const hipStream_t hs = static_cast<hipStream_t>(stream);
+    const int64_t by_tokens = ((int64_t)max_tokens + kPlanTokens - 1) / kPlanTokens;
+    const dim3 grid((unsigned)(by_tokens < 2048 ? by_tokens : 2048));
+    if (cfg->requests <= kPlanChunk) {
+        hipLaunchKernelGGL(agft_kv_plan_kernel, grid, dim3(kPlanThreads), 0, hs, p);
+        return launched();
+    }
+    const dim3 chunks((unsigned)((cfg->requests + kPlanChunk - 1) / kPlanChunk));
+    hipLaunchKernelGGL(agft_kv_plan_sums_kernel, chunks, dim3(kPlanThreads), 0, hs, p);
     st = launched();
     if (st != AGFT_OK) return st;
-    const int64_t blocks = ((int64_t)max_tokens + 255) / 256;
-    hipLaunchKernelGGL(agft_kv_slots_kernel, dim3((unsigned)(blocks < 2048 ? blocks : 2048)), dim3(256), 0,
-                       static_cast<hipStream_t>(stream), p);
+    hipLaunchKernelGGL(agft_kv_plan_slots_kernel, grid, dim3(kPlanThreads), 0, hs, p);
     return launched();
 }
 

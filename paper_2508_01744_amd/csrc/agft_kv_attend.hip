@@ -14,10 +14,11 @@ namespace agft_kv_detail {
 struct AttendArgs {
     const char *codes;
     const int32_t *exps, *table;
-    const int32_t *starts, *granted, *lengths, *work, *tiles;
+    const Work *works;
     const char *q;
     char *out;
     float *lse, *partial;
+    int32_t *arrived;
     int64_t q_token, q_head, out_token, out_head;   // numbers
     float scale;
     int32_t requests, row_pages, pages, page, shift, heads, group;
@@ -111,22 +112,6 @@ struct Half<AGFT_KV_FP16> {
     }
 };
 
-// The last i in [0, n) with a[i] <= x, a[0] <= x and a ascending; the whole
-// wavefront looks, 64 places at a time.
-__device__ __forceinline__ int find_last(const int32_t *a, int n, int32_t x) {
-    const int lane = threadIdx.x & 63;
-    int lo = 0, len = n;
-    while (len > 1) {
-        const int step = (len + 63) >> 6, k = lane * step;
-        const bool below = k < len && a[lo + k] <= x;
-        const int hits = __popcll(__ballot(below));
-        const int skip = (hits < 1 ? 0 : hits - 1) * step;
-        lo += skip;
-        len = len - skip < step ? len - skip : step;
-    }
-    return __builtin_amdgcn_readfirstlane(lo);
-}
-
 // max (or sum) over the lanes that share lane % 16
 __device__ __forceinline__ float across_max(float x) {
     x = fmaxf(x, __shfl_xor(x, 16, 64));
@@ -145,8 +130,8 @@ __device__ __forceinline__ float across_sum(float x) {
 // takes an equal stretch of it, so the split does not depend on how the lengths
 // are spread.  A stretch's part of one request's 16 rows (a segment) is cut among
 // the wavefronts, each keeping its own maximum and sums, and joined in LDS; rows
-// that several workgroups share leave partial sums, joined by
-// agft_kv_join_kernel in the order of the workgroups.
+// that several workgroups share leave partial sums, which the last of them to
+// arrive joins, in the workgroups' order whichever it is.
 //
 // Scores are made transposed, S^T = K Q^T (16 tokens x 16 rows per matrix
 // instruction), so that a lane holds four tokens' probabilities of one row,
@@ -158,32 +143,69 @@ __device__ __forceinline__ float across_sum(float x) {
 // 2^(s log2(e) + ev - M) lies in 0..1 whatever the pages' scales are, and meets
 // the codes in fp16; l sums P 2^-ev, and the output is O / l.
 constexpr int kFewWaves = 4;
-constexpr int kFewGroups = 512;      // workgroups that share the work
+constexpr int kFewPieces = 4;        // pieces that are joined without weights of their own
 constexpr int kFewShare = 4;         // units below which a stretch is not cut
 constexpr float kLog2e = 1.4426950408889634f;
 constexpr float kLn2 = 0.6931471805599453f;
 
-struct Stretch {
-    int32_t total, share;
+// The requests' works as a wavefront sees them: up to 64 requests a lane each,
+// read once.
+struct Works {
+    const Work *w;
+    int n;
+    int4 a;             // few, many, start, granted of request (lane)
+    int length;
+    int4 total;
+    __device__ __forceinline__ Works(const Work *works, int requests) : w(works), n(requests) {
+        const int lane = threadIdx.x & 63;
+        total = *reinterpret_cast<const int4 *>(w + n);
+        if (n <= 64) {
+            const int k = lane < n ? lane : n - 1;
+            a = *reinterpret_cast<const int4 *>(w + k);
+            length = w[k].length;
+        }
+    }
+    // the last request whose few (many) is at most x
+    __device__ __forceinline__ int find(bool many, int32_t x) const {
+        const int lane = threadIdx.x & 63;
+        if (n <= 64) {
+            const int hits = __popcll(__ballot(lane < n && (many ? a.y : a.x) <= x));
+            return __builtin_amdgcn_readfirstlane(hits < 1 ? 0 : hits - 1);
+        }
+        return find_last([&](int k) { return many ? w[k].many : w[k].few; }, n, x);
+    }
+    // a request's own entry, and the next one's few, many, start
+    __device__ __forceinline__ void get(int i, int4 &own, int &len, int4 &next) const {
+        if (n <= 64) {
+            const auto at = [&](int v) { return __builtin_amdgcn_readlane(v, i); };
+            own = make_int4(at(a.x), at(a.y), at(a.z), at(a.w));
+            len = at(length);
+            if (i + 1 < n) {
+                const auto after = [&](int v) { return __builtin_amdgcn_readlane(v, i + 1); };
+                next = make_int4(after(a.x), after(a.y), after(a.z), 0);
+            } else {
+                next = total;
+            }
+            return;
+        }
+        own = *reinterpret_cast<const int4 *>(w + i);
+        len = w[i].length;
+        next = *reinterpret_cast<const int4 *>(w + i + 1);
+    }
 };
-__device__ __forceinline__ Stretch stretch_of(const AttendArgs &p) {
-    Stretch s;
-    s.total = p.work[p.requests] * p.heads;
-    s.share = (s.total + kFewGroups - 1) / kFewGroups;
-    if (s.share < kFewShare) s.share = kFewShare;
-    return s;
-}
 
 // The rows that unit x of the work belongs to, and its place among their units.
 struct Segment {
-    int request, head, row, first, rows, units, at;
+    int request, head, row, first, rows, units, at, granted, length;
 };
-__device__ __forceinline__ Segment segment_of(const AttendArgs &p, int32_t x) {
+__device__ __forceinline__ Segment segment_of(const AttendArgs &p, const Works &works, int32_t x) {
     Segment s;
-    s.request = find_last(p.work, p.requests, x / p.heads);
-    const int32_t base = p.work[s.request], all = p.work[s.request + 1] - base;
-    s.first = p.starts[s.request];
-    const int rows = (p.starts[s.request + 1] - s.first) * p.group;
+    s.request = works.find(false, x / p.heads);
+    int4 own, next;
+    works.get(s.request, own, s.length, next);
+    const int32_t base = own.x, all = next.x - base;
+    s.first = own.z, s.granted = own.w;
+    const int rows = (next.z - own.z) * p.group;
     const int tiles = (rows + kRowTile - 1) / kRowTile;
     if (all <= 0 || tiles <= 0 || all < tiles) {
         s.units = 0;
@@ -217,6 +239,94 @@ __device__ __forceinline__ void store_lse(const AttendArgs &p, int first, int he
     p.lse[(int64_t)t * p.heads * p.group + hq] = m == -INFINITY ? -INFINITY : (m + __log2f(l)) * kLn2;
 }
 
+// Pieces cross between workgroups, which may sit on XCDs with caches of their
+// own.  They are written and read past those caches word by word (relaxed
+// atomics of the whole GPU's scope), and a workgroup's arrival is counted once
+// its words are acknowledged: a fence would write back and drop the whole L2
+// every time (measured: 64 tokens over 100..8,192 tokens 166 us with fences).
+__device__ __forceinline__ void put(float *p, float x) {
+    __hip_atomic_store(p, x, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+}
+__device__ __forceinline__ float get(const float *p) {
+    return __hip_atomic_load(p, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+}
+__device__ __forceinline__ void put2(float *p, float x, float y) {
+    __hip_atomic_store(reinterpret_cast<uint64_t *>(p), (uint64_t)__float_as_uint(x) | (uint64_t)__float_as_uint(y) << 32,
+                       __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+}
+__device__ __forceinline__ float2 get2(const float *p) {
+    const uint64_t v = __hip_atomic_load(reinterpret_cast<const uint64_t *>(p), __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+    return make_float2(__uint_as_float((uint32_t)v), __uint_as_float((uint32_t)(v >> 32)));
+}
+
+// Pieces of rows that begin in workgroup `owner` and go on in the next ones:
+// first every piece's weight, a wavefront per row and a lane per piece, then
+// the sums, a thread per four numbers.  weight: LDS for kRowTile * pieces.
+template <int TYPE, int DIM>
+__device__ __forceinline__ void join_pieces(const AttendArgs &p, int owner, int pieces, int first, int head, int row0,
+                                            int rows, float *weight) {
+    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+    const float *base = p.partial + (int64_t)owner * 2 * partial_floats<DIM>();
+    // the first piece is its workgroup's second one
+    const auto piece = [&](int w) { return base + (int64_t)(2 * w + (w == 0 ? 1 : 0)) * partial_floats<DIM>(); };
+    if (pieces <= kFewPieces) {
+        // one round trip
+        for (int c = threadIdx.x; c < rows * (DIM / 4); c += blockDim.x) {
+            const int r = c / (DIM / 4), d = c % (DIM / 4) * 4;
+            float m[kFewPieces], l[kFewPieces];
+            float2 a[kFewPieces], b[kFewPieces];
+#pragma unroll
+            for (int w = 0; w < kFewPieces; ++w) {
+                const float *at = piece(w < pieces ? w : 0);
+                m[w] = get(at + kRowTile * DIM + r), l[w] = get(at + kRowTile * (DIM + 1) + r);
+                a[w] = get2(at + r * DIM + d), b[w] = get2(at + r * DIM + d + 2);
+            }
+            float top = m[0], sum = 0.0f;
+#pragma unroll
+            for (int w = 1; w < kFewPieces; ++w) top = fmaxf(top, m[w]);
+            float4v o = {0, 0, 0, 0};
+#pragma unroll
+            for (int w = 0; w < kFewPieces; ++w) {
+                const float f = w >= pieces || m[w] == -INFINITY ? 0.0f : exp2f(m[w] - top);
+                sum = fmaf(l[w], f, sum);
+                o += (float4v){a[w].x, a[w].y, b[w].x, b[w].y} * f;
+            }
+            store_row4<TYPE, DIM>(p, first, head, row0 + r, d, o, sum);
+            if (d == 0) store_lse(p, first, head, row0 + r, top, sum);
+        }
+        return;
+    }
+    for (int r = wave; r < rows; r += kFewWaves) {
+        float top = -INFINITY;
+        for (int w = lane; w < pieces; w += 64) top = fmaxf(top, get(piece(w) + kRowTile * DIM + r));
+#pragma unroll
+        for (int z = 1; z < 64; z *= 2) top = fmaxf(top, __shfl_xor(top, z, 64));
+        float sum = 0.0f;
+        for (int w = lane; w < pieces; w += 64) {
+            const float m = get(piece(w) + kRowTile * DIM + r);
+            const float f = m == -INFINITY ? 0.0f : exp2f(m - top);
+            weight[r * pieces + w] = f;
+            sum = fmaf(get(piece(w) + kRowTile * (DIM + 1) + r), f, sum);
+        }
+#pragma unroll
+        for (int z = 1; z < 64; z *= 2) sum += __shfl_xor(sum, z, 64);
+        const float inv = sum > 0.0f || sum != sum ? 1.0f / sum : 0.0f;
+        for (int w = lane; w < pieces; w += 64) weight[r * pieces + w] *= inv;
+        if (lane == 0) store_lse(p, first, head, row0 + r, top, sum);
+    }
+    __syncthreads();
+    for (int c = threadIdx.x; c < rows * (DIM / 4); c += blockDim.x) {
+        const int r = c / (DIM / 4), d = c % (DIM / 4) * 4;
+        float4v o = {0, 0, 0, 0};
+#pragma unroll 8
+        for (int w = 0; w < pieces; ++w) {
+            const float2 a = get2(piece(w) + r * DIM + d), b = get2(piece(w) + r * DIM + d + 2);
+            o += (float4v){a.x, a.y, b.x, b.y} * weight[r * pieces + w];
+        }
+        store_row4<TYPE, DIM>(p, first, head, row0 + r, d, o, 1.0f);
+    }
+}
+
 template <int FORM, int TYPE, int DIM>
 __global__ __launch_bounds__(64 * kFewWaves, 2) void agft_kv_few_kernel(AttendArgs p) {
     constexpr int DG = DIM / kBlockDims;
@@ -224,25 +334,32 @@ __global__ __launch_bounds__(64 * kFewWaves, 2) void agft_kv_few_kernel(AttendAr
     constexpr int ROW = DIM + 4;                  // LDS row, off the banks
     using H = Half<TYPE>;
     using F = Half<AGFT_KV_FP16>;
-    __shared__ float s_o[kFewWaves][kRowTile * ROW];
+    // the wavefronts' sums; then, in a join, weights of at most kFewGroups pieces
+    constexpr int SUMS = kFewWaves * kRowTile * ROW, WEIGHTS = kRowTile * kFewGroups;
+    __shared__ __attribute__((aligned(16))) float s_all[SUMS > WEIGHTS ? SUMS : WEIGHTS];
+    const auto s_o = reinterpret_cast<float (*)[kRowTile * ROW]>(s_all);
     __shared__ float s_m[kFewWaves][kRowTile], s_l[kFewWaves][kRowTile];
+    __shared__ int s_last;
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     const int g = lane >> 4, n = lane & 15;
-    const Stretch st = stretch_of(p);
-    const int64_t x_first = (int64_t)blockIdx.x * st.share;
-    if (x_first >= st.total) return;
-    const int32_t x1 = x_first + st.share < st.total ? (int32_t)x_first + st.share : st.total;
+    const Works works(p.works, p.requests);
+    const int32_t work = works.total.x * p.heads;
+    int32_t share = (work + kFewGroups - 1) / kFewGroups;
+    if (share < kFewShare) share = kFewShare;
+    const int64_t x_first = (int64_t)blockIdx.x * share;
+    if (x_first >= work) return;
+    const int32_t x1 = x_first + share < work ? (int32_t)x_first + share : work;
     const int64_t page_bytes = (int64_t)p.heads * 2 * p.page * DIM;
     const float scale2 = p.scale * kLog2e;
     int32_t x = (int32_t)x_first;
     while (x < x1) {
-        const Segment seg = segment_of(p, x);
+        const Segment seg = segment_of(p, works, x);
         if (seg.units <= 0) break;
         const int i = seg.request, head = seg.head, units = seg.units, u0 = seg.at, row0 = seg.row, rows = seg.rows;
         const int first = seg.first;
         const int count = units - u0 < x1 - x ? units - u0 : x1 - x;
         x += count;
-        const int granted = p.granted[i], len = p.lengths[i];
+        const int granted = seg.granted, len = seg.length;
         if (granted <= 0) {
             // no slots, no keys
             for (int c = threadIdx.x; c < rows * DIM / 4; c += blockDim.x) {
@@ -389,6 +506,8 @@ __global__ __launch_bounds__(64 * kFewWaves, 2) void agft_kv_few_kernel(AttendAr
         }
         __syncthreads();
         const bool whole = count == units;
+        const int32_t from = x - count - u0;                       // the rows' first unit
+        const int owner = from / share, pieces = (from + units - 1) / share - owner + 1;
         float *part = p.partial + ((int64_t)blockIdx.x * 2 + (u0 == 0 ? 1 : 0)) * partial_floats<DIM>();
         for (int c = threadIdx.x; c < rows * (DIM / 4); c += blockDim.x) {
             const int r = c / (DIM / 4), d = c % (DIM / 4) * 4;
@@ -407,67 +526,23 @@ __global__ __launch_bounds__(64 * kFewWaves, 2) void agft_kv_few_kernel(AttendAr
                 store_row4<TYPE, DIM>(p, first, head, row0 + r, d, oo, ll);
                 if (d == 0) store_lse(p, first, head, row0 + r, mm, ll);
             } else {
-                *reinterpret_cast<float4v *>(part + r * DIM + d) = oo;
-                if (d == 0) part[kRowTile * DIM + r] = mm, part[kRowTile * (DIM + 1) + r] = ll;
+                put2(part + r * DIM + d, oo[0], oo[1]);
+                put2(part + r * DIM + d + 2, oo[2], oo[3]);
+                if (d == 0) put(part + kRowTile * DIM + r, mm), put(part + kRowTile * (DIM + 1) + r, ll);
+            }
+        }
+        if (!whole) {
+            __builtin_amdgcn_s_waitcnt(0x0f70);                    // this wavefront's words are out: vmcnt(0)
+            __syncthreads();
+            if (threadIdx.x == 0)
+                s_last = __hip_atomic_fetch_add(p.arrived + owner, 1, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT) == pieces - 1;
+            __syncthreads();
+            if (s_last) {
+                if (threadIdx.x == 0) p.arrived[owner] = 0;        // for the next layer's call
+                join_pieces<TYPE, DIM>(p, owner, pieces, first, head, row0, rows, s_all);
             }
         }
         __syncthreads();
-    }
-}
-
-// Partial sums of the rows whose first unit lies in this workgroup's stretch
-// and whose last does not; a wavefront per row.
-template <int TYPE, int DIM>
-__global__ __launch_bounds__(256) void agft_kv_join_kernel(AttendArgs p) {
-    const Stretch st = stretch_of(p);
-    const int64_t x_first = (int64_t)blockIdx.x * st.share;
-    if (x_first + st.share >= st.total) return;
-    const int32_t x1 = (int32_t)x_first + st.share;               // the next stretch's first unit
-    const Segment seg = segment_of(p, x1 - 1);
-    if (seg.units <= 0) return;
-    const int32_t from = x1 - 1 - seg.at;
-    if (from < x_first || from + seg.units <= x1) return;
-    if (p.granted[seg.request] <= 0) return;
-    const int head = seg.head, first = seg.first, row0 = seg.row, rows = seg.rows;
-    const int last = (from + seg.units - 1) / st.share;           // the workgroup with the last unit
-    const int lane = threadIdx.x & 63;
-    const int r = blockIdx.y * 4 + (threadIdx.x >> 6);
-    if (r >= rows) return;
-    constexpr int PER = DIM / 4;                                  // lanes of a row
-    constexpr int STEP = PER < 64 ? 64 / PER : 1;                 // pieces read at once
-    const int d = lane % PER * 4, ph = lane / PER;
-    const auto piece = [&](int w) {
-        return p.partial + ((int64_t)w * 2 + (w == (int)blockIdx.x ? 1 : 0)) * partial_floats<DIM>();
-    };
-    float mm = -INFINITY, ll = 0.0f;
-    float4v oo = {0, 0, 0, 0};
-    for (int w = blockIdx.x + ph; w <= last; w += STEP) {
-        const float *a = piece(w);
-        const float m = a[kRowTile * DIM + r], l = a[kRowTile * (DIM + 1) + r];
-        const float4v o = *reinterpret_cast<const float4v *>(a + r * DIM + d);
-        const float m1 = fmaxf(mm, m);
-        const float f0 = mm == -INFINITY ? 0.0f : exp2f(mm - m1), f1 = m == -INFINITY ? 0.0f : exp2f(m - m1);
-        oo = oo * f0 + o * f1;
-        ll = ll * f0 + l * f1;
-        mm = m1;
-    }
-#pragma unroll
-    for (int z = PER; z < 64; z *= 2) {
-        const float m = __shfl_xor(mm, z, 64), l = __shfl_xor(ll, z, 64);
-        float4v o;
-#pragma unroll
-        for (int j = 0; j < 4; ++j) o[j] = __shfl_xor(oo[j], z, 64);
-        const float m1 = fmaxf(mm, m);
-        const float f0 = mm == -INFINITY ? 0.0f : exp2f(mm - m1), f1 = m == -INFINITY ? 0.0f : exp2f(m - m1);
-        // (both partners add in one order)
-        const bool low = (lane & z) == 0;
-        oo = low ? oo * f0 + o * f1 : o * f1 + oo * f0;
-        ll = low ? ll * f0 + l * f1 : l * f1 + ll * f0;
-        mm = m1;
-    }
-    if (ph == 0) {
-        store_row4<TYPE, DIM>(p, first, head, row0 + r, d, oo, ll);
-        if (d == 0) store_lse(p, first, head, row0 + r, mm, ll);
     }
 }
 
@@ -504,13 +579,16 @@ __global__ __launch_bounds__(64 * kTileWaves, DIM > 128 ? 1 : 2) void agft_kv_ti
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     const int h = lane >> 5, n = lane & 31, m16 = lane & 15, b16 = (lane >> 4) & 1;
     const int head = blockIdx.x % p.heads;
-    const int back = blockIdx.x / p.heads, total = p.tiles[p.requests];
+    const Works works(p.works, p.requests);
+    const int back = blockIdx.x / p.heads, total = works.total.y;
     if (back >= total) return;
     const int tile = total - 1 - back;
-    const int i = find_last(p.tiles, p.requests, tile);
-    const int first = p.starts[i], all_rows = (p.starts[i + 1] - first) * p.group;
-    const int granted = p.granted[i], len = p.lengths[i];
-    const int row0 = (tile - p.tiles[i]) * kTileRows;
+    const int i = works.find(true, tile);
+    int4 own, next;
+    int len;
+    works.get(i, own, len, next);
+    const int first = own.z, granted = own.w, all_rows = (next.z - own.z) * p.group;
+    const int row0 = (tile - own.y) * kTileRows;
     const int rows = all_rows - row0 < kTileRows ? all_rows - row0 : kTileRows;
     if (rows <= 0) return;
     if (granted <= 0) {
@@ -688,14 +766,14 @@ size_t agft_kv_attend_bytes(const agft_kv_config *cfg, int32_t max_tokens) {
 }
 
 int agft_kv_attend(const agft_kv_config *cfg, const void *d_cache, size_t cache_bytes, const void *d_tables,
-                   size_t tables_bytes, const void *d_step, size_t step_bytes, int32_t max_tokens,
+                   size_t tables_bytes, void *d_step, size_t step_bytes, int32_t max_tokens,
                    int32_t max_new, const agft_kv_dense *q, const agft_kv_dense *out, float *d_lse, float scale,
                    void *d_work, size_t work_bytes, void *stream) {
     agft_kv_tables_view tv;
     agft_kv_step_view sv;
     int st = agft_kv_tables_at(cfg, const_cast<void *>(d_tables), tables_bytes, &tv);
     if (st != AGFT_OK) return st;
-    st = agft_kv_step_at(cfg, max_tokens, const_cast<void *>(d_step), step_bytes, &sv);
+    st = agft_kv_step_at(cfg, max_tokens, d_step, step_bytes, &sv);
     if (st != AGFT_OK) return st;
     const CacheLayout C = cache_layout(cfg);
     if (!buffer_ok(d_cache, cache_bytes, C.total)) return AGFT_E_INVAL;
@@ -707,10 +785,9 @@ int agft_kv_attend(const agft_kv_config *cfg, const void *d_cache, size_t cache_
     p.codes = static_cast<const char *>(d_cache) + C.codes;
     p.exps = reinterpret_cast<const int32_t *>(static_cast<const char *>(d_cache) + C.exps);
     p.table = tv.table;
-    p.starts = sv.starts, p.granted = sv.granted, p.lengths = sv.lengths;
-    p.work = reinterpret_cast<const int32_t *>(static_cast<const char *>(d_step) + step_layout(cfg, max_tokens).work);
-    p.tiles = reinterpret_cast<const int32_t *>(static_cast<const char *>(d_step) + step_layout(cfg, max_tokens).tiles);
+    p.works = reinterpret_cast<const Work *>(static_cast<const char *>(d_step) + step_layout(cfg, max_tokens).works);
     p.partial = static_cast<float *>(d_work);
+    p.arrived = reinterpret_cast<int32_t *>(static_cast<char *>(d_step) + step_layout(cfg, max_tokens).arrived);
     p.q = static_cast<const char *>(q->data), p.out = static_cast<char *>(out->data), p.lse = d_lse;
     p.q_token = q->token_stride, p.q_head = q->head_stride;
     p.out_token = out->token_stride, p.out_head = out->head_stride;
@@ -727,8 +804,6 @@ int agft_kv_attend(const agft_kv_config *cfg, const void *d_cache, size_t cache_
         agft_kv_few_kernel<form(), type(), dim()><<<kFewGroups, 64 * kFewWaves, 0, hs>>>(p);
         int code = launched();
         if (code != AGFT_OK) return code;
-        agft_kv_join_kernel<type(), dim()><<<dim3(kFewGroups, kRowTile / 4), 256, 0, hs>>>(p);
-        code = launched();
         if (code != AGFT_OK || (int64_t)max_new * cfg->group <= kFewRows) return code;
         agft_kv_tile_kernel<form(), type(), dim()><<<(unsigned)tile_groups, 64 * kTileWaves, 0, hs>>>(p);
         return launched();

@@ -21,6 +21,9 @@ constexpr int kUnit = 64;          // tokens of a unit of attention work
 constexpr int kRowTile = 16;       // query rows (tokens x group) of a tile of the attention over few rows
 constexpr int kFewRows = 64;       // query rows of a request up to which that takes it
 constexpr int kTileRows = 128;     // query rows of a tile of the attention over many rows
+constexpr int kFewGroups = 512;    // workgroups that share the work of few rows
+constexpr int kPlanChunk = 1024;   // requests whose prefix sums one workgroup makes
+constexpr int kPlanSums = 6;       // prefix sums per request that count granted tokens only
 constexpr int kMinExp = -64;
 
 inline size_t align_up(size_t n) { return (n + kAlign - 1) / kAlign * kAlign; }
@@ -56,8 +59,19 @@ inline TablesLayout tables_layout(const agft_kv_config *c) {
     return L;
 }
 
+// What the attention reads of a request, in one place: a wavefront that knows
+// the request has everything after one round trip to memory.  The last entry,
+// behind the requests', holds the totals and the last start.
+struct __attribute__((aligned(16))) Work {
+    int32_t few;      // units of few rows of the requests before this one
+    int32_t many;     // tiles of many rows of the requests before this one
+    int32_t start;    // first row
+    int32_t granted, length;
+    int32_t pad[3];
+};
+
 struct StepLayout {
-    size_t counters, starts, granted, lengths, work, tiles, need, touched, back, runs, slots, total;
+    size_t counters, starts, granted, lengths, works, need, touched, back, sums, arrived, runs, slots, total;
 };
 
 // Runs of one page's tokens in a window: a request's n tokens touch at most
@@ -75,11 +89,12 @@ inline StepLayout step_layout(const agft_kv_config *c, int32_t max_tokens) {
     L.starts = at, at += row;
     L.granted = at, at += row;
     L.lengths = at, at += row;
-    L.work = at, at += row;
-    L.tiles = at, at += row;
+    L.works = at, at += align_up(((size_t)c->requests + 1) * sizeof(Work));
     L.need = at, at += row;
     L.touched = at, at += row;
     L.back = at, at += row;
+    L.sums = at, at += align_up((size_t)kPlanSums * ((c->requests + kPlanChunk - 1) / kPlanChunk) * 4);
+    L.arrived = at, at += align_up((size_t)kFewGroups * 4);
     L.runs = at, at += align_up(((size_t)run_cap(c, max_tokens) + 1) * 4);
     L.slots = at, at += align_up((size_t)max_tokens * 8);
     L.total = at;
@@ -119,6 +134,23 @@ inline int launched() { return hipGetLastError() == hipSuccess ? AGFT_OK : AGFT_
 
 // 2^e for e in -126..127
 __device__ __forceinline__ float pow2(int e) { return __uint_as_float((uint32_t)(e + 127) << 23); }
+
+// The last i in [0, n) with at(i) <= x, at(0) <= x and at ascending; the whole
+// wavefront looks, 64 places at a time.
+template <typename F>
+__device__ __forceinline__ int find_last(F at, int n, int32_t x) {
+    const int lane = threadIdx.x & 63;
+    int lo = 0, len = n;
+    while (len > 1) {
+        const int step = (len + 63) >> 6, k = lane * step;
+        const bool below = k < len && at(lo + k) <= x;
+        const int hits = __popcll(__ballot(below));
+        const int skip = (hits < 1 ? 0 : hits - 1) * step;
+        lo += skip;
+        len = len - skip < step ? len - skip : step;
+    }
+    return __builtin_amdgcn_readfirstlane(lo);
+}
 
 template <int FORM>
 struct Code;

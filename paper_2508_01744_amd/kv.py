@@ -37,6 +37,13 @@ def kv_config(requests, row_tokens, pages, page=16, heads=8, group=4, dim=128, f
                             int(dim), FORMS[form])
 
 
+try:
+    _current_raw_stream = torch._C._cuda_getCurrentRawStream
+except AttributeError:
+    def _current_raw_stream(index):
+        return torch.cuda.current_stream(index).cuda_stream
+
+
 def _device(device):
     device = torch.device(device)
     if device.type == "cuda" and device.index is None:
@@ -57,7 +64,8 @@ class _OnStream:
         self.stream = stream
 
     def _s(self):
-        return (self.stream if self.stream is not None else torch.cuda.current_stream(self.device)).cuda_stream
+        # (the raw handle: a window's calls are short enough for the Stream object's microseconds to count)
+        return _current_raw_stream(self.device.index) if self.stream is None else self.stream.cuda_stream
 
     def _buffer(self, nbytes, what):
         if nbytes == 0:
