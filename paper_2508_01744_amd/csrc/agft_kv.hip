@@ -186,7 +186,7 @@ __device__ __forceinline__ void plan_totals(const PlanArgs &p, uint32_t tokens, 
 
 // Nobody has arrived yet at the joins of the window's attention.
 __device__ __forceinline__ void plan_arrived(const PlanArgs &p) {
-    for (int k = threadIdx.x; k < kFewGroups; k += kPlanThreads) p.arrived[k] = 0;
+    for (int k = threadIdx.x; k < kArrivals; k += kPlanThreads) p.arrived[k] = 0;
 }
 
 // place k of the ring from its head on

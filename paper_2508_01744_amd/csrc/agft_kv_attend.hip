@@ -144,6 +144,7 @@ __device__ __forceinline__ float across_sum(float x) {
 // the codes in fp16; l sums P 2^-ev, and the output is O / l.
 constexpr int kFewWaves = 4;
 constexpr int kFewPieces = 4;        // pieces that are joined without weights of their own
+constexpr int kManyPieces = 32;      // pieces that are joined at once
 constexpr int kFewShare = 4;         // units below which a stretch is not cut
 constexpr float kLog2e = 1.4426950408889634f;
 constexpr float kLn2 = 0.6931471805599453f;
@@ -259,18 +260,25 @@ __device__ __forceinline__ float2 get2(const float *p) {
     return make_float2(__uint_as_float((uint32_t)v), __uint_as_float((uint32_t)(v >> 32)));
 }
 
-// Pieces of rows that begin in workgroup `owner` and go on in the next ones:
-// first every piece's weight, a wavefront per row and a lane per piece, then
-// the sums, a thread per four numbers.  weight: LDS for kRowTile * pieces.
-template <int TYPE, int DIM>
-__device__ __forceinline__ void join_pieces(const AttendArgs &p, int owner, int pieces, int first, int head, int row0,
-                                            int rows, float *weight) {
-    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
-    const float *base = p.partial + (int64_t)owner * 2 * partial_floats<DIM>();
-    // the first piece is its workgroup's second one
-    const auto piece = [&](int w) { return base + (int64_t)(2 * w + (w == 0 ? 1 : 0)) * partial_floats<DIM>(); };
-    if (pieces <= kFewPieces) {
-        // one round trip
+// Joins `pieces` (at most kManyPieces) of the same rows.  piece(w): where piece
+// w lies.  into: where the joined piece goes, or NULL: it is the rows' result.
+// weight: LDS for kRowTile * kManyPieces numbers.
+template <int TYPE, int DIM, typename F>
+__device__ __forceinline__ void join_pieces(const AttendArgs &p, F piece, int pieces, float *into, const Segment &seg,
+                                            float *weight) {
+    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, rows = seg.rows;
+    const auto finish = [&](int r, int d, float4v o, float m, float l) {
+        if (into == nullptr) {
+            store_row4<TYPE, DIM>(p, seg.first, seg.head, seg.row + r, d, o, l);
+            if (d == 0) store_lse(p, seg.first, seg.head, seg.row + r, m, l);
+        } else {
+            put2(into + r * DIM + d, o[0], o[1]);
+            put2(into + r * DIM + d + 2, o[2], o[3]);
+            if (d == 0) put(into + kRowTile * DIM + r, m), put(into + kRowTile * (DIM + 1) + r, l);
+        }
+    };
+    if (pieces <= kFewPieces && into == nullptr) {
+        // one round trip (not into a piece's own place, which others still read)
         for (int c = threadIdx.x; c < rows * (DIM / 4); c += blockDim.x) {
             const int r = c / (DIM / 4), d = c % (DIM / 4) * 4;
             float m[kFewPieces], l[kFewPieces];
@@ -291,28 +299,26 @@ __device__ __forceinline__ void join_pieces(const AttendArgs &p, int owner, int 
                 sum = fmaf(l[w], f, sum);
                 o += (float4v){a[w].x, a[w].y, b[w].x, b[w].y} * f;
             }
-            store_row4<TYPE, DIM>(p, first, head, row0 + r, d, o, sum);
-            if (d == 0) store_lse(p, first, head, row0 + r, top, sum);
+            finish(r, d, o, top, sum);
         }
         return;
     }
+    // every piece's weight, a wavefront per row and a lane per piece, then the
+    // sums, a thread per four numbers
+    float *s_top = weight + kRowTile * kManyPieces, *s_sum = s_top + kRowTile;
     for (int r = wave; r < rows; r += kFewWaves) {
-        float top = -INFINITY;
-        for (int w = lane; w < pieces; w += 64) top = fmaxf(top, get(piece(w) + kRowTile * DIM + r));
+        const bool here = lane < pieces;
+        const float *at = piece(here ? lane : 0);
+        const float m = here ? get(at + kRowTile * DIM + r) : -INFINITY, l = get(at + kRowTile * (DIM + 1) + r);
+        float top = m;
 #pragma unroll
         for (int z = 1; z < 64; z *= 2) top = fmaxf(top, __shfl_xor(top, z, 64));
-        float sum = 0.0f;
-        for (int w = lane; w < pieces; w += 64) {
-            const float m = get(piece(w) + kRowTile * DIM + r);
-            const float f = m == -INFINITY ? 0.0f : exp2f(m - top);
-            weight[r * pieces + w] = f;
-            sum = fmaf(get(piece(w) + kRowTile * (DIM + 1) + r), f, sum);
-        }
+        const float f = m == -INFINITY ? 0.0f : exp2f(m - top);
+        if (here) weight[r * kManyPieces + lane] = f;
+        float sum = here ? l * f : 0.0f;
 #pragma unroll
         for (int z = 1; z < 64; z *= 2) sum += __shfl_xor(sum, z, 64);
-        const float inv = sum > 0.0f || sum != sum ? 1.0f / sum : 0.0f;
-        for (int w = lane; w < pieces; w += 64) weight[r * pieces + w] *= inv;
-        if (lane == 0) store_lse(p, first, head, row0 + r, top, sum);
+        if (lane == 0) s_top[r] = top, s_sum[r] = sum;
     }
     __syncthreads();
     for (int c = threadIdx.x; c < rows * (DIM / 4); c += blockDim.x) {
@@ -321,30 +327,50 @@ __device__ __forceinline__ void join_pieces(const AttendArgs &p, int owner, int 
 #pragma unroll 8
         for (int w = 0; w < pieces; ++w) {
             const float2 a = get2(piece(w) + r * DIM + d), b = get2(piece(w) + r * DIM + d + 2);
-            o += (float4v){a.x, a.y, b.x, b.y} * weight[r * pieces + w];
+            o += (float4v){a.x, a.y, b.x, b.y} * weight[r * kManyPieces + w];
         }
-        store_row4<TYPE, DIM>(p, first, head, row0 + r, d, o, 1.0f);
+        finish(r, d, o, s_top[r], s_sum[r]);
     }
 }
 
+// Counts this workgroup's arrival at a join of `parties`; true in the last one,
+// which also sets the counter back for the next layer's call.
+__device__ __forceinline__ bool last_to_arrive(int32_t *counter, int parties, int *s_last) {
+    __builtin_amdgcn_s_waitcnt(0x0f70);                    // this wavefront's words are out: vmcnt(0)
+    __syncthreads();
+    if (threadIdx.x == 0) {
+        const bool last = __hip_atomic_fetch_add(counter, 1, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT) == parties - 1;
+        if (last) __hip_atomic_store(counter, 0, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+        *s_last = last;
+    }
+    __syncthreads();
+    return *s_last != 0;
+}
+
+// Workgroups that share the work: what the registers let stay on 256 compute
+// units at once.
+template <int DIM>
+constexpr int few_groups() {
+    return DIM == 64 ? 1024 : DIM == 128 ? 768 : 512;
+}
+
 template <int FORM, int TYPE, int DIM>
-__global__ __launch_bounds__(64 * kFewWaves, 2) void agft_kv_few_kernel(AttendArgs p) {
+__global__ __launch_bounds__(64 * kFewWaves, few_groups<DIM>() / 256) void agft_kv_few_kernel(AttendArgs p) {
     constexpr int DG = DIM / kBlockDims;
-    constexpr int BLK = DIM > 128 || (DIM == 128 && FORM == AGFT_KV_INT8 && TYPE == AGFT_KV_BF16) ? 2 : 4;   // blocks of 16 tokens at a time
+    constexpr int BLK = 2;                        // blocks of 16 tokens at a time
     constexpr int ROW = DIM + 4;                  // LDS row, off the banks
     using H = Half<TYPE>;
     using F = Half<AGFT_KV_FP16>;
-    // the wavefronts' sums; then, in a join, weights of at most kFewGroups pieces
-    constexpr int SUMS = kFewWaves * kRowTile * ROW, WEIGHTS = kRowTile * kFewGroups;
-    __shared__ __attribute__((aligned(16))) float s_all[SUMS > WEIGHTS ? SUMS : WEIGHTS];
-    const auto s_o = reinterpret_cast<float (*)[kRowTile * ROW]>(s_all);
+    // the wavefronts' sums; then a join's weights, largest maxima and sums
+    static_assert(kFewWaves * ROW >= kManyPieces + 2, "a join's numbers fit where the sums were");
+    __shared__ __attribute__((aligned(16))) float s_o[kFewWaves][kRowTile * ROW];
     __shared__ float s_m[kFewWaves][kRowTile], s_l[kFewWaves][kRowTile];
     __shared__ int s_last;
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     const int g = lane >> 4, n = lane & 15;
     const Works works(p.works, p.requests);
     const int32_t work = works.total.x * p.heads;
-    int32_t share = (work + kFewGroups - 1) / kFewGroups;
+    int32_t share = (work + few_groups<DIM>() - 1) / few_groups<DIM>();
     if (share < kFewShare) share = kFewShare;
     const int64_t x_first = (int64_t)blockIdx.x * share;
     if (x_first >= work) return;
@@ -382,8 +408,8 @@ __global__ __launch_bounds__(64 * kFewWaves, 2) void agft_kv_few_kernel(AttendAr
                 q[c] = __builtin_bit_cast(typename H::x8, v);
             }
         }
-        const int limit = row_here ? len - granted + (row0 + n) / p.group + 1 : len;   // keys that row n sees
-        const int least = len - granted + row0 / p.group + 1;                          // keys that every row sees
+        int limit = row_here ? len - granted + (row0 + n) / p.group + 1 : len;   // keys that row n sees
+        int least = len - granted + row0 / p.group + 1;                          // keys that every row sees
         const int blocks = (len + kBlockTokens - 1) / kBlockTokens;
         const char *codes = p.codes + (int64_t)head * 2 * p.page * DIM;
         const int sub_mask = (p.page >> 4) - 1;
@@ -393,10 +419,12 @@ __global__ __launch_bounds__(64 * kFewWaves, 2) void agft_kv_few_kernel(AttendAr
 #pragma unroll
         for (int c = 0; c < DG * 4; ++c) o[c] = (float4v){0, 0, 0, 0};
 
-        // this wavefront's blocks of the segment
-        const int b_first = (u0 + count * wave / kFewWaves) * (kUnit / kBlockTokens);
-        int b_last = (u0 + count * (wave + 1) / kFewWaves) * (kUnit / kBlockTokens);
-        if (b_last > blocks) b_last = blocks;
+        // this wavefront's blocks of the segment: a quarter (kUnit / kBlockTokens == kFewWaves)
+        static_assert(kUnit == kBlockTokens * kFewWaves, "a unit gives every wavefront a block");
+        const int b_first = u0 * kFewWaves + count * wave;
+        const int b_last = b_first + count < blocks ? b_first + count : blocks;
+        limit = limit < b_last * kBlockTokens ? limit : b_last * kBlockTokens;
+        least = least < b_last * kBlockTokens ? least : b_last * kBlockTokens;
         for (int b0 = b_first; b0 < b_last; b0 += 64) {
             // a lane per block: its page and exponents
             int id;
@@ -414,7 +442,7 @@ __global__ __launch_bounds__(64 * kFewWaves, 2) void agft_kv_few_kernel(AttendAr
 #pragma unroll
                 for (int s = 0; s < BLK; ++s) {
                     int bb = b + s;
-                    if (bb >= blocks) bb = blocks - 1;
+                    if (bb >= b_last) bb = b_last - 1;
                     const int64_t page_id = __builtin_amdgcn_readlane(id, bb - b0);
                     const char *src = codes + page_id * page_bytes + side * p.page * DIM + (bb & sub_mask) * (16 * DIM);
 #pragma unroll
@@ -422,11 +450,12 @@ __global__ __launch_bounds__(64 * kFewWaves, 2) void agft_kv_few_kernel(AttendAr
                         dst[s][dg] = *reinterpret_cast<const uint4v *>(src + dg * kBlockBytes + lane * 16);
                 }
             };
-            uint4v kc[BLK][DG], kn[BLK][DG], vc[BLK][DG];
+            // codes are asked for as soon as their registers are free: the next
+            // keys after the scores, the next values after the sums
+            uint4v kc[BLK][DG], vc[BLK][DG];
             fetch(b0, 0, kc);
+            fetch(b0, 1, vc);
             for (int b = b0; b < b1; b += BLK) {
-                fetch(b, 1, vc);
-                if (b + BLK < b1) fetch(b + BLK, 0, kn);
                 float4v t[BLK];
                 float back[BLK];
 #pragma unroll
@@ -438,13 +467,14 @@ __global__ __launch_bounds__(64 * kFewWaves, 2) void agft_kv_few_kernel(AttendAr
                         acc = H::mfma(H::template decode<FORM>(kc[s][dg][2], kc[s][dg][3]), q[2 * dg + 1], acc);
                     }
                     int bb = b + s;
-                    if (bb >= blocks) bb = blocks - 1;
+                    if (bb >= b_last) bb = b_last - 1;
                     const int ek = __builtin_amdgcn_readlane(ee.x, bb - b0), ev = __builtin_amdgcn_readlane(ee.y, bb - b0);
                     const float ks = scale2 * pow2(ek);
                     back[s] = pow2(-ev);
 #pragma unroll
                     for (int j = 0; j < 4; ++j) t[s][j] = fmaf(acc[j], ks, (float)ev);
                 }
+                if (b + BLK < b1) fetch(b + BLK, 0, kc);
                 if ((b + BLK) * kBlockTokens > least) {
 #pragma unroll
                     for (int s = 0; s < BLK; ++s) {
@@ -491,10 +521,7 @@ __global__ __launch_bounds__(64 * kFewWaves, 2) void agft_kv_few_kernel(AttendAr
                     for (int c = 0; c < DG * 4; ++c)
                         o[c] = F::mfma(F::template decode<FORM>(vc[s][c >> 2][c & 3], vc[s + 1][c >> 2][c & 3]), pp, o[c]);
                 }
-#pragma unroll
-                for (int s = 0; s < BLK; ++s)
-#pragma unroll
-                    for (int dg = 0; dg < DG; ++dg) kc[s][dg] = kn[s][dg];
+                if (b + BLK < b1) fetch(b + BLK, 1, vc);
             }
         }
         l = across_sum(l);
@@ -532,14 +559,20 @@ __global__ __launch_bounds__(64 * kFewWaves, 2) void agft_kv_few_kernel(AttendAr
             }
         }
         if (!whole) {
-            __builtin_amdgcn_s_waitcnt(0x0f70);                    // this wavefront's words are out: vmcnt(0)
-            __syncthreads();
-            if (threadIdx.x == 0)
-                s_last = __hip_atomic_fetch_add(p.arrived + owner, 1, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT) == pieces - 1;
-            __syncthreads();
-            if (s_last) {
-                if (threadIdx.x == 0) p.arrived[owner] = 0;        // for the next layer's call
-                join_pieces<TYPE, DIM>(p, owner, pieces, first, head, row0, rows, s_all);
+            // groups of kManyPieces first, each into its first piece's place
+            const int mine = blockIdx.x - owner, group0 = mine / kManyPieces * kManyPieces;
+            const int members = pieces - group0 < kManyPieces ? pieces - group0 : kManyPieces;
+            const int groups = (pieces + kManyPieces - 1) / kManyPieces;
+            // the first piece of the rows is its workgroup's second one
+            const auto piece = [&](int w) {
+                return p.partial + ((int64_t)(owner + w) * 2 + (w == 0 ? 1 : 0)) * partial_floats<DIM>();
+            };
+            int32_t *counter = p.arrived + kFewGroups + (owner + group0) * 2 + (group0 == 0 ? 1 : 0);
+            if (last_to_arrive(counter, members, &s_last)) {
+                float *into = groups == 1 ? nullptr : piece(group0);
+                join_pieces<TYPE, DIM>(p, [&](int w) { return piece(group0 + w); }, members, into, seg, s_o[0]);
+                if (groups > 1 && last_to_arrive(p.arrived + owner, groups, &s_last))
+                    join_pieces<TYPE, DIM>(p, [&](int w) { return piece(kManyPieces * w); }, groups, nullptr, seg, s_o[0]);
             }
         }
         __syncthreads();
@@ -801,7 +834,7 @@ int agft_kv_attend(const agft_kv_config *cfg, const void *d_cache, size_t cache_
     if (tile_groups > INT32_MAX) return AGFT_E_INVAL;
     const auto go = [&](auto form, auto type, auto dim) {
         const hipStream_t hs = static_cast<hipStream_t>(stream);
-        agft_kv_few_kernel<form(), type(), dim()><<<kFewGroups, 64 * kFewWaves, 0, hs>>>(p);
+        agft_kv_few_kernel<form(), type(), dim()><<<few_groups<dim()>(), 64 * kFewWaves, 0, hs>>>(p);
         int code = launched();
         if (code != AGFT_OK) return code;
         if (code != AGFT_OK || (int64_t)max_new * cfg->group <= kFewRows) return code;

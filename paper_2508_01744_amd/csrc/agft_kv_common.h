@@ -21,7 +21,8 @@ constexpr int kUnit = 64;          // tokens of a unit of attention work
 constexpr int kRowTile = 16;       // query rows (tokens x group) of a tile of the attention over few rows
 constexpr int kFewRows = 64;       // query rows of a request up to which that takes it
 constexpr int kTileRows = 128;     // query rows of a tile of the attention over many rows
-constexpr int kFewGroups = 512;    // workgroups that share the work of few rows
+constexpr int kFewGroups = 1024;   // workgroups, at most, that share the work of few rows
+constexpr int kArrivals = 3 * kFewGroups;   // counters of a window's joins
 constexpr int kPlanChunk = 1024;   // requests whose prefix sums one workgroup makes
 constexpr int kPlanSums = 6;       // prefix sums per request that count granted tokens only
 constexpr int kMinExp = -64;
@@ -94,7 +95,7 @@ inline StepLayout step_layout(const agft_kv_config *c, int32_t max_tokens) {
     L.touched = at, at += row;
     L.back = at, at += row;
     L.sums = at, at += align_up((size_t)kPlanSums * ((c->requests + kPlanChunk - 1) / kPlanChunk) * 4);
-    L.arrived = at, at += align_up((size_t)kFewGroups * 4);
+    L.arrived = at, at += align_up((size_t)kArrivals * 4);
     L.runs = at, at += align_up(((size_t)run_cap(c, max_tokens) + 1) * 4);
     L.slots = at, at += align_up((size_t)max_tokens * 8);
     L.total = at;
