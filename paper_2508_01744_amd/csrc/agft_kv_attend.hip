@@ -497,8 +497,9 @@ __global__ __launch_bounds__(64 * kFewWaves, few_groups<DIM>() / 256) void agft_
                 top = across_max(top);
                 if (__any(top > m)) {
                     const float m1 = fmaxf(m, top);
-                    const float fall = m == -INFINITY ? 0.0f : exp2f(m - m1);
+                    float fall = m == -INFINITY ? 0.0f : exp2f(m - m1);
                     m = m1;
+                    asm volatile("" : "+v"(fall));
                     l *= fall;
 #pragma unroll
                     for (int c = 0; c < DG * 4; ++c) o[c] *= fall;
@@ -582,13 +583,16 @@ __global__ __launch_bounds__(64 * kFewWaves, few_groups<DIM>() / 256) void agft_
 // ---- many query rows: tiles of 128 ----
 //
 // A workgroup takes 128 rows (tokens x group) of one request and head, 32 per
-// wavefront, and goes over the tokens 64 at a time.  The codes come from HBM
-// straight to LDS, one tile ahead, each wavefront fetching one block of 16
-// tokens; the wavefronts turn them into 16 bits on the way to the matrix
-// instructions (32 x 32 x 16).  As above, S^T = K Q^T and O^T = V^T P^T, so a
-// row's probabilities stay in the lanes that made them.  The longest tiles
-// start first, and consecutive workgroups take consecutive heads, so that (with
-// 8 heads) an XCD's L2 holds one head's tokens.
+// wavefront, and goes over the tokens 64 at a time.  Vector instructions, not
+// the matrix cores, are what such a kernel runs out of (the exponentials alone
+// take a quarter of the matrix cores' time), so codes are turned into 16 bits
+// once per workgroup: each wavefront fetches one block of 16 tokens, a tile
+// ahead, and leaves its numbers in LDS as the matrix instructions (32 x 32 x 16)
+// take them, 16 bytes a lane.  As above, S^T = K Q^T and O^T = V^T P^T, so a
+// row's probabilities stay in the lanes that made them.  The tiles of tokens
+// that every row sees whole have a loop of their own, without masks.  The
+// longest tiles of rows start first, and consecutive workgroups take consecutive
+// heads, so that (with 8 heads) an XCD's L2 holds one head's tokens.
 typedef float float16v __attribute__((ext_vector_type(16)));
 
 template <int TYPE>
@@ -604,13 +608,14 @@ constexpr float kSlack = 8.0f;    // powers of two that a maximum may grow befor
 template <int FORM, int TYPE, int DIM>
 __global__ __launch_bounds__(64 * kTileWaves, DIM > 128 ? 1 : 2) void agft_kv_tile_kernel(AttendArgs p) {
     constexpr int DG = DIM / kBlockDims;
-    constexpr int SIDE = kBlockBytes * DG;                 // one block's keys (or values)
+    constexpr int SIDE = kTileKeys * DIM * 2;              // a tile's keys (or values) in 16 bits
     using H = Half<TYPE>;
     using F = Half<AGFT_KV_FP16>;
-    __shared__ __attribute__((aligned(16))) char s_codes[2][4][2][SIDE];   // buffer, block, side
-    __shared__ int2 s_exps[2][4];
+    // operands of 1 KB, 16 bytes a lane; keys: [32 tokens][64 numbers][32][16], values: [16 tokens][32 numbers]
+    __shared__ __attribute__((aligned(16))) char s_tile[2][2][SIDE];
+    __shared__ float4 s_scale[2][4];                       // a block's factor of the scores, ev, 2^-ev
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-    const int h = lane >> 5, n = lane & 31, m16 = lane & 15, b16 = (lane >> 4) & 1;
+    const int h = lane >> 5, n = lane & 31;
     const int head = blockIdx.x % p.heads;
     const Works works(p.works, p.requests);
     const int back = blockIdx.x / p.heads, total = works.total.y;
@@ -633,15 +638,11 @@ __global__ __launch_bounds__(64 * kTileWaves, DIM > 128 ? 1 : 2) void agft_kv_ti
         return;
     }
     const int past = len - granted;
-    const int wrow = row0 + 32 * wave;                     // this wavefront's rows
     const bool busy = 32 * wave < rows, row_here = 32 * wave + n < rows;
-    const int row = row_here ? wrow + n : row0 + rows - 1;
+    const int row = row_here ? row0 + 32 * wave + n : row0 + rows - 1;
     const int limit = past + row / p.group + 1;            // keys that this lane's row sees
-    const int least = past + wrow / p.group + 1;           // keys that every row of the wavefront sees
-    const int wlast = 32 * wave + 31 < rows ? wrow + 31 : row0 + rows - 1;
-    const int most = busy ? past + wlast / p.group + 1 : 0;
-    const int keys = past + (row0 + rows - 1) / p.group + 1;
-    const int tiles = (keys + kTileKeys - 1) / kTileKeys;
+    const int whole = (past + row0 / p.group + 1) / kTileKeys;             // tiles that every row sees whole
+    const int tiles = (past + (row0 + rows - 1) / p.group + kTileKeys) / kTileKeys;
     const int blocks = (len + kBlockTokens - 1) / kBlockTokens;
 
     typename H::x8 q[DG * 4];
@@ -669,7 +670,8 @@ __global__ __launch_bounds__(64 * kTileWaves, DIM > 128 ? 1 : 2) void agft_kv_ti
         id = (int)z;
         ee = *reinterpret_cast<const int2 *>(p.exps + ((int64_t)id * p.heads + head) * 2);
     };
-    const auto fetch = [&](int t, int buf) {
+    uint4v ahead[2][DG];                                   // the next tile's codes on their way
+    const auto fetch = [&](int t) {
         if ((t & 63) == 0) look_up(t);
         int b = t * 4 + wave;
         if (b >= blocks) b = blocks - 1;
@@ -679,11 +681,38 @@ __global__ __launch_bounds__(64 * kTileWaves, DIM > 128 ? 1 : 2) void agft_kv_ti
         for (int side = 0; side < 2; ++side)
 #pragma unroll
             for (int dg = 0; dg < DG; ++dg)
-                __builtin_amdgcn_global_load_lds(
-                    (const __attribute__((address_space(1))) void *)(src + side * p.page * DIM + dg * kBlockBytes),
-                    (__attribute__((address_space(3))) void *)&s_codes[buf][wave][side][dg * kBlockBytes],
-                    16, 0, 0);
-        if (lane == (t & 63)) s_exps[buf][wave] = ee;
+                ahead[side][dg] = *reinterpret_cast<const uint4v *>(src + side * p.page * DIM + dg * kBlockBytes);
+    };
+    // Entry 16 g + m of the codes to the lanes that take its numbers: token m's
+    // numbers 16 g.. as a row of the left operand of the scores, numbers m, 16 + m,
+    // .. of tokens 4 g.. as rows of the left operand of the sums.
+    const int g = lane >> 4, m16 = lane & 15;
+    const int to_key = (((wave >> 1) * DG * 4 + (g >> 1) * 2) * 64 + 32 * (g & 1) + 16 * (wave & 1) + m16) * 16;
+    const int to_value = (wave * DG * 2 * 64 + 32 * (g & 1) + m16) * 16 + 8 * (g >> 1);
+    const auto stage = [&](int t, int buf) {
+        const int valid = len - (t * kTileKeys + 16 * wave + 4 * g);
+        if ((t * 4 + wave + 1) * kBlockTokens > len) {
+            // codes past the request's tokens may be anything, NaN too
+            const uint32_t keep = valid >= 4 ? ~0u : valid <= 0 ? 0u : (1u << (8 * valid)) - 1u;
+#pragma unroll
+            for (int dg = 0; dg < DG; ++dg) ahead[1][dg] &= keep;
+        }
+#pragma unroll
+        for (int dg = 0; dg < DG; ++dg) {
+            const uint4v k = ahead[0][dg], v = ahead[1][dg];
+#pragma unroll
+            for (int e = 0; e < 2; ++e)
+                *reinterpret_cast<typename H::x8 *>(&s_tile[buf][0][to_key + (dg * 4 + e) * 1024]) =
+                    H::template decode<FORM>(k[2 * e], k[2 * e + 1]);
+#pragma unroll
+            for (int b = 0; b < 2; ++b) {                  // words 2 b, 2 b + 1: rows 16 b + m of two operands
+                const fp16x8 x = F::template decode<FORM>(v[2 * b], v[2 * b + 1]);
+                char *dst = &s_tile[buf][1][to_value + dg * 2 * 1024 + b * 256];
+                *reinterpret_cast<fp16x4 *>(dst) = __builtin_shufflevector(x, x, 0, 1, 2, 3);
+                *reinterpret_cast<fp16x4 *>(dst + 1024) = __builtin_shufflevector(x, x, 4, 5, 6, 7);
+            }
+        }
+        if (lane == (t & 63)) s_scale[buf][wave] = make_float4(scale2 * pow2(ee.x), (float)ee.y, pow2(-ee.y), 0.0f);
     };
 
     float m = -INFINITY, l = 0.0f;
@@ -693,37 +722,30 @@ __global__ __launch_bounds__(64 * kTileWaves, DIM > 128 ? 1 : 2) void agft_kv_ti
 #pragma unroll
         for (int j = 0; j < 16; ++j) o[c][j] = 0.0f;
 
-    fetch(0, 0);
-    for (int t = 0; t < tiles; ++t) {
-        const int buf = t & 1;
-        __builtin_amdgcn_s_waitcnt(0x0f70);                // this wavefront's codes have landed: vmcnt(0)
-        __syncthreads();                                   // everybody's have, and the other buffer is read
-        if (t + 1 < tiles) fetch(t + 1, buf ^ 1);
-        const int key0 = t * kTileKeys;
-        if (key0 >= most) continue;
+    // One tile of keys.  MASK: some row may not see all of them.
+    const auto attend_tile = [&](int buf, int key0, auto mask) {
+        constexpr bool MASK = mask();
+        const float off = m == -INFINITY ? 0.0f : m;
         float16v s[2];
 #pragma unroll
         for (int half = 0; half < 2; ++half) {
 #pragma unroll
             for (int j = 0; j < 16; ++j) s[half][j] = 0.0f;
 #pragma unroll
-            for (int c = 0; c < DG * 2; ++c) {             // 16-byte entry 16 (2 (c % 2) + h) + m16 of block 2 half + b16
-                const uint4v k = *reinterpret_cast<const uint4v *>(
-                    &s_codes[buf][2 * half + b16][0][(c >> 1) * kBlockBytes + (16 * (2 * (c & 1) + h) + m16) * 16]);
-                s[half] = mfma32<TYPE>(H::template decode<FORM>(k[0], k[1]), q[2 * c], s[half]);
-                s[half] = mfma32<TYPE>(H::template decode<FORM>(k[2], k[3]), q[2 * c + 1], s[half]);
-            }
+            for (int c = 0; c < DG * 4; ++c)
+                s[half] = mfma32<TYPE>(*reinterpret_cast<const typename H::x8 *>(
+                                           &s_tile[buf][0][((half * DG * 4 + c) * 64 + lane) * 16]), q[c], s[half]);
         }
         float pow_back[4];
 #pragma unroll
         for (int b = 0; b < 4; ++b) {
-            const int2 e = s_exps[buf][b];
-            const float ks = scale2 * pow2(e.x), ev = (float)e.y;
-            pow_back[b] = pow2(-e.y);
+            const float4 f = s_scale[buf][b];
+            const float ev = f.y - off;
+            pow_back[b] = f.z;
 #pragma unroll
-            for (int j = 0; j < 8; ++j) s[b >> 1][8 * (b & 1) + j] = fmaf(s[b >> 1][8 * (b & 1) + j], ks, ev);
+            for (int j = 0; j < 8; ++j) s[b >> 1][8 * (b & 1) + j] = fmaf(s[b >> 1][8 * (b & 1) + j], f.x, ev);
         }
-        if (key0 + kTileKeys > least) {
+        if constexpr (MASK) {
 #pragma unroll
             for (int half = 0; half < 2; ++half)
 #pragma unroll
@@ -736,43 +758,56 @@ __global__ __launch_bounds__(64 * kTileWaves, DIM > 128 ? 1 : 2) void agft_kv_ti
 #pragma unroll
             for (int j = 0; j < 16; ++j) top = fmaxf(top, s[half][j]);
         top = fmaxf(top, __shfl_xor(top, 32, 64));
-        if (__any(top > m + kSlack || m == -INFINITY)) {
-            const float m1 = fmaxf(m, top);
-            const float fall = m == -INFINITY ? 0.0f : exp2f(m - m1);
+        // the maximum that the sums are relative to follows the real one at some distance
+        if (__builtin_expect(__any(top > kSlack || m == -INFINITY), 0)) {
+            const float m1 = fmaxf(m, off + top);
+            float fall = m == -INFINITY ? 0.0f : exp2f(m - m1), shift = m1 == -INFINITY ? 0.0f : off - m1;
             m = m1;
+            // (keeps the compiler from multiplying ahead of the branch, which is rarely taken)
+            asm volatile("" : "+v"(fall), "+v"(shift));
             l *= fall;
 #pragma unroll
             for (int c = 0; c < DG * 2; ++c) o[c] *= fall;
+#pragma unroll
+            for (int half = 0; half < 2; ++half) s[half] += shift;
         }
-        const float off = m == -INFINITY ? 0.0f : m;
-        const bool tail = key0 + kTileKeys > len;
 #pragma unroll
         for (int b = 0; b < 4; ++b) {
             float e[8];
 #pragma unroll
-            for (int j = 0; j < 8; ++j) e[j] = __builtin_amdgcn_exp2f(s[b >> 1][8 * (b & 1) + j] - off);
+            for (int j = 0; j < 8; ++j) e[j] = __builtin_amdgcn_exp2f(s[b >> 1][8 * (b & 1) + j]);
             l = fmaf(((e[0] + e[1]) + (e[2] + e[3])) + ((e[4] + e[5]) + (e[6] + e[7])), pow_back[b], l);
             fp16x8 pr;
 #pragma unroll
             for (int j = 0; j < 8; ++j) pr[j] = (_Float16)e[j];
-            uint32_t keep[2] = {~0u, ~0u};
-            if (tail) {
-                // codes past the request's tokens may be anything, NaN too
 #pragma unroll
-                for (int z = 0; z < 2; ++z) {
-                    const int valid = len - (key0 + 16 * b + 8 * z + 4 * h);
-                    keep[z] = valid >= 4 ? ~0u : valid <= 0 ? 0u : (1u << (8 * valid)) - 1u;
-                }
-            }
-#pragma unroll
-            for (int dg = 0; dg < DG; ++dg) {              // words 2 b16, 2 b16 + 1 of entries 16 h + m16, 16 (h + 2) + m16
-                const char *src = &s_codes[buf][b][1][dg * kBlockBytes + (16 * h + m16) * 16 + 8 * b16];
-                uint2 v0 = *reinterpret_cast<const uint2 *>(src), v1 = *reinterpret_cast<const uint2 *>(src + 512);
-                if (tail) v0.x &= keep[0], v0.y &= keep[0], v1.x &= keep[1], v1.y &= keep[1];
-                o[2 * dg] = mfma32<AGFT_KV_FP16>(F::template decode<FORM>(v0.x, v1.x), pr, o[2 * dg]);
-                o[2 * dg + 1] = mfma32<AGFT_KV_FP16>(F::template decode<FORM>(v0.y, v1.y), pr, o[2 * dg + 1]);
-            }
+            for (int c = 0; c < DG * 2; ++c)
+                o[c] = mfma32<AGFT_KV_FP16>(*reinterpret_cast<const fp16x8 *>(
+                                                &s_tile[buf][1][((b * DG * 2 + c) * 64 + lane) * 16]), pr, o[c]);
         }
+    };
+
+    fetch(0);
+    stage(0, 0);
+    if (!busy) {                                           // no rows of its own: only fetches
+        for (int t = 0; t < tiles; ++t) {
+            __syncthreads();
+            if (t + 1 < tiles) fetch(t + 1), stage(t + 1, (t + 1) & 1);
+        }
+        return;
+    }
+    int t = 0;
+    for (; t < whole; ++t) {
+        __syncthreads();                                   // this tile is in LDS, and the other buffer is read
+        if (t + 1 < tiles) fetch(t + 1);
+        attend_tile(t & 1, t * kTileKeys, std::false_type{});
+        if (t + 1 < tiles) stage(t + 1, (t + 1) & 1);
+    }
+    for (; t < tiles; ++t) {
+        __syncthreads();
+        if (t + 1 < tiles) fetch(t + 1);
+        attend_tile(t & 1, t * kTileKeys, std::true_type{});
+        if (t + 1 < tiles) stage(t + 1, (t + 1) & 1);
     }
     l += __shfl_xor(l, 32, 64);
     if (!row_here) return;
