@@ -112,14 +112,31 @@ struct Half<AGFT_KV_FP16> {
     }
 };
 
-// max (or sum) over the lanes that share lane % 16
+// max (or sum) over the lanes that share lane % 32, and over those that share
+// lane % 16: halves (rows of 16) change places between two copies
+__device__ __forceinline__ float2 halves(float x) {
+    const auto r = __builtin_amdgcn_permlane32_swap(__float_as_uint(x), __float_as_uint(x), false, false);
+    return make_float2(__uint_as_float(r[0]), __uint_as_float(r[1]));
+}
+__device__ __forceinline__ float2 quarters(float x) {
+    const auto r = __builtin_amdgcn_permlane16_swap(__float_as_uint(x), __float_as_uint(x), false, false);
+    return make_float2(__uint_as_float(r[0]), __uint_as_float(r[1]));
+}
+__device__ __forceinline__ float halves_max(float x) {
+    const float2 y = halves(x);
+    return fmaxf(y.x, y.y);
+}
+__device__ __forceinline__ float halves_sum(float x) {
+    const float2 y = halves(x);
+    return y.x + y.y;
+}
 __device__ __forceinline__ float across_max(float x) {
-    x = fmaxf(x, __shfl_xor(x, 16, 64));
-    return fmaxf(x, __shfl_xor(x, 32, 64));
+    const float2 y = quarters(x);
+    return halves_max(fmaxf(y.x, y.y));
 }
 __device__ __forceinline__ float across_sum(float x) {
-    x += __shfl_xor(x, 16, 64);
-    return x + __shfl_xor(x, 32, 64);
+    const float2 y = quarters(x);
+    return halves_sum(y.x + y.y);
 }
 
 // ---- few query rows: shared out over the cached tokens ----
@@ -613,7 +630,7 @@ __global__ __launch_bounds__(64 * kTileWaves, DIM > 128 ? 1 : 2) void agft_kv_ti
     using F = Half<AGFT_KV_FP16>;
     // operands of 1 KB, 16 bytes a lane; keys: [32 tokens][64 numbers][32][16], values: [16 tokens][32 numbers]
     __shared__ __attribute__((aligned(16))) char s_tile[2][2][SIDE];
-    __shared__ float4 s_scale[2][4];                       // a block's factor of the scores, ev, 2^-ev
+    __shared__ float4 s_scale[4][4];                       // by tile % 4: a block's factor of the scores, ev, 2^-ev
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     const int h = lane >> 5, n = lane & 31;
     const int head = blockIdx.x % p.heads;
@@ -670,49 +687,60 @@ __global__ __launch_bounds__(64 * kTileWaves, DIM > 128 ? 1 : 2) void agft_kv_ti
         id = (int)z;
         ee = *reinterpret_cast<const int2 *>(p.exps + ((int64_t)id * p.heads + head) * 2);
     };
-    uint4v ahead[2][DG];                                   // the next tile's codes on their way
-    const auto fetch = [&](int t) {
+    // Step t makes the scores of tile t + 1 beside the sums of tile t, so its
+    // operands are the keys of one tile and the values of the one before.
+    uint4v ahead[2][DG];                                   // codes of the next step on their way
+    const char *values = codes;                            // this wavefront's values of the tile whose keys were last
+    const auto fetch = [&](int t, bool both) {             // keys of tile t, values of tile t - 1
+        if (both) {
+#pragma unroll
+            for (int dg = 0; dg < DG; ++dg) ahead[1][dg] = *reinterpret_cast<const uint4v *>(values + dg * kBlockBytes);
+        }
         if ((t & 63) == 0) look_up(t);
         int b = t * 4 + wave;
         if (b >= blocks) b = blocks - 1;
         const int64_t page_id = __builtin_amdgcn_readlane(id, t & 63);
         const char *src = codes + page_id * page_bytes + (b & sub_mask) * (16 * DIM) + lane * 16;
 #pragma unroll
-        for (int side = 0; side < 2; ++side)
-#pragma unroll
-            for (int dg = 0; dg < DG; ++dg)
-                ahead[side][dg] = *reinterpret_cast<const uint4v *>(src + side * p.page * DIM + dg * kBlockBytes);
+        for (int dg = 0; dg < DG; ++dg) ahead[0][dg] = *reinterpret_cast<const uint4v *>(src + dg * kBlockBytes);
+        values = src + p.page * DIM;
     };
     // Entry 16 g + m of the codes to the lanes that take its numbers: token m's
     // numbers 16 g.. as a row of the left operand of the scores, numbers m, 16 + m,
     // .. of tokens 4 g.. as rows of the left operand of the sums.
     const int g = lane >> 4, m16 = lane & 15;
     const int to_key = (((wave >> 1) * DG * 4 + (g >> 1) * 2) * 64 + 32 * (g & 1) + 16 * (wave & 1) + m16) * 16;
-    const int to_value = (wave * DG * 2 * 64 + 32 * (g & 1) + m16) * 16 + 8 * (g >> 1);
-    const auto stage = [&](int t, int buf) {
-        const int valid = len - (t * kTileKeys + 16 * wave + 4 * g);
-        if ((t * 4 + wave + 1) * kBlockTokens > len) {
+    const int to_value = (wave * DG * 2 * 64 + 32 * (g & 1) + 16 * (g >> 1) + m16) * 16;
+    const auto stage = [&](int t, bool both) {             // what fetch(t, both) brought
+        const int buf = (t + 1) & 1;
+#pragma unroll
+        for (int dg = 0; dg < DG; ++dg) {
+            const uint4v k = ahead[0][dg];
+#pragma unroll
+            for (int e = 0; e < 2; ++e)
+                *reinterpret_cast<typename H::x8 *>(&s_tile[buf][0][to_key + (dg * 4 + e) * 1024]) =
+                    H::template decode<FORM>(k[2 * e], k[2 * e + 1]);
+        }
+        if (lane == (t & 63)) s_scale[t & 3][wave] = make_float4(scale2 * pow2(ee.x), (float)ee.y, pow2(-ee.y), 0.0f);
+        if (!both) return;
+        if (((t - 1) * 4 + wave + 1) * kBlockTokens > len) {
             // codes past the request's tokens may be anything, NaN too
+            const int valid = len - ((t - 1) * kTileKeys + 16 * wave + 4 * g);
             const uint32_t keep = valid >= 4 ? ~0u : valid <= 0 ? 0u : (1u << (8 * valid)) - 1u;
 #pragma unroll
             for (int dg = 0; dg < DG; ++dg) ahead[1][dg] &= keep;
         }
 #pragma unroll
         for (int dg = 0; dg < DG; ++dg) {
-            const uint4v k = ahead[0][dg], v = ahead[1][dg];
+            // words 0, 1 (2, 3) of the entries 16 g + m and 16 (g + 2) + m come
+            // together in the lower (upper) half: rows m (16 + m) of two operands
 #pragma unroll
-            for (int e = 0; e < 2; ++e)
-                *reinterpret_cast<typename H::x8 *>(&s_tile[buf][0][to_key + (dg * 4 + e) * 1024]) =
-                    H::template decode<FORM>(k[2 * e], k[2 * e + 1]);
-#pragma unroll
-            for (int b = 0; b < 2; ++b) {                  // words 2 b, 2 b + 1: rows 16 b + m of two operands
-                const fp16x8 x = F::template decode<FORM>(v[2 * b], v[2 * b + 1]);
-                char *dst = &s_tile[buf][1][to_value + dg * 2 * 1024 + b * 256];
-                *reinterpret_cast<fp16x4 *>(dst) = __builtin_shufflevector(x, x, 0, 1, 2, 3);
-                *reinterpret_cast<fp16x4 *>(dst + 1024) = __builtin_shufflevector(x, x, 4, 5, 6, 7);
+            for (int z = 0; z < 2; ++z) {
+                const auto w = __builtin_amdgcn_permlane32_swap(ahead[1][dg][z], ahead[1][dg][2 + z], false, false);
+                *reinterpret_cast<fp16x8 *>(&s_tile[buf][1][to_value + (dg * 2 + z) * 1024]) =
+                    F::template decode<FORM>(w[0], w[1]);
             }
         }
-        if (lane == (t & 63)) s_scale[buf][wave] = make_float4(scale2 * pow2(ee.x), (float)ee.y, pow2(-ee.y), 0.0f);
     };
 
     float m = -INFINITY, l = 0.0f;
@@ -722,24 +750,27 @@ __global__ __launch_bounds__(64 * kTileWaves, DIM > 128 ? 1 : 2) void agft_kv_ti
 #pragma unroll
         for (int j = 0; j < 16; ++j) o[c][j] = 0.0f;
 
-    // One tile of keys.  MASK: some row may not see all of them.
-    const auto attend_tile = [&](int buf, int key0, auto mask) {
-        constexpr bool MASK = mask();
-        const float off = m == -INFINITY ? 0.0f : m;
-        float16v s[2];
+    float16v s[2];                                         // scores of the tile whose turn is next
+    const auto scores = [&](int buf, float16v *z) {
 #pragma unroll
         for (int half = 0; half < 2; ++half) {
 #pragma unroll
-            for (int j = 0; j < 16; ++j) s[half][j] = 0.0f;
+            for (int j = 0; j < 16; ++j) z[half][j] = 0.0f;
 #pragma unroll
             for (int c = 0; c < DG * 4; ++c)
-                s[half] = mfma32<TYPE>(*reinterpret_cast<const typename H::x8 *>(
-                                           &s_tile[buf][0][((half * DG * 4 + c) * 64 + lane) * 16]), q[c], s[half]);
+                z[half] = mfma32<TYPE>(*reinterpret_cast<const typename H::x8 *>(
+                                           &s_tile[buf][0][((half * DG * 4 + c) * 64 + lane) * 16]), q[c], z[half]);
         }
+    };
+    // One step.  MASK: some row may not see all of the tile's keys.
+    const auto step = [&](int t, auto mask) {
+        constexpr bool MASK = mask();
+        const int buf = t & 1;
+        const float off = m == -INFINITY ? 0.0f : m;
         float pow_back[4];
 #pragma unroll
         for (int b = 0; b < 4; ++b) {
-            const float4 f = s_scale[buf][b];
+            const float4 f = s_scale[t & 3][b];
             const float ev = f.y - off;
             pow_back[b] = f.z;
 #pragma unroll
@@ -750,14 +781,14 @@ __global__ __launch_bounds__(64 * kTileWaves, DIM > 128 ? 1 : 2) void agft_kv_ti
             for (int half = 0; half < 2; ++half)
 #pragma unroll
                 for (int j = 0; j < 16; ++j)
-                    if (key0 + 32 * half + 8 * (j >> 2) + 4 * h + (j & 3) >= limit) s[half][j] = -INFINITY;
+                    if (t * kTileKeys + 32 * half + 8 * (j >> 2) + 4 * h + (j & 3) >= limit) s[half][j] = -INFINITY;
         }
         float top = s[0][0];
 #pragma unroll
         for (int half = 0; half < 2; ++half)
 #pragma unroll
             for (int j = 0; j < 16; ++j) top = fmaxf(top, s[half][j]);
-        top = fmaxf(top, __shfl_xor(top, 32, 64));
+        top = halves_max(top);
         // the maximum that the sums are relative to follows the real one at some distance
         if (__builtin_expect(__any(top > kSlack || m == -INFINITY), 0)) {
             const float m1 = fmaxf(m, off + top);
@@ -771,6 +802,8 @@ __global__ __launch_bounds__(64 * kTileWaves, DIM > 128 ? 1 : 2) void agft_kv_ti
 #pragma unroll
             for (int half = 0; half < 2; ++half) s[half] += shift;
         }
+        float16v z[2];
+        scores(buf, z);
 #pragma unroll
         for (int b = 0; b < 4; ++b) {
             float e[8];
@@ -785,31 +818,36 @@ __global__ __launch_bounds__(64 * kTileWaves, DIM > 128 ? 1 : 2) void agft_kv_ti
                 o[c] = mfma32<AGFT_KV_FP16>(*reinterpret_cast<const fp16x8 *>(
                                                 &s_tile[buf][1][((b * DG * 2 + c) * 64 + lane) * 16]), pr, o[c]);
         }
+        s[0] = z[0], s[1] = z[1];
     };
 
-    fetch(0);
-    stage(0, 0);
+    fetch(0, false);
+    stage(0, false);
+    fetch(1, true);
+    __syncthreads();
+    if (busy) scores(1, s);                                // of tile 0, whose keys lie in the buffer of step -1
+    stage(1, true);
     if (!busy) {                                           // no rows of its own: only fetches
         for (int t = 0; t < tiles; ++t) {
             __syncthreads();
-            if (t + 1 < tiles) fetch(t + 1), stage(t + 1, (t + 1) & 1);
+            if (t + 1 < tiles) fetch(t + 2, true), stage(t + 2, true);
         }
         return;
     }
     int t = 0;
     for (; t < whole; ++t) {
-        __syncthreads();                                   // this tile is in LDS, and the other buffer is read
-        if (t + 1 < tiles) fetch(t + 1);
-        attend_tile(t & 1, t * kTileKeys, std::false_type{});
-        if (t + 1 < tiles) stage(t + 1, (t + 1) & 1);
+        __syncthreads();                                   // this step's operands are in LDS, and the other buffer is read
+        if (t + 1 < tiles) fetch(t + 2, true);
+        step(t, std::false_type{});
+        if (t + 1 < tiles) stage(t + 2, true);
     }
     for (; t < tiles; ++t) {
         __syncthreads();
-        if (t + 1 < tiles) fetch(t + 1);
-        attend_tile(t & 1, t * kTileKeys, std::true_type{});
-        if (t + 1 < tiles) stage(t + 1, (t + 1) & 1);
+        if (t + 1 < tiles) fetch(t + 2, true);
+        step(t, std::true_type{});
+        if (t + 1 < tiles) stage(t + 2, true);
     }
-    l += __shfl_xor(l, 32, 64);
+    l = halves_sum(l);
     if (!row_here) return;
 #pragma unroll
     for (int c = 0; c < DG * 2; ++c)
