@@ -584,35 +584,47 @@ struct ExportArgs {
     int32_t heads, page, shift;
 };
 
-// One thread per number pair (key and value) of a slot.
+// Four threads per slot, a head and a side per workgroup; a thread takes 16
+// numbers of each 64: one key entry, or one byte of each of 16 value entries
+// (which neighbouring slots' threads read too, from the same lines).
+// [17,699 slots of 8 heads x 128 numbers, e4m3 to bf16: PLACE]
+constexpr int kExportSlots = 64;
+
 template <int FORM, int TYPE, int DIM>
-__global__ __launch_bounds__(256) void agft_kv_export_kernel(ExportArgs p) {
+__global__ __launch_bounds__(4 * kExportSlots) void agft_kv_export_kernel(ExportArgs p) {
     using T = typename Dense<TYPE>::type;
-    const int64_t count = p.n * p.heads * DIM;
-    for (int64_t id = (int64_t)blockIdx.x * blockDim.x + threadIdx.x; id < count; id += (int64_t)gridDim.x * blockDim.x) {
-        const int d = (int)(id % DIM);
-        const int64_t rest = id / DIM;
-        const int head = (int)(rest % p.heads);
-        const int64_t t = rest / p.heads;
-        const int64_t slot = p.slots[t];
-        const bool here = slot >= 0 && slot < p.pool_tokens;
-        const int64_t page_id = here ? slot >> p.shift : 0;
-        const int pos = (int)(slot & (p.page - 1)), m = pos & 15, dg = d / 64, in = d % 64;
-        const int64_t base = (page_id * p.heads + head) * 2;
-        const size_t at[2] = {(size_t)(((in >> 4) * 16 + m) * 16 + (in & 15)),
-                              (size_t)(((m >> 2) * 16 + (in & 15)) * 16 + (in >> 4) * 4 + (m & 3))};
-        for (int side = 0; side < 2; ++side) {
-            float x[4] = {0.0f, 0.0f, 0.0f, 0.0f};
-            if (here) {
-                const uint8_t c = (uint8_t)p.codes[(base + side) * p.page * DIM +
-                                                   ((size_t)(pos >> 4) * (DIM / 64) + dg) * kBlockBytes + at[side]];
-                Code<FORM>::unpack4(c, x);
-                const int e = p.exps[base + side];
-                x[0] = ldexpf(x[0], e);
-            }
-            static_cast<T *>(p.data[side])[t * p.token_stride[side] + head * p.head_stride[side] + d] =
-                Dense<TYPE>::from(x[0]);
+    const int part = threadIdx.x & 3, head = blockIdx.y, side = blockIdx.z;
+    const int64_t t = (int64_t)blockIdx.x * kExportSlots + (threadIdx.x >> 2);
+    if (t >= p.n) return;
+    const int64_t slot = p.slots[t];
+    const bool here = slot >= 0 && slot < p.pool_tokens;
+    const int64_t base = ((here ? slot >> p.shift : 0) * p.heads + head) * 2 + side;
+    const int pos = (int)(slot & (p.page - 1)), m = pos & 15;
+    const char *block = p.codes + base * p.page * DIM + (pos >> 4) * (kBlockTokens * DIM);
+    const float f = here ? pow2(p.exps[base]) : 0.0f;
+    T *dst = static_cast<T *>(p.data[side]) + t * p.token_stride[side] + head * p.head_stride[side] + 16 * part;
+#pragma unroll
+    for (int dg = 0; dg < DIM / kBlockDims; ++dg) {
+        uint32_t w[4] = {0, 0, 0, 0};
+        if (here && side == 0) {
+            const uint4 v = *reinterpret_cast<const uint4 *>(block + dg * kBlockBytes + (16 * part + m) * 16);
+            w[0] = v.x, w[1] = v.y, w[2] = v.z, w[3] = v.w;
+        } else if (here) {
+            const uint8_t *v = reinterpret_cast<const uint8_t *>(block) + dg * kBlockBytes + (m >> 2) * 256 + 4 * part + (m & 3);
+#pragma unroll
+            for (int j = 0; j < 16; ++j) w[j >> 2] |= (uint32_t)v[16 * j] << (8 * (j & 3));
         }
+        __attribute__((aligned(16))) T out[16];
+#pragma unroll
+        for (int j = 0; j < 4; ++j) {
+            float x[4];
+            Code<FORM>::unpack4(w[j], x);
+#pragma unroll
+            for (int i = 0; i < 4; ++i) out[4 * j + i] = Dense<TYPE>::from(x[i] * f);
+        }
+#pragma unroll
+        for (int j = 0; j < (int)sizeof(out) / 16; ++j)
+            reinterpret_cast<uint4 *>(dst + dg * kBlockDims)[j] = reinterpret_cast<const uint4 *>(out)[j];
     }
 }
 
@@ -792,10 +804,9 @@ int agft_kv_export(const agft_kv_config *cfg, const void *d_cache, size_t cache_
     p.n = n;
     p.pool_tokens = (int64_t)cfg->pages * cfg->page;
     p.heads = cfg->heads, p.page = cfg->page, p.shift = log2_of(cfg->page);
-    const int64_t blocks = (n * cfg->heads * cfg->dim + 255) / 256;
-    const dim3 grid((unsigned)(blocks < 65536 ? blocks : 65536));
+    const dim3 grid((unsigned)((n + kExportSlots - 1) / kExportSlots), (unsigned)cfg->heads, 2);
     return by_form_type_dim(cfg, k->type, [&](auto form, auto type, auto dim) {
-        agft_kv_export_kernel<form(), type(), dim()><<<grid, dim3(256), 0, static_cast<hipStream_t>(stream)>>>(p);
+        agft_kv_export_kernel<form(), type(), dim()><<<grid, dim3(4 * kExportSlots), 0, static_cast<hipStream_t>(stream)>>>(p);
         return launched();
     });
 }

@@ -200,6 +200,9 @@ class KvCache(_OnStream):
 
     def __init__(self, cfg, device="cuda", stream=None):
         self._init(cfg, device, stream)
+        # what calls tell the library of their tensors (a front end is not thread-safe, like a Tuner)
+        self._d0, self._d1 = L.agft_kv_dense(), L.agft_kv_dense()
+        self._b0, self._b1 = ctypes.byref(self._d0), ctypes.byref(self._d1)
         self.nbytes = self._lib.agft_kv_cache_bytes(self._cfg)
         self.buffer = self._buffer(self.nbytes, "cache")
         self.ptr = self.buffer.data_ptr()
@@ -236,17 +239,22 @@ class KvCache(_OnStream):
         if t.device != self.device:
             raise ValueError(f"expected a tensor on {self.device}")
 
-    def _dense(self, t, heads, rows, what, types=TYPES):
-        """The agft_kv_dense of a [tokens][heads][dim] tensor of at least `rows` tokens."""
-        shape, strides = t.shape, t.stride()
-        if (t.device != self.device or t.dtype not in types or len(shape) != 3 or shape[0] < rows or
-                shape[1] != heads or shape[2] != self.cfg.dim or strides[2] != 1):
+    def _dense(self, d, t, heads, rows, what, types=TYPES):
+        """Fill the agft_kv_dense d from a [tokens][heads][dim] tensor of at least `rows` tokens."""
+        try:
+            n, h, dim = t.shape
+            token, head, one = t.stride()
+            kind = types[t.dtype]
+        except (ValueError, KeyError):
+            n = h = dim = one = -1
+        if n < rows or h != heads or dim != self.cfg.dim or one != 1 or t.get_device() != self.device.index:
             raise ValueError(f"{what} must be [{rows} or more][{heads}][{self.cfg.dim}] on {self.device}, "
                              f"{' or '.join(str(d) for d in types)}, with contiguous numbers of a head")
-        per = 16 // t.element_size()
-        if t.data_ptr() % 16 or strides[0] % per or strides[1] % per:
+        ptr = t.data_ptr()
+        per = 7 if kind != L.AGFT_KV_FP32 else 3
+        if ptr & 15 or token & per or head & per:
             raise ValueError(f"{what}: rows must start at multiples of 16 bytes")
-        return L.agft_kv_dense(t.data_ptr(), strides[0], strides[1], types[t.dtype])
+        d.data, d.token_stride, d.head_stride, d.type = ptr, token, head, kind
 
     def append(self, step, k, v):
         """Store the window's keys and values, [max_tokens][heads][dim] each
@@ -254,9 +262,10 @@ class KvCache(_OnStream):
         H, n = self.cfg.heads, step.max_tokens
         if k.dtype != v.dtype:
             raise ValueError("k and v must have one type")
-        dk, dv = self._dense(k, H, n, "k"), self._dense(v, H, n, "v")
-        code = self._lib.agft_kv_append(self._cfg, self.ptr, self.nbytes, step.ptr, step.nbytes, n, ctypes.byref(dk),
-                                        ctypes.byref(dv), self._s())
+        self._dense(self._d0, k, H, n, "k")
+        self._dense(self._d1, v, H, n, "v")
+        code = self._lib.agft_kv_append(self._cfg, self.ptr, self.nbytes, step.ptr, step.nbytes, n, self._b0, self._b1,
+                                        self._s())
         if code != L.AGFT_OK:
             L.check("agft_kv_append", code)
 
@@ -272,13 +281,14 @@ class KvCache(_OnStream):
             out = torch.empty(n, hq, c.dim, dtype=q.dtype, device=self.device)
         elif out.dtype != q.dtype:
             raise ValueError("q and out must have one type")
-        dq, do = self._dense(q, hq, n, "q", HALVES), self._dense(out, hq, n, "out", HALVES)
+        self._dense(self._d0, q, hq, n, "q", HALVES)
+        self._dense(self._d1, out, hq, n, "out", HALVES)
         if lse is not None and (lse.device != self.device or lse.dtype != torch.float32 or
                                 lse.shape != (n, hq) or not lse.is_contiguous()):
             raise ValueError(f"lse must be a contiguous float32 tensor [{n}][{hq}] on {self.device}")
         work = step.work()
         code = self._lib.agft_kv_attend(self._cfg, self.ptr, self.nbytes, tables.ptr, tables.nbytes, step.ptr,
-                                        step.nbytes, n, step.max_new, ctypes.byref(dq), ctypes.byref(do),
+                                        step.nbytes, n, step.max_new, self._b0, self._b1,
                                         None if lse is None else lse.data_ptr(),
                                         1.0 / math.sqrt(c.dim) if scale is None else float(scale), work.data_ptr(),
                                         work.numel(), self._s())
@@ -294,13 +304,12 @@ class KvCache(_OnStream):
         if dtype not in TYPES:
             raise ValueError(f"no exports in {dtype}")
         n, H, D = slots.numel(), self.cfg.heads, self.cfg.dim
-        k = torch.empty(n, H, D, dtype=dtype, device=self.device)
-        v = torch.empty(n, H, D, dtype=dtype, device=self.device)
+        k, v = torch.empty(2, n, H, D, dtype=dtype, device=self.device)
         if n:
-            dk = L.agft_kv_dense(k.data_ptr(), H * D, D, TYPES[dtype])
-            dv = L.agft_kv_dense(v.data_ptr(), H * D, D, TYPES[dtype])
-            code = self._lib.agft_kv_export(self._cfg, self.ptr, self.nbytes, slots.data_ptr(), n, ctypes.byref(dk),
-                                            ctypes.byref(dv), self._s())
+            for d, t in ((self._d0, k), (self._d1, v)):
+                d.data, d.token_stride, d.head_stride, d.type = t.data_ptr(), H * D, D, TYPES[dtype]
+            code = self._lib.agft_kv_export(self._cfg, self.ptr, self.nbytes, slots.data_ptr(), n, self._b0, self._b1,
+                                            self._s())
             if code != L.AGFT_OK:
                 L.check("agft_kv_export", code)
         return k, v
