@@ -17,10 +17,11 @@ struct PlanArgs {
     const int32_t *add;
     const int32_t *counters, *lengths;
     int32_t *table, *ring;
-    int32_t *out_counters, *starts, *granted, *out_lengths, *need, *touched, *back, *sums, *arrived, *runs;
+    int32_t *out_counters, *starts, *granted, *out_lengths, *tiles, *need, *touched, *back, *sums, *arrived, *runs;
     Work *works;
+    Item *items;
     int64_t *slots;
-    int32_t requests, row_pages, pages, page, shift, group, max_tokens;
+    int32_t requests, row_pages, pages, page, shift, group, heads, max_tokens;
 };
 
 __device__ __forceinline__ int32_t pages_of(int32_t n, int32_t page, int32_t shift) { return (n + page - 1) >> shift; }
@@ -65,11 +66,43 @@ __device__ __forceinline__ uint32_t add_sat(uint32_t a, uint32_t b) { return __b
 struct PlanLds {
     uint32_t asked[2][kPlanThreads / 64];
     int32_t sums[kPlanSums][kPlanThreads / 64];
+    float cost[kPlanThreads / 64];
 };
+
+// Sums over the threads before this one, and over all of them.
+__device__ __forceinline__ void plan_scan(const int32_t *mine, int32_t *before, int32_t *all, PlanLds &lds) {
+    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+    int32_t in[kPlanSums];
+#pragma unroll
+    for (int k = 0; k < kPlanSums; ++k) in[k] = mine[k];
+#pragma unroll
+    for (int s = 1; s < 64; s *= 2)
+#pragma unroll
+        for (int k = 0; k < kPlanSums; ++k) {
+            const int32_t x = __shfl_up(in[k], s, 64);
+            if (lane >= s) in[k] += x;
+        }
+    __syncthreads();                        // (an earlier scan's sums have been read)
+#pragma unroll
+    for (int k = 0; k < kPlanSums; ++k)
+        if (lane == 63) lds.sums[k][wave] = in[k];
+    __syncthreads();
+#pragma unroll
+    for (int k = 0; k < kPlanSums; ++k) {
+        before[k] = in[k] - mine[k];
+        all[k] = 0;
+#pragma unroll
+        for (int w = 0; w < kPlanThreads / 64; ++w) {
+            if (w < wave) before[k] += lds.sums[k][w];
+            all[k] += lds.sums[k][w];
+        }
+    }
+}
 
 // The requests [r0 + kPlanPer * thread, ..) of one thread.
 struct PlanPart {
     int32_t past[kPlanPer], held[kPlanPer], granted[kPlanPer], after[kPlanPer], first[kPlanPer], need[kPlanPer];
+    int32_t tiles[kPlanPer];                // tiles of many rows
     int32_t sums[kPlanSums][kPlanPer];      // sums over the chunk's earlier requests
     int32_t all[kPlanSums];                 // over the chunk
     uint32_t tokens;                        // asked by the chunk and all before it
@@ -123,11 +156,12 @@ __device__ __forceinline__ void plan_chunk(const PlanArgs &p, int r0, uint32_t n
         const int32_t rows = last - o.first[j];                         // rows of the window's tensors
         const int64_t wide = (int64_t)rows * p.group;
         const bool few = wide <= kFewRows;
+        o.tiles[j] = rows == 0 || few ? 0 : (int32_t)((wide + kTileRows - 1) / kTileRows);
         const int32_t v[kPlanSums] = {
             ok ? pages_of(o.after[j], p.page, p.shift) - (a[j].past >> p.shift) : 0,    // pages written to
             // units of few rows: every 16 rows read the request's tokens (one unit where there are none)
             rows == 0 || !few ? 0 : (ok ? (o.after[j] + kUnit - 1) / kUnit : 1) * (((int32_t)wide + kRowTile - 1) / kRowTile),
-            rows == 0 || few ? 0 : (int32_t)((wide + kTileRows - 1) / kTileRows),       // tiles of many rows
+            o.tiles[j],                                                                 // tiles of many rows
             a[j].ends ? a[j].held : 0,                                                  // pages given back
             a[j].wants && !ok ? 1 : 0,
             ok ? a[j].need : 0,
@@ -139,32 +173,70 @@ __device__ __forceinline__ void plan_chunk(const PlanArgs &p, int r0, uint32_t n
         }
         need_at = need_to, tok_at = tok_to;
     }
-    int32_t in[kPlanSums];
-#pragma unroll
-    for (int k = 0; k < kPlanSums; ++k) in[k] = mine[k];
-#pragma unroll
-    for (int s = 1; s < 64; s *= 2)
-#pragma unroll
-        for (int k = 0; k < kPlanSums; ++k) {
-            const int32_t x = __shfl_up(in[k], s, 64);
-            if (lane >= s) in[k] += x;
-        }
+    int32_t before[kPlanSums];
+    plan_scan(mine, before, o.all, lds);
 #pragma unroll
     for (int k = 0; k < kPlanSums; ++k)
-        if (lane == 63) lds.sums[k][wave] = in[k];
+#pragma unroll
+        for (int j = 0; j < kPlanPer; ++j) o.sums[k][j] += before[k];
+}
+
+// Many rows: in which order the workgroups take their tiles, the longest first
+// (by a factor of two), and which tiles several workgroups share, so that few
+// tiles over many tokens fill the chip.  A tile's parts cover at least
+// kPartTiles key tiles and at least an even share of all.  (For up to
+// kPlanChunk requests; beyond, tiles go by request, in one part.)
+constexpr int kPartTiles = 16;
+constexpr int kMaxParts = 64;
+
+__device__ __forceinline__ void plan_order(const PlanArgs &p, const PlanPart &o, PlanLds &lds, int32_t *base, int32_t *parts,
+                                           int32_t *items) {
+    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+    float cost = 0.0f;                                                  // key tiles of all tiles
+#pragma unroll
+    for (int j = 0; j < kPlanPer; ++j)
+        if (o.tiles[j] > 0) cost += (float)o.tiles[j] * (float)((o.after[j] + kUnit - 1) / kUnit);
+#pragma unroll
+    for (int s = 1; s < 64; s *= 2) cost += __shfl_xor(cost, s, 64);
+    if (lane == 0) lds.cost[wave] = cost;
     __syncthreads();
+    cost = 0.0f;
+#pragma unroll
+    for (int w = 0; w < kPlanThreads / 64; ++w) cost += lds.cost[w];
+    const float even = ceilf(cost / (float)tile_slots(p.heads));
+    const float least = even > (float)kPartTiles ? even : (float)kPartTiles;
+    int32_t mine[kPlanSums] = {}, at[kPlanPer], kind[kPlanPer];
+#pragma unroll
+    for (int j = 0; j < kPlanPer; ++j) {
+        const int32_t keys = o.granted[j] > 0 ? (o.after[j] + kUnit - 1) / kUnit : 1;
+        const float share = ceilf((float)keys / least);
+        parts[j] = share > (float)kMaxParts ? kMaxParts : share > 1.0f ? (int32_t)share : 1;
+        kind[j] = parts[j] > 1 ? 0 : keys >= 64 ? 1 : keys >= 32 ? 2 : keys >= 16 ? 3 : keys >= 8 ? 4 : 5;
+        at[j] = 0;
+#pragma unroll
+        for (int k = 0; k < kPlanSums; ++k)
+            if (k == kind[j]) at[j] = mine[k], mine[k] += o.tiles[j] * parts[j];
+    }
+    int32_t before[kPlanSums], all[kPlanSums];
+    plan_scan(mine, before, all, lds);
+    *items = 0;
 #pragma unroll
     for (int k = 0; k < kPlanSums; ++k) {
-        int32_t before = in[k] - mine[k];
-        o.all[k] = 0;
 #pragma unroll
-        for (int w = 0; w < W; ++w) {
-            if (w < wave) before += lds.sums[k][w];
-            o.all[k] += lds.sums[k][w];
-        }
-#pragma unroll
-        for (int j = 0; j < kPlanPer; ++j) o.sums[k][j] += before;
+        for (int j = 0; j < kPlanPer; ++j)
+            if (k == kind[j]) base[j] = *items + before[k] + at[j];
+        *items += all[k];
     }
+}
+
+// The item(s) of the tile that begins with one of token k's rows, if one does;
+// a request's last tile, which sees the most tokens, comes first.
+__device__ __forceinline__ void plan_items(const PlanArgs &p, int32_t i, int32_t k, int32_t tiles, int32_t base,
+                                           int32_t parts) {
+    const int64_t row = (int64_t)k * p.group, tile = (row + kTileRows - 1) / kTileRows;
+    if (tiles == 0 || tile * kTileRows >= row + p.group) return;
+    Item *item = p.items + base + (int64_t)(tiles - 1 - tile) * parts;
+    for (int32_t z = 0; z < parts; ++z) item[z] = Item{i, (int32_t)tile, z, parts};
 }
 
 // The window's totals: ends of the prefix sums, and the counters.
@@ -247,7 +319,7 @@ __device__ __forceinline__ int32_t last_at_most(const int32_t *a, int32_t lo, in
 __global__ __launch_bounds__(kPlanThreads) void agft_kv_plan_kernel(PlanArgs p) {
     __shared__ PlanLds lds;
     __shared__ int32_t s_first[kPlanChunk], s_past[kPlanChunk], s_granted[kPlanChunk], s_need[kPlanChunk],
-        s_touched[kPlanChunk], s_back[kPlanChunk];
+        s_touched[kPlanChunk], s_back[kPlanChunk], s_tiles[kPlanChunk], s_items[kPlanChunk], s_parts[kPlanChunk];
     const int32_t head = p.counters[0], free_pages = p.counters[1];
     PlanPart o;
     plan_chunk(p, 0, 0, 0, free_pages, lds, o);
@@ -257,13 +329,19 @@ __global__ __launch_bounds__(kPlanThreads) void agft_kv_plan_kernel(PlanArgs p) 
         s_first[i0 + j] = o.first[j], s_past[i0 + j] = o.past[j], s_granted[i0 + j] = o.granted[j];
         s_need[i0 + j] = o.need[j], s_touched[i0 + j] = o.sums[0][j], s_back[i0 + j] = o.sums[3][j];
     }
+    if (o.all[2] > 0) {
+        int32_t base[kPlanPer], parts[kPlanPer];
+        plan_order(p, o, lds, base, parts, &o.all[2]);
+#pragma unroll
+        for (int j = 0; j < kPlanPer; ++j) s_tiles[i0 + j] = o.tiles[j], s_items[i0 + j] = base[j], s_parts[i0 + j] = parts[j];
+    }
     if (blockIdx.x == 0) {
 #pragma unroll
         for (int j = 0; j < kPlanPer; ++j) {
             const int i = i0 + j;
             if (i >= p.requests) continue;
             p.starts[i] = o.first[j], p.granted[i] = o.granted[j], p.out_lengths[i] = o.after[j];
-            p.works[i] = Work{o.sums[1][j], o.sums[2][j], o.first[j], o.granted[j], o.after[j], {0, 0, 0}};
+            p.works[i] = Work{o.sums[1][j], 0, o.first[j], o.granted[j], o.after[j], {0, 0, 0}};
         }
         if (threadIdx.x == 0) plan_totals(p, o.tokens, o.all, head, free_pages);
         plan_arrived(p);
@@ -273,6 +351,7 @@ __global__ __launch_bounds__(kPlanThreads) void agft_kv_plan_kernel(PlanArgs p) 
     for (int64_t t0 = (int64_t)blockIdx.x * kPlanTokens; t0 < p.max_tokens; t0 += (int64_t)gridDim.x * kPlanTokens)
         for (int64_t t = t0 + threadIdx.x; t < t0 + kPlanTokens && t < p.max_tokens; t += kPlanThreads) {
             const int32_t i = t < total ? last_at_most(s_first, 0, p.requests, (int32_t)t) : 0;
+            if (t < total && o.all[2] > 0) plan_items(p, i, (int32_t)t - s_first[i], s_tiles[i], s_items[i], s_parts[i]);
             if (t < total && s_granted[i] > 0)
                 plan_token(p, t, i, s_past[i], (int32_t)t - s_first[i], s_need[i], s_touched[i], head);
             else
@@ -313,8 +392,8 @@ __global__ __launch_bounds__(kPlanThreads) void agft_kv_plan_sums_kernel(PlanArg
         const int i = r0 + threadIdx.x * kPlanPer + j;
         if (i >= p.requests) continue;
         p.starts[i] = o.first[j], p.granted[i] = o.granted[j], p.out_lengths[i] = o.after[j], p.need[i] = o.need[j];
-        p.touched[i] = o.sums[0][j], p.back[i] = o.sums[3][j];
-        p.works[i] = Work{o.sums[1][j], o.sums[2][j], o.first[j], o.granted[j], o.after[j], {0, 0, 0}};
+        p.touched[i] = o.sums[0][j], p.tiles[i] = o.sums[2][j], p.back[i] = o.sums[3][j];
+        p.works[i] = Work{o.sums[1][j], 0, o.first[j], o.granted[j], o.after[j], {0, 0, 0}};
     }
     if (threadIdx.x == 0) {
         for (int k = 0; k < kPlanSums; ++k) p.sums[blockIdx.x * kPlanSums + k] = o.all[k];
@@ -355,7 +434,6 @@ __global__ __launch_bounds__(kPlanThreads) void agft_kv_plan_slots_kernel(PlanAr
         const bool live = i < p.requests;
         if (live) {
             p.works[i].few += s_off[1][i / kPlanChunk];
-            p.works[i].many += s_off[2][i / kPlanChunk];
         }
         const bool ends = live && p.add[i] < 0;
         const Ask a = ask_of(p, ends ? p.lengths[i] : 0, 0);
@@ -378,6 +456,12 @@ __global__ __launch_bounds__(kPlanThreads) void agft_kv_plan_slots_kernel(PlanAr
             int32_t i = 0;
             if (t < total)
                 i = near ? lo + last_at_most(s_first, 0, hi - lo, (int32_t)t) : last_at_most(p.starts, lo, hi, (int32_t)t);
+            if (t < total && s_all[2] > 0) {
+                const int32_t first = p.starts[i], rows = p.starts[i + 1] - first;
+                const int64_t wide = (int64_t)rows * p.group;
+                const int32_t tiles = wide <= kFewRows ? 0 : (int32_t)((wide + kTileRows - 1) / kTileRows);
+                plan_items(p, i, (int32_t)t - first, tiles, s_off[2][i / kPlanChunk] + p.tiles[i], 1);
+            }
             if (t < total && p.granted[i] > 0)
                 plan_token(p, t, i, ask_of(p, p.lengths[i], 0).past, (int32_t)t - p.starts[i], p.need[i],
                            p.touched[i] + s_off[0][i / kPlanChunk], head);
@@ -720,10 +804,11 @@ int agft_kv_plan(const agft_kv_config *cfg, void *d_tables, size_t tables_bytes,
     p.add = d_add;
     p.counters = tv.counters, p.lengths = tv.lengths, p.table = tv.table, p.ring = tv.ring;
     p.out_counters = sv.counters, p.starts = sv.starts, p.granted = sv.granted, p.out_lengths = sv.lengths;
-    p.works = reinterpret_cast<Work *>(base + L.works), p.need = part(L.need), p.touched = part(L.touched);
+    p.works = reinterpret_cast<Work *>(base + L.works), p.need = part(L.need), p.touched = part(L.touched), p.tiles = part(L.tiles);
     p.back = part(L.back), p.sums = part(L.sums), p.arrived = part(L.arrived), p.runs = part(L.runs), p.slots = sv.slots;
     p.requests = cfg->requests, p.row_pages = cfg->row_pages, p.pages = cfg->pages, p.page = cfg->page;
-    p.shift = log2_of(cfg->page), p.group = cfg->group, p.max_tokens = max_tokens;
+    p.shift = log2_of(cfg->page), p.group = cfg->group, p.heads = cfg->heads, p.max_tokens = max_tokens;
+    p.items = reinterpret_cast<Item *>(base + L.items);
     const hipStream_t hs = static_cast<hipStream_t>(stream);
     const int64_t by_tokens = ((int64_t)max_tokens + kPlanTokens - 1) / kPlanTokens;
     const dim3 grid((unsigned)(by_tokens < 2048 ? by_tokens : 2048));

@@ -15,6 +15,7 @@ struct AttendArgs {
     const char *codes;
     const int32_t *exps, *table;
     const Work *works;
+    const Item *items;
     const char *q;
     char *out;
     float *lse, *partial;
@@ -171,7 +172,7 @@ constexpr float kLn2 = 0.6931471805599453f;
 struct Works {
     const Work *w;
     int n;
-    int4 a;             // few, many, start, granted of request (lane)
+    int4 a;             // few, items, start, granted of request (lane)
     int length;
     int4 total;
     __device__ __forceinline__ Works(const Work *works, int requests) : w(works), n(requests) {
@@ -183,16 +184,16 @@ struct Works {
             length = w[k].length;
         }
     }
-    // the last request whose few (many) is at most x
-    __device__ __forceinline__ int find(bool many, int32_t x) const {
+    // the last request whose few is at most x
+    __device__ __forceinline__ int find(int32_t x) const {
         const int lane = threadIdx.x & 63;
         if (n <= 64) {
-            const int hits = __popcll(__ballot(lane < n && (many ? a.y : a.x) <= x));
+            const int hits = __popcll(__ballot(lane < n && a.x <= x));
             return __builtin_amdgcn_readfirstlane(hits < 1 ? 0 : hits - 1);
         }
-        return find_last([&](int k) { return many ? w[k].many : w[k].few; }, n, x);
+        return find_last([&](int k) { return w[k].few; }, n, x);
     }
-    // a request's own entry, and the next one's few, many, start
+    // a request's own entry, and the next one's few, items, start
     __device__ __forceinline__ void get(int i, int4 &own, int &len, int4 &next) const {
         if (n <= 64) {
             const auto at = [&](int v) { return __builtin_amdgcn_readlane(v, i); };
@@ -218,7 +219,7 @@ struct Segment {
 };
 __device__ __forceinline__ Segment segment_of(const AttendArgs &p, const Works &works, int32_t x) {
     Segment s;
-    s.request = works.find(false, x / p.heads);
+    s.request = works.find(x / p.heads);
     int4 own, next;
     works.get(s.request, own, s.length, next);
     const int32_t base = own.x, all = next.x - base;
@@ -633,20 +634,18 @@ __global__ __launch_bounds__(64 * kTileWaves, DIM > 128 ? 1 : 2) void agft_kv_ti
     __shared__ float4 s_scale[4][4];                       // by tile % 4: a block's factor of the scores, ev, 2^-ev
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     const int h = lane >> 5, n = lane & 31;
-    const int head = blockIdx.x % p.heads;
-    const Works works(p.works, p.requests);
-    const int back = blockIdx.x / p.heads, total = works.total.y;
-    if (back >= total) return;
-    const int tile = total - 1 - back;
-    const int i = works.find(true, tile);
-    int4 own, next;
-    int len;
-    works.get(i, own, len, next);
-    const int first = own.z, granted = own.w, all_rows = (next.z - own.z) * p.group;
-    const int row0 = (tile - own.y) * kTileRows;
+    const int head = blockIdx.x % p.heads, place = blockIdx.x / p.heads;
+    if (place >= p.works[p.requests].items) return;
+    const Item item = p.items[place];
+    const int i = item.request;
+    const int4 own = *reinterpret_cast<const int4 *>(p.works + i);
+    const int len = p.works[i].length;
+    const int first = own.z, granted = own.w, all_rows = (p.works[i + 1].start - first) * p.group;
+    const int row0 = item.tile * kTileRows;
     const int rows = all_rows - row0 < kTileRows ? all_rows - row0 : kTileRows;
     if (rows <= 0) return;
     if (granted <= 0) {
+        if (item.part > 0) return;
         for (int c = threadIdx.x; c < rows * DIM / 4; c += blockDim.x) {
             const int r = c / (DIM / 4), d = c % (DIM / 4) * 4;
             store_row4<TYPE, DIM>(p, first, head, row0 + r, d, (float4v){0, 0, 0, 0}, 0.0f);
@@ -658,8 +657,11 @@ __global__ __launch_bounds__(64 * kTileWaves, DIM > 128 ? 1 : 2) void agft_kv_ti
     const bool busy = 32 * wave < rows, row_here = 32 * wave + n < rows;
     const int row = row_here ? row0 + 32 * wave + n : row0 + rows - 1;
     const int limit = past + row / p.group + 1;            // keys that this lane's row sees
-    const int whole = (past + row0 / p.group + 1) / kTileKeys;             // tiles that every row sees whole
-    const int tiles = (past + (row0 + rows - 1) / p.group + kTileKeys) / kTileKeys;
+    const int all_tiles = (past + (row0 + rows - 1) / p.group + kTileKeys) / kTileKeys;
+    const int begin = (int)((int64_t)all_tiles * item.part / item.parts);   // this part's tiles
+    const int tiles = (int)((int64_t)all_tiles * (item.part + 1) / item.parts);
+    int whole = (past + row0 / p.group + 1) / kTileKeys;                    // tiles that every row sees whole
+    if (whole > tiles) whole = tiles;
     const int blocks = (len + kBlockTokens - 1) / kBlockTokens;
 
     typename H::x8 q[DG * 4];
@@ -696,7 +698,7 @@ __global__ __launch_bounds__(64 * kTileWaves, DIM > 128 ? 1 : 2) void agft_kv_ti
 #pragma unroll
             for (int dg = 0; dg < DG; ++dg) ahead[1][dg] = *reinterpret_cast<const uint4v *>(values + dg * kBlockBytes);
         }
-        if ((t & 63) == 0) look_up(t);
+        if ((t & 63) == 0 || !both) look_up(t & ~63);
         int b = t * 4 + wave;
         if (b >= blocks) b = blocks - 1;
         const int64_t page_id = __builtin_amdgcn_readlane(id, t & 63);
@@ -821,20 +823,18 @@ __global__ __launch_bounds__(64 * kTileWaves, DIM > 128 ? 1 : 2) void agft_kv_ti
         s[0] = z[0], s[1] = z[1];
     };
 
-    fetch(0, false);
-    stage(0, false);
-    fetch(1, true);
+    fetch(begin, false);
+    stage(begin, false);
+    fetch(begin + 1, true);
     __syncthreads();
-    if (busy) scores(1, s);                                // of tile 0, whose keys lie in the buffer of step -1
-    stage(1, true);
-    if (!busy) {                                           // no rows of its own: only fetches
-        for (int t = 0; t < tiles; ++t) {
+    if (busy) scores((begin + 1) & 1, s);                  // of the first tile, whose keys lie in the buffer of the step before
+    stage(begin + 1, true);
+    if (!busy)                                             // no rows of its own: only fetches
+        for (int t = begin; t < tiles; ++t) {
             __syncthreads();
             if (t + 1 < tiles) fetch(t + 2, true), stage(t + 2, true);
         }
-        return;
-    }
-    int t = 0;
+    int t = busy ? begin : tiles;
     for (; t < whole; ++t) {
         __syncthreads();                                   // this step's operands are in LDS, and the other buffer is read
         if (t + 1 < tiles) fetch(t + 2, true);
@@ -848,14 +848,55 @@ __global__ __launch_bounds__(64 * kTileWaves, DIM > 128 ? 1 : 2) void agft_kv_ti
         if (t + 1 < tiles) stage(t + 2, true);
     }
     l = halves_sum(l);
-    if (!row_here) return;
+    // rows 8 z + 4 h.. of O^T: numbers 64 dg + 32 (z / 2) + 16 T + ..
+    const auto number = [&](int c, int z) { return 64 * (c >> 1) + 32 * (z >> 1) + 16 * (c & 1) + 8 * (z & 1) + 4 * h; };
+    if (item.parts == 1) {
+        if (!row_here) return;
 #pragma unroll
-    for (int c = 0; c < DG * 2; ++c)
+        for (int c = 0; c < DG * 2; ++c)
 #pragma unroll
-        for (int z = 0; z < 4; ++z)                        // rows 8 z + 4 h.. of O^T: numbers 64 dg + 32 (z / 2) + 16 T + ..
-            store_row4<TYPE, DIM>(p, first, head, row, 64 * (c >> 1) + 32 * (z >> 1) + 16 * (c & 1) + 8 * (z & 1) + 4 * h,
-                                  (float4v){o[c][4 * z], o[c][4 * z + 1], o[c][4 * z + 2], o[c][4 * z + 3]}, l);
-    if (h == 0) store_lse(p, first, head, row, m, l);
+            for (int z = 0; z < 4; ++z)
+                store_row4<TYPE, DIM>(p, first, head, row, number(c, z),
+                                      (float4v){o[c][4 * z], o[c][4 * z + 1], o[c][4 * z + 2], o[c][4 * z + 3]}, l);
+        if (h == 0) store_lse(p, first, head, row, m, l);
+        return;
+    }
+    // parts meet as the pieces of few rows do
+    __shared__ int s_last;
+    constexpr int64_t PART = kTileRows * (DIM + 2);
+    float *parts = p.partial + kFewGroups * 2 * partial_floats<DIM>() + ((int64_t)(place - item.part) * p.heads + head) * PART;
+    const int64_t stride = p.heads * PART;
+    if (row_here) {
+        float *at = parts + item.part * stride;
+        const int r = row - row0;
+#pragma unroll
+        for (int c = 0; c < DG * 2; ++c)
+#pragma unroll
+            for (int z = 0; z < 4; ++z) {
+                put2(at + r * DIM + number(c, z), o[c][4 * z], o[c][4 * z + 1]);
+                put2(at + r * DIM + number(c, z) + 2, o[c][4 * z + 2], o[c][4 * z + 3]);
+            }
+        if (h == 0) put(at + kTileRows * DIM + r, m), put(at + kTileRows * (DIM + 1) + r, l);
+    }
+    if (!last_to_arrive(p.arrived + 3 * kFewGroups + (place - item.part) * p.heads + head, item.parts, &s_last)) return;
+    for (int c = threadIdx.x; c < rows * (DIM / 4); c += blockDim.x) {
+        const int r = c / (DIM / 4), d = c % (DIM / 4) * 4;
+        float top = -INFINITY, sum = 0.0f;
+        float4v all = {0, 0, 0, 0};
+#pragma unroll 4
+        for (int w = 0; w < item.parts; ++w) {
+            const float *at = parts + w * stride;
+            const float mw = get(at + kTileRows * DIM + r), lw = get(at + kTileRows * (DIM + 1) + r);
+            const float2 a = get2(at + r * DIM + d), b = get2(at + r * DIM + d + 2);
+            const float m1 = fmaxf(top, mw);
+            const float f0 = top == -INFINITY ? 0.0f : exp2f(top - m1), f1 = mw == -INFINITY ? 0.0f : exp2f(mw - m1);
+            all = all * f0 + (float4v){a.x, a.y, b.x, b.y} * f1;
+            sum = sum * f0 + lw * f1;
+            top = m1;
+        }
+        store_row4<TYPE, DIM>(p, first, head, row0 + r, d, all, sum);
+        if (d == 0) store_lse(p, first, head, row0 + r, top, sum);
+    }
 }
 
 inline int log2_of(int32_t page) { return page == 16 ? 4 : page == 32 ? 5 : page == 64 ? 6 : 7; }
@@ -868,7 +909,10 @@ extern "C" {
 
 size_t agft_kv_attend_bytes(const agft_kv_config *cfg, int32_t max_tokens) {
     if (config_status(cfg) != AGFT_OK || !tokens_ok(max_tokens)) return 0;
-    return align_up((size_t)kFewGroups * 2 * kRowTile * (cfg->dim + 2) * sizeof(float));
+    // pieces of few rows, and parts of many
+    const int64_t items = item_cap(cfg, max_tokens) * cfg->heads;
+    const size_t parts = (size_t)(items < kTileParts ? items : kTileParts);
+    return align_up(((size_t)kFewGroups * 2 * kRowTile + parts * kTileRows) * (cfg->dim + 2) * sizeof(float));
 }
 
 int agft_kv_attend(const agft_kv_config *cfg, const void *d_cache, size_t cache_bytes, const void *d_tables,
@@ -900,10 +944,8 @@ int agft_kv_attend(const agft_kv_config *cfg, const void *d_cache, size_t cache_
     p.scale = scale;
     p.requests = cfg->requests, p.row_pages = cfg->row_pages, p.pages = cfg->pages;
     p.page = cfg->page, p.shift = log2_of(cfg->page), p.heads = cfg->heads, p.group = cfg->group;
-    // tiles of many rows: the rows' own and a last one of each request that has more than kFewRows
-    const int64_t all_rows = (int64_t)max_tokens * cfg->group;
-    const int64_t many = all_rows / (kFewRows + 1) < cfg->requests ? all_rows / (kFewRows + 1) : cfg->requests;
-    const int64_t tile_groups = (all_rows / kTileRows + many) * cfg->heads;
+    p.items = reinterpret_cast<const Item *>(static_cast<const char *>(d_step) + step_layout(cfg, max_tokens).items);
+    const int64_t tile_groups = item_cap(cfg, max_tokens) * cfg->heads;
     if (tile_groups > INT32_MAX) return AGFT_E_INVAL;
     const auto go = [&](auto form, auto type, auto dim) {
         const hipStream_t hs = static_cast<hipStream_t>(stream);

@@ -22,7 +22,9 @@ constexpr int kRowTile = 16;       // query rows (tokens x group) of a tile of t
 constexpr int kFewRows = 64;       // query rows of a request up to which that takes it
 constexpr int kTileRows = 128;     // query rows of a tile of the attention over many rows
 constexpr int kFewGroups = 1024;   // workgroups, at most, that share the work of few rows
-constexpr int kArrivals = 3 * kFewGroups;   // counters of a window's joins
+constexpr int kTileSlots = 512;    // workgroups of the attention over many rows that run at once
+constexpr int kTileParts = 2 * kTileSlots;  // of them, at most, that share rows with others
+constexpr int kArrivals = 3 * kFewGroups + kTileParts;   // counters of a window's joins
 constexpr int kPlanChunk = 1024;   // requests whose prefix sums one workgroup makes
 constexpr int kPlanSums = 6;       // prefix sums per request that count granted tokens only
 constexpr int kMinExp = -64;
@@ -65,14 +67,36 @@ inline TablesLayout tables_layout(const agft_kv_config *c) {
 // behind the requests', holds the totals and the last start.
 struct __attribute__((aligned(16))) Work {
     int32_t few;      // units of few rows of the requests before this one
-    int32_t many;     // tiles of many rows of the requests before this one
+    int32_t items;    // in the last entry: items of many rows
     int32_t start;    // first row
     int32_t granted, length;
     int32_t pad[3];
 };
 
+// One workgroup's task, per head, in the attention over many rows: part `part`
+// of `parts` of the tokens that tile `tile` of the request's rows sees.
+struct __attribute__((aligned(16))) Item {
+    int32_t request, tile, part, parts;
+};
+
+// Tiles of many rows: the rows' own and a last one of each request that has
+// more than kFewRows.
+inline int64_t tile_cap(const agft_kv_config *c, int64_t max_tokens) {
+    const int64_t rows = max_tokens * c->group, many = rows / (kFewRows + 1);
+    return many == 0 ? 0 : rows / kTileRows + (many < c->requests ? many : c->requests);
+}
+
+// Items run per head; a share of the chip's slots is a head's.
+__host__ __device__ inline int32_t tile_slots(int32_t heads) { return heads < kTileSlots ? kTileSlots / heads : 1; }
+
+// (parts come to at most one per tile and one per slot)
+inline int64_t item_cap(const agft_kv_config *c, int64_t max_tokens) {
+    const int64_t tiles = tile_cap(c, max_tokens);
+    return tiles == 0 ? 0 : tiles + tile_slots(c->heads);
+}
+
 struct StepLayout {
-    size_t counters, starts, granted, lengths, works, need, touched, back, sums, arrived, runs, slots, total;
+    size_t counters, starts, granted, lengths, works, tiles, need, touched, back, sums, arrived, items, runs, slots, total;
 };
 
 // Runs of one page's tokens in a window: a request's n tokens touch at most
@@ -91,11 +115,13 @@ inline StepLayout step_layout(const agft_kv_config *c, int32_t max_tokens) {
     L.granted = at, at += row;
     L.lengths = at, at += row;
     L.works = at, at += align_up(((size_t)c->requests + 1) * sizeof(Work));
+    L.tiles = at, at += row;
     L.need = at, at += row;
     L.touched = at, at += row;
     L.back = at, at += row;
     L.sums = at, at += align_up((size_t)kPlanSums * ((c->requests + kPlanChunk - 1) / kPlanChunk) * 4);
     L.arrived = at, at += align_up((size_t)kArrivals * 4);
+    L.items = at, at += align_up((size_t)item_cap(c, max_tokens) * sizeof(Item));
     L.runs = at, at += align_up(((size_t)run_cap(c, max_tokens) + 1) * 4);
     L.slots = at, at += align_up((size_t)max_tokens * 8);
     L.total = at;
