@@ -31,13 +31,16 @@ __device__ __forceinline__ int32_t pages_of(int32_t n, int32_t page, int32_t shi
 // A window's table work is prefix sums over the requests and a search for every
 // token's request: a few hundred KB at most, so latency is all of it.  Up to
 // 1,024 requests every workgroup makes all the prefix sums for itself, in LDS,
-// and then its own 1,024 tokens' slots: one launch, no workgroup waits for
+// and then its own tokens' slots: one launch, no workgroup waits for
 // another.  Beyond that one launch makes the sums of 1,024 requests per
 // workgroup, and a second adds the other chunks' totals while it makes the
 // slots.
 constexpr int kPlanThreads = 256;
-constexpr int kPlanPer = kPlanChunk / kPlanThreads;    // requests of a thread
-constexpr int kPlanTokens = 1024;                      // tokens of a workgroup
+constexpr int kSumsThreads = 1024;                     // of a workgroup that makes one chunk's sums
+template <int THREADS>
+constexpr int plan_per = kPlanChunk / THREADS;         // requests of a thread
+constexpr int kPlanTokens = 256;                       // tokens of a workgroup at a time
+constexpr int kPlanNear = 1024;                        // requests whose starts it keeps in LDS
 
 // What a request asks of the window, from its own lengths alone.
 struct Ask {
@@ -63,14 +66,16 @@ __device__ __forceinline__ Ask ask_of(const PlanArgs &p, int32_t past, int32_t a
 // above every limit.
 __device__ __forceinline__ uint32_t add_sat(uint32_t a, uint32_t b) { return __builtin_elementwise_add_sat(a, b); }
 
+template <int THREADS>
 struct PlanLds {
-    uint32_t asked[2][kPlanThreads / 64];
-    int32_t sums[kPlanSums][kPlanThreads / 64];
-    float cost[kPlanThreads / 64];
+    uint32_t asked[2][THREADS / 64];
+    int32_t sums[kPlanSums][THREADS / 64];
+    float cost[THREADS / 64];
 };
 
 // Sums over the threads before this one, and over all of them.
-__device__ __forceinline__ void plan_scan(const int32_t *mine, int32_t *before, int32_t *all, PlanLds &lds) {
+template <int THREADS>
+__device__ __forceinline__ void plan_scan(const int32_t *mine, int32_t *before, int32_t *all, PlanLds<THREADS> &lds) {
     const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
     int32_t in[kPlanSums];
 #pragma unroll
@@ -92,32 +97,35 @@ __device__ __forceinline__ void plan_scan(const int32_t *mine, int32_t *before, 
         before[k] = in[k] - mine[k];
         all[k] = 0;
 #pragma unroll
-        for (int w = 0; w < kPlanThreads / 64; ++w) {
+        for (int w = 0; w < THREADS / 64; ++w) {
             if (w < wave) before[k] += lds.sums[k][w];
             all[k] += lds.sums[k][w];
         }
     }
 }
 
-// The requests [r0 + kPlanPer * thread, ..) of one thread.
+// The requests [r0 + plan_per * thread, ..) of one thread.
+template <int THREADS>
 struct PlanPart {
-    int32_t past[kPlanPer], held[kPlanPer], granted[kPlanPer], after[kPlanPer], first[kPlanPer], need[kPlanPer];
-    int32_t tiles[kPlanPer];                // tiles of many rows
-    int32_t sums[kPlanSums][kPlanPer];      // sums over the chunk's earlier requests
+    static constexpr int PER = plan_per<THREADS>;
+    int32_t past[PER], held[PER], granted[PER], after[PER], first[PER], need[PER];
+    int32_t tiles[PER];                // tiles of many rows
+    int32_t sums[kPlanSums][PER];      // sums over the chunk's earlier requests
     int32_t all[kPlanSums];                 // over the chunk
     uint32_t tokens;                        // asked by the chunk and all before it
 };
 
 // Prefix sums over a chunk, behind requests that ask for need0 pages and tok0 tokens.
+template <int THREADS>
 __device__ __forceinline__ void plan_chunk(const PlanArgs &p, int r0, uint32_t need0, uint32_t tok0, int32_t free_pages,
-                                           PlanLds &lds, PlanPart &o) {
-    constexpr int W = kPlanThreads / 64;
+                                           PlanLds<THREADS> &lds, PlanPart<THREADS> &o) {
+    constexpr int W = THREADS / 64, PER = plan_per<THREADS>;
     const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
-    const int i0 = r0 + threadIdx.x * kPlanPer;
-    Ask a[kPlanPer];
+    const int i0 = r0 + threadIdx.x * PER;
+    Ask a[PER];
     uint32_t need = 0, tok = 0;
 #pragma unroll
-    for (int j = 0; j < kPlanPer; ++j) {
+    for (int j = 0; j < PER; ++j) {
         const bool live = i0 + j < p.requests;
         a[j] = ask_of(p, live ? p.lengths[i0 + j] : 0, live ? p.add[i0 + j] : 0);
         need = add_sat(need, a[j].need), tok = add_sat(tok, a[j].tokens);
@@ -141,7 +149,7 @@ __device__ __forceinline__ void plan_chunk(const PlanArgs &p, int r0, uint32_t n
     }
     int32_t mine[kPlanSums] = {};
 #pragma unroll
-    for (int j = 0; j < kPlanPer; ++j) {
+    for (int j = 0; j < PER; ++j) {
         const uint32_t need_to = add_sat(need_at, a[j].need), tok_to = add_sat(tok_at, a[j].tokens);
         const bool ok = a[j].tokens > 0 && (a[j].need == 0 || need_to <= (uint32_t)free_pages) &&
                         tok_to <= (uint32_t)p.max_tokens;
@@ -178,7 +186,7 @@ __device__ __forceinline__ void plan_chunk(const PlanArgs &p, int r0, uint32_t n
 #pragma unroll
     for (int k = 0; k < kPlanSums; ++k)
 #pragma unroll
-        for (int j = 0; j < kPlanPer; ++j) o.sums[k][j] += before[k];
+        for (int j = 0; j < PER; ++j) o.sums[k][j] += before[k];
 }
 
 // Many rows: in which order the workgroups take their tiles, the longest first
@@ -189,12 +197,13 @@ __device__ __forceinline__ void plan_chunk(const PlanArgs &p, int r0, uint32_t n
 constexpr int kPartTiles = 16;
 constexpr int kMaxParts = 64;
 
-__device__ __forceinline__ void plan_order(const PlanArgs &p, const PlanPart &o, PlanLds &lds, int32_t *base, int32_t *parts,
+__device__ __forceinline__ void plan_order(const PlanArgs &p, const PlanPart<kPlanThreads> &o, PlanLds<kPlanThreads> &lds, int32_t *base, int32_t *parts,
                                            int32_t *items) {
+    constexpr int PER = plan_per<kPlanThreads>;
     const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
     float cost = 0.0f;                                                  // key tiles of all tiles
 #pragma unroll
-    for (int j = 0; j < kPlanPer; ++j)
+    for (int j = 0; j < PER; ++j)
         if (o.tiles[j] > 0) cost += (float)o.tiles[j] * (float)((o.after[j] + kUnit - 1) / kUnit);
 #pragma unroll
     for (int s = 1; s < 64; s *= 2) cost += __shfl_xor(cost, s, 64);
@@ -205,9 +214,9 @@ __device__ __forceinline__ void plan_order(const PlanArgs &p, const PlanPart &o,
     for (int w = 0; w < kPlanThreads / 64; ++w) cost += lds.cost[w];
     const float even = ceilf(cost / (float)tile_slots(p.heads));
     const float least = even > (float)kPartTiles ? even : (float)kPartTiles;
-    int32_t mine[kPlanSums] = {}, at[kPlanPer], kind[kPlanPer];
+    int32_t mine[kPlanSums] = {}, at[PER], kind[PER];
 #pragma unroll
-    for (int j = 0; j < kPlanPer; ++j) {
+    for (int j = 0; j < PER; ++j) {
         const int32_t keys = o.granted[j] > 0 ? (o.after[j] + kUnit - 1) / kUnit : 1;
         const float share = ceilf((float)keys / least);
         parts[j] = share > (float)kMaxParts ? kMaxParts : share > 1.0f ? (int32_t)share : 1;
@@ -223,7 +232,7 @@ __device__ __forceinline__ void plan_order(const PlanArgs &p, const PlanPart &o,
 #pragma unroll
     for (int k = 0; k < kPlanSums; ++k) {
 #pragma unroll
-        for (int j = 0; j < kPlanPer; ++j)
+        for (int j = 0; j < PER; ++j)
             if (k == kind[j]) base[j] = *items + before[k] + at[j];
         *items += all[k];
     }
@@ -317,27 +326,28 @@ __device__ __forceinline__ int32_t last_at_most(const int32_t *a, int32_t lo, in
 }
 
 __global__ __launch_bounds__(kPlanThreads) void agft_kv_plan_kernel(PlanArgs p) {
-    __shared__ PlanLds lds;
+    constexpr int PER = plan_per<kPlanThreads>;
+    __shared__ PlanLds<kPlanThreads> lds;
     __shared__ int32_t s_first[kPlanChunk], s_past[kPlanChunk], s_granted[kPlanChunk], s_need[kPlanChunk],
         s_touched[kPlanChunk], s_back[kPlanChunk], s_tiles[kPlanChunk], s_items[kPlanChunk], s_parts[kPlanChunk];
     const int32_t head = p.counters[0], free_pages = p.counters[1];
-    PlanPart o;
+    PlanPart<kPlanThreads> o;
     plan_chunk(p, 0, 0, 0, free_pages, lds, o);
-    const int i0 = threadIdx.x * kPlanPer;
+    const int i0 = threadIdx.x * PER;
 #pragma unroll
-    for (int j = 0; j < kPlanPer; ++j) {
+    for (int j = 0; j < PER; ++j) {
         s_first[i0 + j] = o.first[j], s_past[i0 + j] = o.past[j], s_granted[i0 + j] = o.granted[j];
         s_need[i0 + j] = o.need[j], s_touched[i0 + j] = o.sums[0][j], s_back[i0 + j] = o.sums[3][j];
     }
     if (o.all[2] > 0) {
-        int32_t base[kPlanPer], parts[kPlanPer];
+        int32_t base[PER], parts[PER];
         plan_order(p, o, lds, base, parts, &o.all[2]);
 #pragma unroll
-        for (int j = 0; j < kPlanPer; ++j) s_tiles[i0 + j] = o.tiles[j], s_items[i0 + j] = base[j], s_parts[i0 + j] = parts[j];
+        for (int j = 0; j < PER; ++j) s_tiles[i0 + j] = o.tiles[j], s_items[i0 + j] = base[j], s_parts[i0 + j] = parts[j];
     }
     if (blockIdx.x == 0) {
 #pragma unroll
-        for (int j = 0; j < kPlanPer; ++j) {
+        for (int j = 0; j < PER; ++j) {
             const int i = i0 + j;
             if (i >= p.requests) continue;
             p.starts[i] = o.first[j], p.granted[i] = o.granted[j], p.out_lengths[i] = o.after[j];
@@ -365,14 +375,15 @@ __global__ __launch_bounds__(kPlanThreads) void agft_kv_plan_kernel(PlanArgs p) 
 }
 
 // More than kPlanChunk requests, first launch: a workgroup per chunk.
-__global__ __launch_bounds__(kPlanThreads) void agft_kv_plan_sums_kernel(PlanArgs p) {
-    __shared__ PlanLds lds;
-    __shared__ uint32_t s_before[2][kPlanThreads / 64];
+__global__ __launch_bounds__(kSumsThreads) void agft_kv_plan_sums_kernel(PlanArgs p) {
+    constexpr int PER = plan_per<kSumsThreads>;
+    __shared__ PlanLds<kSumsThreads> lds;
+    __shared__ uint32_t s_before[2][kSumsThreads / 64];
     const int32_t free_pages = p.counters[1];
     const int r0 = blockIdx.x * kPlanChunk, lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
     uint32_t need0 = 0, tok0 = 0;
-#pragma unroll 4
-    for (int i = threadIdx.x; i < r0; i += kPlanThreads) {
+#pragma unroll 8
+    for (int i = threadIdx.x; i < r0; i += kSumsThreads) {
         const Ask a = ask_of(p, p.lengths[i], p.add[i]);
         need0 = add_sat(need0, a.need), tok0 = add_sat(tok0, a.tokens);
     }
@@ -384,12 +395,12 @@ __global__ __launch_bounds__(kPlanThreads) void agft_kv_plan_sums_kernel(PlanArg
     if (lane == 0) s_before[0][wave] = need0, s_before[1][wave] = tok0;
     __syncthreads();
     need0 = tok0 = 0;
-    for (int w = 0; w < kPlanThreads / 64; ++w) need0 = add_sat(need0, s_before[0][w]), tok0 = add_sat(tok0, s_before[1][w]);
-    PlanPart o;
+    for (int w = 0; w < kSumsThreads / 64; ++w) need0 = add_sat(need0, s_before[0][w]), tok0 = add_sat(tok0, s_before[1][w]);
+    PlanPart<kSumsThreads> o;
     plan_chunk(p, r0, need0, tok0, free_pages, lds, o);
 #pragma unroll
-    for (int j = 0; j < kPlanPer; ++j) {
-        const int i = r0 + threadIdx.x * kPlanPer + j;
+    for (int j = 0; j < PER; ++j) {
+        const int i = r0 + threadIdx.x * PER + j;
         if (i >= p.requests) continue;
         p.starts[i] = o.first[j], p.granted[i] = o.granted[j], p.out_lengths[i] = o.after[j], p.need[i] = o.need[j];
         p.touched[i] = o.sums[0][j], p.tiles[i] = o.sums[2][j], p.back[i] = o.sums[3][j];
@@ -406,7 +417,7 @@ __global__ __launch_bounds__(kPlanThreads) void agft_kv_plan_sums_kernel(PlanArg
 __global__ __launch_bounds__(kPlanThreads) void agft_kv_plan_slots_kernel(PlanArgs p) {
     constexpr int kMaxChunks = 65536 / kPlanChunk;
     static_assert(kMaxChunks <= 64, "a wavefront's lanes hold the chunks' totals");
-    __shared__ int32_t s_off[kPlanSums][kMaxChunks], s_all[kPlanSums], s_first[kPlanTokens], s_range[2];
+    __shared__ int32_t s_off[kPlanSums][kMaxChunks], s_all[kPlanSums], s_first[kPlanNear], s_range[2];
     const int32_t head = p.counters[0], free_pages = p.counters[1];
     const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
     const int chunks = (p.requests + kPlanChunk - 1) / kPlanChunk;
@@ -429,12 +440,12 @@ __global__ __launch_bounds__(kPlanThreads) void agft_kv_plan_slots_kernel(PlanAr
         for (int k = 0; k < kPlanSums; ++k) all[k] = s_all[k];
         plan_totals(p, (uint32_t)total, all, head, free_pages);
     }
-    // sums that other kernels read become sums over all requests
-    for (int i = blockIdx.x * kPlanThreads + threadIdx.x; (i & ~63) < p.requests; i += gridDim.x * kPlanThreads) {
-        const bool live = i < p.requests;
-        if (live) {
-            p.works[i].few += s_off[1][i / kPlanChunk];
-        }
+    // 16 requests per wavefront: sums that other kernels read become sums over
+    // all requests, and pages come back
+    for (int r0 = (blockIdx.x * (kPlanThreads / 64) + wave) * 16; r0 < p.requests; r0 += gridDim.x * (kPlanThreads / 64) * 16) {
+        const int i = r0 + lane;
+        const bool live = lane < 16 && i < p.requests;
+        if (live) p.works[i].few += s_off[1][i / kPlanChunk];
         const bool ends = live && p.add[i] < 0;
         const Ask a = ask_of(p, ends ? p.lengths[i] : 0, 0);
         plan_give_back(p, ends, i, a.held, ends ? p.back[i] + s_off[3][i / kPlanChunk] : 0, head, free_pages);
@@ -449,7 +460,7 @@ __global__ __launch_bounds__(kPlanThreads) void agft_kv_plan_slots_kernel(PlanAr
         }
         __syncthreads();
         const int32_t lo = s_range[0], hi = s_range[1] + 1;
-        const bool near = hi - lo <= kPlanTokens;      // (requests without tokens may lie between)
+        const bool near = hi - lo <= kPlanNear;      // (requests without tokens may lie between)
         for (int i = lo + threadIdx.x; near && i < hi; i += kPlanThreads) s_first[i - lo] = p.starts[i];
         __syncthreads();
         for (int64_t t = t0 + threadIdx.x; t < t0 + kPlanTokens && t < p.max_tokens; t += kPlanThreads) {
@@ -811,16 +822,17 @@ int agft_kv_plan(const agft_kv_config *cfg, void *d_tables, size_t tables_bytes,
     p.items = reinterpret_cast<Item *>(base + L.items);
     const hipStream_t hs = static_cast<hipStream_t>(stream);
     const int64_t by_tokens = ((int64_t)max_tokens + kPlanTokens - 1) / kPlanTokens;
-    const dim3 grid((unsigned)(by_tokens < 2048 ? by_tokens : 2048));
+    const auto grid = [&](int64_t most) { return dim3((unsigned)(by_tokens < most ? by_tokens : most)); };
     if (cfg->requests <= kPlanChunk) {
-        hipLaunchKernelGGL(agft_kv_plan_kernel, grid, dim3(kPlanThreads), 0, hs, p);
+        // (every workgroup makes all the sums, so no more of them than run at once)
+        hipLaunchKernelGGL(agft_kv_plan_kernel, grid(512), dim3(kPlanThreads), 0, hs, p);
         return launched();
     }
     const dim3 chunks((unsigned)((cfg->requests + kPlanChunk - 1) / kPlanChunk));
-    hipLaunchKernelGGL(agft_kv_plan_sums_kernel, chunks, dim3(kPlanThreads), 0, hs, p);
+    hipLaunchKernelGGL(agft_kv_plan_sums_kernel, chunks, dim3(kSumsThreads), 0, hs, p);
     st = launched();
     if (st != AGFT_OK) return st;
-    hipLaunchKernelGGL(agft_kv_plan_slots_kernel, grid, dim3(kPlanThreads), 0, hs, p);
+    hipLaunchKernelGGL(agft_kv_plan_slots_kernel, grid(2048), dim3(kPlanThreads), 0, hs, p);
     return launched();
 }
 

@@ -167,49 +167,43 @@ constexpr int kFewShare = 4;         // units below which a stretch is not cut
 constexpr float kLog2e = 1.4426950408889634f;
 constexpr float kLn2 = 0.6931471805599453f;
 
-// The requests' works as a wavefront sees them: up to 64 requests a lane each,
-// read once.
+// The requests' works as a wavefront sees them: those of 64 requests, a lane
+// each, from request `from` on.
 struct Works {
     const Work *w;
-    int n;
-    int4 a;             // few, items, start, granted of request (lane)
+    int n, from;
+    int4 a;             // few, items, start, granted of request from + lane
     int length;
     int4 total;
-    __device__ __forceinline__ Works(const Work *works, int requests) : w(works), n(requests) {
-        const int lane = threadIdx.x & 63;
+    __device__ __forceinline__ Works(const Work *works, int requests) : w(works), n(requests), from(0) {
         total = *reinterpret_cast<const int4 *>(w + n);
-        if (n <= 64) {
-            const int k = lane < n ? lane : n - 1;
-            a = *reinterpret_cast<const int4 *>(w + k);
-            length = w[k].length;
-        }
+        if (n <= 64) read();
     }
-    // the last request whose few is at most x
-    __device__ __forceinline__ int find(int32_t x) const {
+    __device__ __forceinline__ void read() {
+        const int lane = threadIdx.x & 63, k = from + lane < n ? from + lane : n - 1;
+        a = *reinterpret_cast<const int4 *>(w + k);
+        length = w[k].length;
+    }
+    // the requests about unit x, for more requests than lanes
+    __device__ __forceinline__ void look(int32_t x) {
+        if (n <= 64) return;
+        from = find_last([&](int k) { return w[k].few; }, n, x);
+        read();
+    }
+    // whether unit x's request and the next one are among the 64
+    __device__ __forceinline__ bool has(int32_t x) const {
+        return n <= 64 || from + 64 >= n || __builtin_amdgcn_readlane(a.x, 63) > x;
+    }
+    // the request with unit x: its number, entry, length, and the next one's entry
+    __device__ __forceinline__ int get(int32_t x, int4 &own, int &len, int4 &next) const {
         const int lane = threadIdx.x & 63;
-        if (n <= 64) {
-            const int hits = __popcll(__ballot(lane < n && a.x <= x));
-            return __builtin_amdgcn_readfirstlane(hits < 1 ? 0 : hits - 1);
-        }
-        return find_last([&](int k) { return w[k].few; }, n, x);
-    }
-    // a request's own entry, and the next one's few, items, start
-    __device__ __forceinline__ void get(int i, int4 &own, int &len, int4 &next) const {
-        if (n <= 64) {
-            const auto at = [&](int v) { return __builtin_amdgcn_readlane(v, i); };
-            own = make_int4(at(a.x), at(a.y), at(a.z), at(a.w));
-            len = at(length);
-            if (i + 1 < n) {
-                const auto after = [&](int v) { return __builtin_amdgcn_readlane(v, i + 1); };
-                next = make_int4(after(a.x), after(a.y), after(a.z), 0);
-            } else {
-                next = total;
-            }
-            return;
-        }
-        own = *reinterpret_cast<const int4 *>(w + i);
-        len = w[i].length;
-        next = *reinterpret_cast<const int4 *>(w + i + 1);
+        const int hits = __popcll(__ballot(from + lane < n && a.x <= x));
+        const int i = __builtin_amdgcn_readfirstlane(hits < 1 ? 0 : hits - 1);
+        const auto at = [&](int v, int k) { return __builtin_amdgcn_readlane(v, k); };
+        own = make_int4(at(a.x, i), at(a.y, i), at(a.z, i), at(a.w, i));
+        len = at(length, i);
+        next = from + i + 1 < n ? make_int4(at(a.x, i + 1), 0, at(a.z, i + 1), 0) : total;
+        return from + i;
     }
 };
 
@@ -217,11 +211,11 @@ struct Works {
 struct Segment {
     int request, head, row, first, rows, units, at, granted, length;
 };
-__device__ __forceinline__ Segment segment_of(const AttendArgs &p, const Works &works, int32_t x) {
+__device__ __forceinline__ Segment segment_of(const AttendArgs &p, Works &works, int32_t x) {
     Segment s;
-    s.request = works.find(x / p.heads);
     int4 own, next;
-    works.get(s.request, own, s.length, next);
+    if (!works.has(x / p.heads)) works.look(x / p.heads);
+    s.request = works.get(x / p.heads, own, s.length, next);
     const int32_t base = own.x, all = next.x - base;
     s.first = own.z, s.granted = own.w;
     const int rows = (next.z - own.z) * p.group;
@@ -386,7 +380,7 @@ __global__ __launch_bounds__(64 * kFewWaves, few_groups<DIM>() / 256) void agft_
     __shared__ int s_last;
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     const int g = lane >> 4, n = lane & 15;
-    const Works works(p.works, p.requests);
+    Works works(p.works, p.requests);
     const int32_t work = works.total.x * p.heads;
     int32_t share = (work + few_groups<DIM>() - 1) / few_groups<DIM>();
     if (share < kFewShare) share = kFewShare;
@@ -396,6 +390,7 @@ __global__ __launch_bounds__(64 * kFewWaves, few_groups<DIM>() / 256) void agft_
     const int64_t page_bytes = (int64_t)p.heads * 2 * p.page * DIM;
     const float scale2 = p.scale * kLog2e;
     int32_t x = (int32_t)x_first;
+    works.look(x / p.heads);
     while (x < x1) {
         const Segment seg = segment_of(p, works, x);
         if (seg.units <= 0) break;
