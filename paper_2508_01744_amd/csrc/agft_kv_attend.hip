@@ -366,25 +366,32 @@ constexpr int few_groups() {
     return DIM == 64 ? 1024 : DIM == 128 ? 768 : 512;
 }
 
+template <int DIM>
+struct FewLds {
+    static constexpr int ROW = DIM + 4;                   // off the banks
+    // the wavefronts' sums; then a join's weights, largest maxima and sums
+    __attribute__((aligned(16))) float o[kFewWaves][kRowTile * ROW];
+    float m[kFewWaves][kRowTile], l[kFewWaves][kRowTile];
+    int last;
+    static_assert(kFewWaves * ROW >= kManyPieces + 2, "a join's numbers fit where the sums were");
+};
+
 template <int FORM, int TYPE, int DIM>
-__global__ __launch_bounds__(64 * kFewWaves, few_groups<DIM>() / 256) void agft_kv_few_kernel(AttendArgs p) {
+__device__ __forceinline__ void attend_few(const AttendArgs &p, FewLds<DIM> &lds, int block) {
     constexpr int DG = DIM / kBlockDims;
     constexpr int BLK = 2;                        // blocks of 16 tokens at a time
-    constexpr int ROW = DIM + 4;                  // LDS row, off the banks
+    constexpr int ROW = FewLds<DIM>::ROW;
     using H = Half<TYPE>;
     using F = Half<AGFT_KV_FP16>;
-    // the wavefronts' sums; then a join's weights, largest maxima and sums
-    static_assert(kFewWaves * ROW >= kManyPieces + 2, "a join's numbers fit where the sums were");
-    __shared__ __attribute__((aligned(16))) float s_o[kFewWaves][kRowTile * ROW];
-    __shared__ float s_m[kFewWaves][kRowTile], s_l[kFewWaves][kRowTile];
-    __shared__ int s_last;
+    const auto s_o = lds.o;
+    const auto s_m = lds.m, s_l = lds.l;
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     const int g = lane >> 4, n = lane & 15;
     Works works(p.works, p.requests);
     const int32_t work = works.total.x * p.heads;
     int32_t share = (work + few_groups<DIM>() - 1) / few_groups<DIM>();
     if (share < kFewShare) share = kFewShare;
-    const int64_t x_first = (int64_t)blockIdx.x * share;
+    const int64_t x_first = (int64_t)block * share;
     if (x_first >= work) return;
     const int32_t x1 = x_first + share < work ? (int32_t)x_first + share : work;
     const int64_t page_bytes = (int64_t)p.heads * 2 * p.page * DIM;
@@ -549,7 +556,7 @@ __global__ __launch_bounds__(64 * kFewWaves, few_groups<DIM>() / 256) void agft_
         const bool whole = count == units;
         const int32_t from = x - count - u0;                       // the rows' first unit
         const int owner = from / share, pieces = (from + units - 1) / share - owner + 1;
-        float *part = p.partial + ((int64_t)blockIdx.x * 2 + (u0 == 0 ? 1 : 0)) * partial_floats<DIM>();
+        float *part = p.partial + ((int64_t)block * 2 + (u0 == 0 ? 1 : 0)) * partial_floats<DIM>();
         for (int c = threadIdx.x; c < rows * (DIM / 4); c += blockDim.x) {
             const int r = c / (DIM / 4), d = c % (DIM / 4) * 4;
             float mm = s_m[0][r];
@@ -574,7 +581,7 @@ __global__ __launch_bounds__(64 * kFewWaves, few_groups<DIM>() / 256) void agft_
         }
         if (!whole) {
             // groups of kManyPieces first, each into its first piece's place
-            const int mine = blockIdx.x - owner, group0 = mine / kManyPieces * kManyPieces;
+            const int mine = block - owner, group0 = mine / kManyPieces * kManyPieces;
             const int members = pieces - group0 < kManyPieces ? pieces - group0 : kManyPieces;
             const int groups = (pieces + kManyPieces - 1) / kManyPieces;
             // the first piece of the rows is its workgroup's second one
@@ -582,10 +589,10 @@ __global__ __launch_bounds__(64 * kFewWaves, few_groups<DIM>() / 256) void agft_
                 return p.partial + ((int64_t)(owner + w) * 2 + (w == 0 ? 1 : 0)) * partial_floats<DIM>();
             };
             int32_t *counter = p.arrived + kFewGroups + (owner + group0) * 2 + (group0 == 0 ? 1 : 0);
-            if (last_to_arrive(counter, members, &s_last)) {
+            if (last_to_arrive(counter, members, &lds.last)) {
                 float *into = groups == 1 ? nullptr : piece(group0);
                 join_pieces<TYPE, DIM>(p, [&](int w) { return piece(group0 + w); }, members, into, seg, s_o[0]);
-                if (groups > 1 && last_to_arrive(p.arrived + owner, groups, &s_last))
+                if (groups > 1 && last_to_arrive(p.arrived + owner, groups, &lds.last))
                     join_pieces<TYPE, DIM>(p, [&](int w) { return piece(kManyPieces * w); }, groups, nullptr, seg, s_o[0]);
             }
         }
@@ -618,18 +625,25 @@ constexpr int kTileWaves = 4;
 constexpr int kTileKeys = 64;
 constexpr float kSlack = 8.0f;    // powers of two that a maximum may grow before the sums are rescaled
 
+template <int DIM>
+struct TileLds {
+    static constexpr int SIDE = kTileKeys * DIM * 2;       // a tile's keys (or values) in 16 bits
+    // operands of 1 KB, 16 bytes a lane; keys: [32 tokens][64 numbers][32][16], values: [16 tokens][32 numbers]
+    __attribute__((aligned(16))) char tile[2][2][SIDE];
+    float4 scale[4][4];                                    // by tile % 4: a block's factor of the scores, ev, 2^-ev
+    int last;
+};
+
 template <int FORM, int TYPE, int DIM>
-__global__ __launch_bounds__(64 * kTileWaves, DIM > 128 ? 1 : 2) void agft_kv_tile_kernel(AttendArgs p) {
+__device__ __forceinline__ void attend_many(const AttendArgs &p, TileLds<DIM> &lds, int block) {
     constexpr int DG = DIM / kBlockDims;
-    constexpr int SIDE = kTileKeys * DIM * 2;              // a tile's keys (or values) in 16 bits
     using H = Half<TYPE>;
     using F = Half<AGFT_KV_FP16>;
-    // operands of 1 KB, 16 bytes a lane; keys: [32 tokens][64 numbers][32][16], values: [16 tokens][32 numbers]
-    __shared__ __attribute__((aligned(16))) char s_tile[2][2][SIDE];
-    __shared__ float4 s_scale[4][4];                       // by tile % 4: a block's factor of the scores, ev, 2^-ev
+    const auto s_tile = lds.tile;
+    const auto s_scale = lds.scale;
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     const int h = lane >> 5, n = lane & 31;
-    const int head = blockIdx.x % p.heads, place = blockIdx.x / p.heads;
+    const int head = block % p.heads, place = block / p.heads;
     if (place >= p.works[p.requests].items) return;
     const Item item = p.items[place];
     const int i = item.request;
@@ -799,21 +813,46 @@ __global__ __launch_bounds__(64 * kTileWaves, DIM > 128 ? 1 : 2) void agft_kv_ti
 #pragma unroll
             for (int half = 0; half < 2; ++half) s[half] += shift;
         }
+        // Matrix instructions in the order of their operands in LDS, each of which
+        // is read AHEAD instructions before its use; the scores' instructions
+        // alternate between the two halves of the tile, with this tile's
+        // exponentials between them.  (Left to itself the compiler reads every
+        // operand right before its use and waits for it.)
+        constexpr int N = DG * 8, AHEAD = 4;               // instructions of the scores, and of the sums
+        const auto operand = [&](int c) {
+            return *reinterpret_cast<const uint4v *>(
+                c < N ? &s_tile[buf][0][(((c & 1) * (N / 2) + (c >> 1)) * 64 + lane) * 16]
+                      : &s_tile[buf][1][((c - N) * 64 + lane) * 16]);
+        };
+        uint4v ring[AHEAD];
         float16v z[2];
-        scores(buf, z);
 #pragma unroll
-        for (int b = 0; b < 4; ++b) {
-            float e[8];
+        for (int c = 0; c < AHEAD; ++c) ring[c] = operand(c);
 #pragma unroll
-            for (int j = 0; j < 8; ++j) e[j] = __builtin_amdgcn_exp2f(s[b >> 1][8 * (b & 1) + j]);
-            l = fmaf(((e[0] + e[1]) + (e[2] + e[3])) + ((e[4] + e[5]) + (e[6] + e[7])), pow_back[b], l);
-            fp16x8 pr;
+        for (int half = 0; half < 2; ++half)
 #pragma unroll
-            for (int j = 0; j < 8; ++j) pr[j] = (_Float16)e[j];
+            for (int j = 0; j < 16; ++j) z[half][j] = 0.0f;
+        fp16x8 pr[4];
+        float sum = 0.0f;
 #pragma unroll
-            for (int c = 0; c < DG * 2; ++c)
-                o[c] = mfma32<AGFT_KV_FP16>(*reinterpret_cast<const fp16x8 *>(
-                                                &s_tile[buf][1][((b * DG * 2 + c) * 64 + lane) * 16]), pr, o[c]);
+        for (int c = 0; c < N; ++c) {
+            z[c & 1] = mfma32<TYPE>(__builtin_bit_cast(typename H::x8, ring[c % AHEAD]), q[c >> 1], z[c & 1]);
+            ring[c % AHEAD] = operand(c + AHEAD);
+#pragma unroll
+            for (int x = c * 32 / N; x < (c + 1) * 32 / N; ++x) {
+                const float e = __builtin_amdgcn_exp2f(s[x >> 4][x & 15]);
+                sum = (x & 7) == 0 ? e : sum + e;
+                pr[x >> 3][x & 7] = (_Float16)e;
+                if ((x & 7) == 7) l = fmaf(sum, pow_back[x >> 3], l);
+            }
+            __builtin_amdgcn_sched_barrier(0);
+        }
+#pragma unroll
+        for (int c = N; c < 2 * N; ++c) {
+            const int b = (c - N) / (DG * 2), y = (c - N) % (DG * 2);
+            o[y] = mfma32<AGFT_KV_FP16>(__builtin_bit_cast(fp16x8, ring[c % AHEAD]), pr[b], o[y]);
+            if (c + AHEAD < 2 * N) ring[c % AHEAD] = operand(c + AHEAD);
+            __builtin_amdgcn_sched_barrier(0);
         }
         s[0] = z[0], s[1] = z[1];
     };
@@ -857,7 +896,6 @@ __global__ __launch_bounds__(64 * kTileWaves, DIM > 128 ? 1 : 2) void agft_kv_ti
         return;
     }
     // parts meet as the pieces of few rows do
-    __shared__ int s_last;
     constexpr int64_t PART = kTileRows * (DIM + 2);
     float *parts = p.partial + kFewGroups * 2 * partial_floats<DIM>() + ((int64_t)(place - item.part) * p.heads + head) * PART;
     const int64_t stride = p.heads * PART;
@@ -873,7 +911,7 @@ __global__ __launch_bounds__(64 * kTileWaves, DIM > 128 ? 1 : 2) void agft_kv_ti
             }
         if (h == 0) put(at + kTileRows * DIM + r, m), put(at + kTileRows * (DIM + 1) + r, l);
     }
-    if (!last_to_arrive(p.arrived + 3 * kFewGroups + (place - item.part) * p.heads + head, item.parts, &s_last)) return;
+    if (!last_to_arrive(p.arrived + 3 * kFewGroups + (place - item.part) * p.heads + head, item.parts, &lds.last)) return;
     for (int c = threadIdx.x; c < rows * (DIM / 4); c += blockDim.x) {
         const int r = c / (DIM / 4), d = c % (DIM / 4) * 4;
         float top = -INFINITY, sum = 0.0f;
@@ -892,6 +930,27 @@ __global__ __launch_bounds__(64 * kTileWaves, DIM > 128 ? 1 : 2) void agft_kv_ti
         store_row4<TYPE, DIM>(p, first, head, row0 + r, d, all, sum);
         if (d == 0) store_lse(p, first, head, row0 + r, top, sum);
     }
+}
+
+// ---- launches ----
+
+template <int FORM, int TYPE, int DIM>
+__global__ __launch_bounds__(64 * kFewWaves, few_groups<DIM>() / 256) void agft_kv_few_kernel(AttendArgs p) {
+    __shared__ FewLds<DIM> lds;
+    attend_few<FORM, TYPE, DIM>(p, lds, blockIdx.x);
+}
+
+// Requests of few rows and of many in one launch, the few ones' workgroups
+// first: chunks of prompts beside single tokens take PLACE2
+template <int FORM, int TYPE, int DIM>
+__global__ __launch_bounds__(64 * kTileWaves, DIM > 128 ? 1 : 2) void agft_kv_tile_kernel(AttendArgs p) {
+    static_assert(kFewWaves == kTileWaves, "one workgroup size");
+    __shared__ union {
+        FewLds<DIM> few;
+        TileLds<DIM> many;
+    } lds;
+    if (blockIdx.x < few_groups<DIM>()) attend_few<FORM, TYPE, DIM>(p, lds.few, blockIdx.x);
+    else attend_many<FORM, TYPE, DIM>(p, lds.many, blockIdx.x - few_groups<DIM>());
 }
 
 inline int log2_of(int32_t page) { return page == 16 ? 4 : page == 32 ? 5 : page == 64 ? 6 : 7; }
@@ -941,14 +1000,14 @@ int agft_kv_attend(const agft_kv_config *cfg, const void *d_cache, size_t cache_
     p.page = cfg->page, p.shift = log2_of(cfg->page), p.heads = cfg->heads, p.group = cfg->group;
     p.items = reinterpret_cast<const Item *>(static_cast<const char *>(d_step) + step_layout(cfg, max_tokens).items);
     const int64_t tile_groups = item_cap(cfg, max_tokens) * cfg->heads;
-    if (tile_groups > INT32_MAX) return AGFT_E_INVAL;
+    if (tile_groups > INT32_MAX - kFewGroups) return AGFT_E_INVAL;
     const auto go = [&](auto form, auto type, auto dim) {
         const hipStream_t hs = static_cast<hipStream_t>(stream);
-        agft_kv_few_kernel<form(), type(), dim()><<<few_groups<dim()>(), 64 * kFewWaves, 0, hs>>>(p);
-        int code = launched();
-        if (code != AGFT_OK) return code;
-        if (code != AGFT_OK || (int64_t)max_new * cfg->group <= kFewRows) return code;
-        agft_kv_tile_kernel<form(), type(), dim()><<<(unsigned)tile_groups, 64 * kTileWaves, 0, hs>>>(p);
+        if ((int64_t)max_new * cfg->group <= kFewRows)
+            agft_kv_few_kernel<form(), type(), dim()><<<few_groups<dim()>(), 64 * kFewWaves, 0, hs>>>(p);
+        else
+            agft_kv_tile_kernel<form(), type(), dim()>
+                <<<(unsigned)(few_groups<dim()>() + tile_groups), 64 * kTileWaves, 0, hs>>>(p);
         return launched();
     };
     const auto dims = [&](auto form, auto type) {
