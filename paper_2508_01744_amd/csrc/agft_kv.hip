@@ -563,17 +563,35 @@ __global__ void agft_kv_append_kernel(AppendArgs p) {
     constexpr int DG = DIM / kBlockDims;
     __shared__ float s_top[8];
     __shared__ uint32_t s_turn[8][kBlockBytes / 4];
-    if ((int)blockIdx.x >= p.runs[0]) return;
     const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, g = lane >> 4, m = lane & 15;
     const int head = blockIdx.y, side = blockIdx.z;
-    const int32_t t0 = p.runs[1 + blockIdx.x], total = p.counters[2];
-    const int64_t slot0 = p.slots[t0];
+    // A single token's write is a chain of loads, so whatever can be asked for
+    // at once is: the run, the slots about its first token, then numbers,
+    // exponent and older codes together.
+    const int32_t runs = p.runs[0], t0 = p.runs[1 + blockIdx.x], total = p.counters[2];
+    if ((int)blockIdx.x >= runs) return;
+    int64_t near[2];                            // slots of tokens t0 + lane, t0 + 64 + lane
+#pragma unroll
+    for (int z = 0; z < 2; ++z) near[z] = t0 + 64 * z + lane < total ? p.slots[t0 + 64 * z + lane] : -1;
+    const int64_t slot0 = __shfl(near[0], 0, 64);
     if (slot0 < 0 || slot0 >= p.pool_tokens) return;
     const int64_t page_id = slot0 >> p.shift;
     const int off = (int)(slot0 & (p.page - 1));
     // this lane's token
     const int pos = 16 * wave + m, k = pos - off;
-    const bool live = k >= 0 && t0 + k < total && p.slots[t0 + k < total ? t0 + k : t0] == slot0 + k;
+    const int64_t at0 = __shfl(near[0], k & 63, 64), at1 = __shfl(near[1], k & 63, 64);
+    const bool live = k >= 0 && (k < 64 ? at0 : at1) == slot0 + k;
+    const bool older = off > 16 * wave;         // tokens of earlier windows among these 16
+    int32_t *ep = p.exps + (page_id * p.heads + head) * 2 + side;
+    uint4 *block = reinterpret_cast<uint4 *>(p.codes + ((page_id * p.heads + head) * 2 + side) * p.page * DIM) +
+                   (size_t)wave * DG * 64;
+    const int old = off > 0 ? *ep : kMinExp;
+    uint4 held[DG];
+#pragma unroll
+    for (int dg = 0; dg < DG; ++dg) {
+        held[dg] = make_uint4(0, 0, 0, 0);
+        if (older) held[dg] = block[dg * 64 + lane];
+    }
     float x[DG][16];
     float top = 0.0f;
     if (live) {
@@ -597,25 +615,17 @@ __global__ void agft_kv_append_kernel(AppendArgs p) {
 #pragma unroll
     for (int s = 1; s < 64; s *= 2) top = fmaxf(top, __shfl_xor(top, s, 64));
     if (lane == 0) s_top[wave] = top;
+    asm volatile("" ::"v"(old));               // the old exponent has arrived before anyone writes the new one
     __syncthreads();
     top = s_top[0];
     for (int w = 1; w < (int)blockDim.x / 64; ++w) top = fmaxf(top, s_top[w]);
     int e = exponent<FORM>(top);
-    int32_t *ep = p.exps + (page_id * p.heads + head) * 2 + side;
-    int drop = 0;                              // how far the older codes' exponent rises
-    if (off > 0) {
-        const int old = *ep;
-        if (e < old) e = old;
-        drop = e - old;
-    }
-    __syncthreads();                           // every wavefront has read the exponent
+    if (e < old) e = old;
+    const int drop = off > 0 ? e - old : 0;    // how far the older codes' exponent rises
     if (threadIdx.x == 0) *ep = e;
-    const bool older = off > 16 * wave;        // tokens of earlier windows among these 16
     const bool any = __ballot(live) != 0;
     if (!any && !(older && drop > 0)) return;
     const float inv = pow2(-e), fall = drop > 126 ? 0.0f : pow2(-drop);
-    uint4 *block = reinterpret_cast<uint4 *>(p.codes + ((page_id * p.heads + head) * 2 + side) * p.page * DIM) +
-                   (size_t)wave * DG * 64;
 #pragma unroll
     for (int dg = 0; dg < DG; ++dg) {
         uint32_t c[4];
@@ -629,21 +639,18 @@ __global__ void agft_kv_append_kernel(AppendArgs p) {
             }
             c[j] = Code<FORM>::pack4(y[0], y[1], y[2], y[3]);
         }
-        uint4 held = make_uint4(0, 0, 0, 0);
-        if (older) {
-            held = block[dg * 64 + lane];
-            uint32_t h[4] = {held.x, held.y, held.z, held.w};
-            if (drop > 0)
+        if (older && drop > 0) {
+            uint32_t h[4] = {held[dg].x, held[dg].y, held[dg].z, held[dg].w};
 #pragma unroll
-                for (int j = 0; j < 4; ++j) {
-                    float y[4];
-                    Code<FORM>::unpack4(h[j], y);
-                    h[j] = Code<FORM>::pack4(y[0] * fall, y[1] * fall, y[2] * fall, y[3] * fall);
-                }
-            held = make_uint4(h[0], h[1], h[2], h[3]);
+            for (int j = 0; j < 4; ++j) {
+                float y[4];
+                Code<FORM>::unpack4(h[j], y);
+                h[j] = Code<FORM>::pack4(y[0] * fall, y[1] * fall, y[2] * fall, y[3] * fall);
+            }
+            held[dg] = make_uint4(h[0], h[1], h[2], h[3]);
         }
         if (side == 0) {
-            block[dg * 64 + lane] = live ? make_uint4(c[0], c[1], c[2], c[3]) : held;
+            block[dg * 64 + lane] = live ? make_uint4(c[0], c[1], c[2], c[3]) : held[dg];
         } else {
             // values: byte (m % 4) of word g of entry 16 (m / 4) + number
             uint8_t *turn = reinterpret_cast<uint8_t *>(s_turn[wave]);
@@ -661,8 +668,8 @@ __global__ void agft_kv_append_kernel(AppendArgs p) {
             const uint64_t lives = __ballot(live);
 #pragma unroll
             for (int i = 0; i < 4; ++i) mask |= (lives >> (4 * g + i)) & 1 ? 255u << (8 * i) : 0u;
-            block[dg * 64 + lane] = make_uint4((fresh.x & mask) | (held.x & ~mask), (fresh.y & mask) | (held.y & ~mask),
-                                               (fresh.z & mask) | (held.z & ~mask), (fresh.w & mask) | (held.w & ~mask));
+            block[dg * 64 + lane] = make_uint4((fresh.x & mask) | (held[dg].x & ~mask), (fresh.y & mask) | (held[dg].y & ~mask),
+                                               (fresh.z & mask) | (held[dg].z & ~mask), (fresh.w & mask) | (held[dg].w & ~mask));
         }
     }
 }
