@@ -92,14 +92,29 @@ __device__ __forceinline__ void plan_scan(const int32_t *mine, int32_t *before, 
     for (int k = 0; k < kPlanSums; ++k)
         if (lane == 63) lds.sums[k][wave] = in[k];
     __syncthreads();
+    constexpr int W = THREADS / 64;
 #pragma unroll
     for (int k = 0; k < kPlanSums; ++k) {
         before[k] = in[k] - mine[k];
-        all[k] = 0;
+        if constexpr (W <= 4) {
+            all[k] = 0;
 #pragma unroll
-        for (int w = 0; w < THREADS / 64; ++w) {
-            if (w < wave) before[k] += lds.sums[k][w];
-            all[k] += lds.sums[k][w];
+            for (int w = 0; w < W; ++w) {
+                if (w < wave) before[k] += lds.sums[k][w];
+                all[k] += lds.sums[k][w];
+            }
+        } else {
+            // many wavefronts: their sums a lane each (read one by one they cost
+            // spilled registers, or 6 us of waiting)
+            int32_t v = lane < W ? lds.sums[k][lane] : 0;
+#pragma unroll
+            for (int s = 1; s < W; s *= 2) {
+                const int32_t x = __shfl_up(v, s, 64);
+                if (lane >= s) v += x;
+            }
+            const int32_t to_here = __shfl(v, wave > 0 ? wave - 1 : 0, 64);
+            if (wave > 0) before[k] += to_here;
+            all[k] = __shfl(v, W - 1, 64);
         }
     }
 }
@@ -382,10 +397,19 @@ __global__ __launch_bounds__(kSumsThreads) void agft_kv_plan_sums_kernel(PlanArg
     const int32_t free_pages = p.counters[1];
     const int r0 = blockIdx.x * kPlanChunk, lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
     uint32_t need0 = 0, tok0 = 0;
-#pragma unroll 8
-    for (int i = threadIdx.x; i < r0; i += kSumsThreads) {
-        const Ask a = ask_of(p, p.lengths[i], p.add[i]);
-        need0 = add_sat(need0, a.need), tok0 = add_sat(tok0, a.tokens);
+    constexpr int AHEAD = 16;                  // earlier requests of a thread on their way at once
+    for (int i0 = threadIdx.x; i0 < r0; i0 += AHEAD * kSumsThreads) {
+        int32_t past[AHEAD], add[AHEAD];
+#pragma unroll
+        for (int z = 0; z < AHEAD; ++z) {
+            const int i = i0 + z * kSumsThreads;
+            past[z] = i < r0 ? p.lengths[i] : 0, add[z] = i < r0 ? p.add[i] : 0;
+        }
+#pragma unroll
+        for (int z = 0; z < AHEAD; ++z) {
+            const Ask a = ask_of(p, past[z], add[z]);
+            need0 = add_sat(need0, a.need), tok0 = add_sat(tok0, a.tokens);
+        }
     }
 #pragma unroll
     for (int s = 1; s < 64; s *= 2) {
