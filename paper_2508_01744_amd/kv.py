@@ -11,7 +11,9 @@ One window of a node with a KvTables `tables` and, per layer, a KvCache `cache`:
 
 Calls enqueue on the stream given to the object, or else on the stream that is
 current when they are called; nothing here waits for the GPU except load().
+Tensors of another stream are the caller's to order, as for any torch call.
 """
+import contextlib
 import ctypes
 import math
 
@@ -67,10 +69,26 @@ class _OnStream:
         # (the raw handle: a window's calls are short enough for the Stream object's microseconds to count)
         return _current_raw_stream(self.device.index) if self.stream is None else self.stream.cuda_stream
 
+    @contextlib.contextmanager
+    def _settled(self):
+        """Set-up work on the object's stream: after what the caller's stream
+        holds, and done when it ends, so that any stream may go on from there."""
+        torch.cuda.current_stream(self.device).synchronize()
+        with torch.cuda.stream(self.stream) if self.stream is not None else contextlib.nullcontext():
+            yield
+            torch.cuda.current_stream(self.device).synchronize()
+
+    def _empty(self, *shape, dtype):
+        """Memory that belongs to the stream which the work on it is enqueued on."""
+        if self.stream is None:
+            return torch.empty(*shape, dtype=dtype, device=self.device)
+        with torch.cuda.stream(self.stream):
+            return torch.empty(*shape, dtype=dtype, device=self.device)
+
     def _buffer(self, nbytes, what):
         if nbytes == 0:
             raise ValueError(f"invalid {what} configuration")
-        return torch.empty(nbytes, dtype=torch.uint8, device=self.device)
+        return self._empty(nbytes, dtype=torch.uint8)
 
     def _ints(self, t, shape, what):
         if t.device != self.device or t.dtype != torch.int32 or not t.is_contiguous() or tuple(t.shape) != shape:
@@ -93,8 +111,8 @@ class KvStep(_OnStream):
     slots [max_tokens] int64, -1 where nothing is stored
     """
 
-    def __init__(self, cfg, max_tokens, max_new=None, device="cuda"):
-        self._init(cfg, device, None)
+    def __init__(self, cfg, max_tokens, max_new=None, device="cuda", stream=None):
+        self._init(cfg, device, stream)
         self.max_tokens = int(max_tokens)
         if not 1 <= self.max_tokens <= 1 << 30:
             raise ValueError("max_tokens must be in 1..2^30")
@@ -119,10 +137,11 @@ class KvStep(_OnStream):
         if not 1 <= self.max_new <= self.max_tokens:
             raise ValueError("max_new must be in 1..max_tokens")
 
-    def work(self):
-        """The attention's workspace, shared by the layers, which run one after another."""
+    def work(self, owner=None):
+        """The attention's workspace, shared by the layers, which run one after
+        another; made for the stream of `owner` when it is first asked for."""
         if self._work is None:
-            self._work = self._buffer(self._lib.agft_kv_attend_bytes(self._cfg, self.max_tokens), "cache")
+            self._work = (owner or self)._buffer(self._lib.agft_kv_attend_bytes(self._cfg, self.max_tokens), "cache")
         return self._work
 
 
@@ -157,20 +176,18 @@ class KvTables(_OnStream):
         if free.dim() != 1 or free.numel() > cfg.pages:
             raise ValueError("free must list at most the pool's pages")
         self._ints(free, (free.numel(),), "free")
-        for t, top, what in ((lengths, cfg.row_pages * cfg.page + 1, "lengths"), (table, cfg.pages, "table"),
-                             (free, cfg.pages, "free")):
-            if t.numel() and (int(t.min()) < 0 or int(t.max()) >= top):
+        bad = [((t < 0) | (t >= top)).any() for t, top in ((lengths, cfg.row_pages * cfg.page + 1), (table, cfg.pages),
+                                                           (free, cfg.pages))]
+        for wrong, what in zip(torch.stack(bad).tolist(), ("lengths", "table", "free")):
+            if wrong:
                 raise ValueError(f"{what} out of range")
-        stream = self.stream if self.stream is not None else torch.cuda.current_stream(self.device)
-        torch.cuda.current_stream(self.device).synchronize()
-        with torch.cuda.stream(stream):
+        counters = torch.tensor([0, free.numel(), 0, 0, 0, 0, 0, 0], dtype=torch.int32)
+        with self._settled():
             self.lengths.copy_(lengths)
             self.table.copy_(table)
             self.ring.zero_()
             self.ring[:free.numel()].copy_(free)
-            self.counters.zero_()
-            self.counters[1:2].fill_(free.numel())
-        stream.synchronize()
+            self.counters.copy_(counters)
 
     def plan(self, add, max_tokens, max_new=None, step=None):
         """Plan a window: add [R] int32 new tokens per request (0: none, < 0: it
@@ -178,7 +195,7 @@ class KvTables(_OnStream):
         host knows).  step: a KvStep of the same max_tokens to write again."""
         self._ints(add, (self.cfg.requests,), "add")
         if step is None:
-            step = KvStep(self.cfg, max_tokens, max_new, self.device)
+            step = KvStep(self.cfg, max_tokens, max_new, self.device, self.stream)
         elif step.max_tokens != max_tokens:
             raise ValueError(f"step is for {step.max_tokens} tokens, not {max_tokens}")
         else:
@@ -221,9 +238,7 @@ class KvCache(_OnStream):
         if exps.dtype != torch.int32 or tuple(exps.shape) != (c.pages, c.heads, 2):
             raise ValueError("exps must be int32 [pages][heads][2]")
         self._dev(codes), self._dev(exps)
-        stream = self.stream if self.stream is not None else torch.cuda.current_stream(self.device)
-        torch.cuda.current_stream(self.device).synchronize()
-        with torch.cuda.stream(stream):
+        with self._settled():
             self.exps.copy_(exps)
             part = max(1, (1 << 28) // (c.heads * 2 * c.page * c.dim))
             for p in range(0, c.pages, part):
@@ -233,7 +248,6 @@ class KvCache(_OnStream):
                 self.codes[p:q, :, 0] = k.permute(0, 1, 2, 4, 5, 3, 6).reshape(q - p, c.heads, -1)
                 v = codes[p:q, :, 1].reshape(*lead, 4, 4, c.dim // 64, 4, 16)
                 self.codes[p:q, :, 1] = v.permute(0, 1, 2, 5, 3, 7, 6, 4).reshape(q - p, c.heads, -1)
-        stream.synchronize()
 
     def _dev(self, t):
         if t.device != self.device:
@@ -278,7 +292,7 @@ class KvCache(_OnStream):
         c, n = self.cfg, step.max_tokens
         hq = c.heads * c.group
         if out is None:
-            out = torch.empty(n, hq, c.dim, dtype=q.dtype, device=self.device)
+            out = self._empty(n, hq, c.dim, dtype=q.dtype)
         elif out.dtype != q.dtype:
             raise ValueError("q and out must have one type")
         self._dense(self._d0, q, hq, n, "q", HALVES)
@@ -286,7 +300,7 @@ class KvCache(_OnStream):
         if lse is not None and (lse.device != self.device or lse.dtype != torch.float32 or
                                 lse.shape != (n, hq) or not lse.is_contiguous()):
             raise ValueError(f"lse must be a contiguous float32 tensor [{n}][{hq}] on {self.device}")
-        work = step.work()
+        work = step.work(self)
         code = self._lib.agft_kv_attend(self._cfg, self.ptr, self.nbytes, tables.ptr, tables.nbytes, step.ptr,
                                         step.nbytes, n, step.max_new, self._b0, self._b1,
                                         None if lse is None else lse.data_ptr(),
@@ -304,7 +318,7 @@ class KvCache(_OnStream):
         if dtype not in TYPES:
             raise ValueError(f"no exports in {dtype}")
         n, H, D = slots.numel(), self.cfg.heads, self.cfg.dim
-        k, v = torch.empty(2, n, H, D, dtype=dtype, device=self.device)
+        k, v = self._empty(2, n, H, D, dtype=dtype)
         if n:
             for d, t in ((self._d0, k), (self._d1, v)):
                 d.data, d.token_stride, d.head_stride, d.type = t.data_ptr(), H * D, D, TYPES[dtype]
