@@ -163,6 +163,7 @@ __device__ __forceinline__ float across_sum(float x) {
 constexpr int kFewWaves = 4;
 constexpr int kFewPieces = 4;        // pieces that are joined without weights of their own
 constexpr int kManyPieces = 32;      // pieces that are joined at once
+constexpr int kAtOnce = 8;           // of them on their way at once
 constexpr int kFewShare = 4;         // units below which a stretch is not cut
 constexpr float kLog2e = 1.4426950408889634f;
 constexpr float kLn2 = 0.6931471805599453f;
@@ -336,10 +337,16 @@ __device__ __forceinline__ void join_pieces(const AttendArgs &p, F piece, int pi
     for (int c = threadIdx.x; c < rows * (DIM / 4); c += blockDim.x) {
         const int r = c / (DIM / 4), d = c % (DIM / 4) * 4;
         float4v o = {0, 0, 0, 0};
-#pragma unroll 8
-        for (int w = 0; w < pieces; ++w) {
-            const float2 a = get2(piece(w) + r * DIM + d), b = get2(piece(w) + r * DIM + d + 2);
-            o += (float4v){a.x, a.y, b.x, b.y} * weight[r * kManyPieces + w];
+        for (int w0 = 0; w0 < pieces; w0 += kAtOnce) {
+            float2 a[kAtOnce], b[kAtOnce];
+#pragma unroll
+            for (int z = 0; z < kAtOnce; ++z) {
+                const float *at = piece(w0 + z < pieces ? w0 + z : w0) + r * DIM + d;
+                a[z] = get2(at), b[z] = get2(at + 2);
+            }
+#pragma unroll
+            for (int z = 0; z < kAtOnce; ++z)
+                if (w0 + z < pieces) o += (float4v){a[z].x, a[z].y, b[z].x, b[z].y} * weight[r * kManyPieces + w0 + z];
         }
         finish(r, d, o, s_top[r], s_sum[r]);
     }
@@ -348,6 +355,7 @@ __device__ __forceinline__ void join_pieces(const AttendArgs &p, F piece, int pi
 // Counts this workgroup's arrival at a join of `parties`; true in the last one,
 // which also sets the counter back for the next layer's call.
 __device__ __forceinline__ bool last_to_arrive(int32_t *counter, int parties, int *s_last) {
+    __builtin_amdgcn_fence(__ATOMIC_RELEASE, "workgroup"); // (no word is moved past the wait)
     __builtin_amdgcn_s_waitcnt(0x0f70);                    // this wavefront's words are out: vmcnt(0)
     __syncthreads();
     if (threadIdx.x == 0) {
