@@ -164,6 +164,7 @@ constexpr int kFewWaves = 4;
 constexpr int kFewPieces = 4;        // pieces that are joined without weights of their own
 constexpr int kManyPieces = 32;      // pieces that are joined at once
 constexpr int kAtOnce = 8;           // of them on their way at once
+constexpr int kFewEven = 8;          // share up to which rows are cut evenly
 constexpr int kFewShare = 4;         // units below which a stretch is not cut
 constexpr float kLog2e = 1.4426950408889634f;
 constexpr float kLn2 = 0.6931471805599453f;
@@ -207,6 +208,45 @@ struct Works {
         return from + i;
     }
 };
+
+// Little work: a workgroup per piece, each of one request's rows alone, so that
+// nobody goes through two of them one after the other.
+struct Piece {
+    int32_t first, last;    // units of the work
+    int owner, pieces;      // the workgroup with the rows' first piece, and their pieces
+};
+
+// The piece of workgroup `block` (last = first: none) where rows of `units`
+// units are cut into ceil(units / share) even pieces; false if that takes more
+// than `groups` workgroups.  For up to 64 requests, a lane each.
+__device__ __forceinline__ bool piece_of(const AttendArgs &p, const Works &works, int share, int groups, int block, Piece *o) {
+    const int lane = threadIdx.x & 63;
+    const int few_next = __shfl_down(works.a.x, 1, 64), start_next = __shfl_down(works.a.z, 1, 64);
+    const bool end = lane + 1 >= works.n;
+    const int all = lane < works.n ? (end ? works.total.x : few_next) - works.a.x : 0;
+    const int rows = ((end ? works.total.z : start_next) - works.a.z) * p.group;
+    const int tiles = all > 0 ? (rows + kRowTile - 1) / kRowTile : 0;
+    const int units = tiles > 0 ? all / tiles : 0;
+    const int pieces = (units + share - 1) / share, mine = tiles * pieces * p.heads;
+    int to = mine;
+#pragma unroll
+    for (int s = 1; s < 64; s *= 2) {
+        const int x = __shfl_up(to, s, 64);
+        if (lane >= s) to += x;
+    }
+    if (__builtin_amdgcn_readlane(to, 63) > groups) return false;
+    const int i = __popcll(__ballot(to <= block));
+    if (i >= works.n) {
+        o->first = o->last = 0;
+        return true;
+    }
+    const auto at = [&](int v) { return __builtin_amdgcn_readlane(v, i); };
+    const int n = at(pieces), u = at(units), in = block - (at(to) - at(mine)), row = in / n, part = in - row * n;
+    const int32_t from = at(works.a.x) * p.heads + row * u;
+    o->first = from + u * part / n, o->last = from + u * (part + 1) / n;
+    o->owner = block - part, o->pieces = n;
+    return true;
+}
 
 // The rows that unit x of the work belongs to, and its place among their units.
 struct Segment {
@@ -399,9 +439,14 @@ __device__ __forceinline__ void attend_few(const AttendArgs &p, FewLds<DIM> &lds
     const int32_t work = works.total.x * p.heads;
     int32_t share = (work + few_groups<DIM>() - 1) / few_groups<DIM>();
     if (share < kFewShare) share = kFewShare;
-    const int64_t x_first = (int64_t)block * share;
-    if (x_first >= work) return;
-    const int32_t x1 = x_first + share < work ? (int32_t)x_first + share : work;
+    int64_t x_first = (int64_t)block * share;
+    int32_t x1 = x_first + share < work ? (int32_t)x_first + share : work;
+    Piece cut;
+    const bool even = works.n <= 64 && share <= kFewEven &&
+                      (piece_of(p, works, share, few_groups<DIM>(), block, &cut) ||
+                       piece_of(p, works, share + 2, few_groups<DIM>(), block, &cut));
+    if (even) x_first = cut.first, x1 = cut.last;
+    if (x_first >= x1) return;
     const int64_t page_bytes = (int64_t)p.heads * 2 * p.page * DIM;
     const float scale2 = p.scale * kLog2e;
     int32_t x = (int32_t)x_first;
@@ -563,7 +608,8 @@ __device__ __forceinline__ void attend_few(const AttendArgs &p, FewLds<DIM> &lds
         __syncthreads();
         const bool whole = count == units;
         const int32_t from = x - count - u0;                       // the rows' first unit
-        const int owner = from / share, pieces = (from + units - 1) / share - owner + 1;
+        const int owner = even ? cut.owner : from / share;
+        const int pieces = even ? cut.pieces : (from + units - 1) / share - owner + 1;
         float *part = p.partial + ((int64_t)block * 2 + (u0 == 0 ? 1 : 0)) * partial_floats<DIM>();
         for (int c = threadIdx.x; c < rows * (DIM / 4); c += blockDim.x) {
             const int r = c / (DIM / 4), d = c % (DIM / 4) * 4;
