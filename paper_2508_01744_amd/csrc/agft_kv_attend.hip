@@ -192,6 +192,11 @@ struct Works {
         from = find_last([&](int k) { return w[k].few; }, n, x);
         read();
     }
+    __device__ __forceinline__ void look_at(int request) {
+        if (n <= 64) return;
+        from = __builtin_amdgcn_readfirstlane(request);
+        read();
+    }
     // whether unit x's request and the next one are among the 64
     __device__ __forceinline__ bool has(int32_t x) const {
         return n <= 64 || from + 64 >= n || __builtin_amdgcn_readlane(a.x, 63) > x;
@@ -214,7 +219,24 @@ struct Works {
 struct Piece {
     int32_t first, last;    // units of the work
     int owner, pieces;      // the workgroup with the rows' first piece, and their pieces
+    int request;
 };
+
+// A request's rows in tiles of 16, and the units of each, from the entries of
+// the request and the next one.
+__device__ __forceinline__ void tiles_of(const AttendArgs &p, int few, int start, int few_next, int start_next, int &tiles,
+                                         int &units) {
+    const int all = few_next - few, rows = (start_next - start) * p.group;
+    tiles = all > 0 ? (rows + kRowTile - 1) / kRowTile : 0;
+    units = tiles > 0 ? all / tiles : 0;
+}
+
+// Piece `in` of request i's: tiles of `units` units, cut into `pieces` each.
+__device__ __forceinline__ Piece piece_at(const AttendArgs &p, int i, int few, int units, int pieces, int in, int block) {
+    const int row = in / pieces, part = in - row * pieces;
+    const int32_t from = few * p.heads + row * units;
+    return Piece{from + units * part / pieces, from + units * (part + 1) / pieces, block - part, pieces, i};
+}
 
 // The piece of workgroup `block` (last = first: none) where rows of `units`
 // units are cut into ceil(units / share) even pieces; false if that takes more
@@ -223,10 +245,9 @@ __device__ __forceinline__ bool piece_of(const AttendArgs &p, const Works &works
     const int lane = threadIdx.x & 63;
     const int few_next = __shfl_down(works.a.x, 1, 64), start_next = __shfl_down(works.a.z, 1, 64);
     const bool end = lane + 1 >= works.n;
-    const int all = lane < works.n ? (end ? works.total.x : few_next) - works.a.x : 0;
-    const int rows = ((end ? works.total.z : start_next) - works.a.z) * p.group;
-    const int tiles = all > 0 ? (rows + kRowTile - 1) / kRowTile : 0;
-    const int units = tiles > 0 ? all / tiles : 0;
+    int tiles, units;
+    tiles_of(p, works.a.x, works.a.z, end ? works.total.x : few_next, end ? works.total.z : start_next, tiles, units);
+    if (lane >= works.n) tiles = 0;
     const int pieces = (units + share - 1) / share, mine = tiles * pieces * p.heads;
     int to = mine;
 #pragma unroll
@@ -237,15 +258,73 @@ __device__ __forceinline__ bool piece_of(const AttendArgs &p, const Works &works
     if (__builtin_amdgcn_readlane(to, 63) > groups) return false;
     const int i = __popcll(__ballot(to <= block));
     if (i >= works.n) {
-        o->first = o->last = 0;
+        *o = Piece{0, 0, 0, 1, 0};
         return true;
     }
     const auto at = [&](int v) { return __builtin_amdgcn_readlane(v, i); };
-    const int n = at(pieces), u = at(units), in = block - (at(to) - at(mine)), row = in / n, part = in - row * n;
-    const int32_t from = at(works.a.x) * p.heads + row * u;
-    o->first = from + u * part / n, o->last = from + u * (part + 1) / n;
-    o->owner = block - part, o->pieces = n;
+    *o = piece_at(p, i, at(works.a.x), at(units), at(pieces), block - (at(to) - at(mine)), block);
     return true;
+}
+
+// The same for up to kEvenRequests requests, by the whole workgroup.
+constexpr int kEvenPer = 4;
+constexpr int kEvenRequests = 64 * kFewWaves * kEvenPer;
+struct EvenLds {
+    int sums[kFewWaves];
+    Piece piece;
+};
+__device__ __forceinline__ bool piece_of(const AttendArgs &p, const Works &works, int share, int groups, int block, EvenLds &lds,
+                                         Piece *o) {
+    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, i0 = threadIdx.x * kEvenPer;
+    int4 w[kEvenPer + 1];
+#pragma unroll
+    for (int j = 0; j <= kEvenPer; ++j) w[j] = *reinterpret_cast<const int4 *>(works.w + (i0 + j < works.n ? i0 + j : works.n));
+    int tiles[kEvenPer], units[kEvenPer];
+#pragma unroll
+    for (int j = 0; j < kEvenPer; ++j) tiles_of(p, w[j].x, w[j].z, w[j + 1].x, w[j + 1].z, tiles[j], units[j]);
+    for (int attempt = 0; attempt < 2; ++attempt, share += 2) {
+        int mine = 0, at[kEvenPer];
+#pragma unroll
+        for (int j = 0; j < kEvenPer; ++j) {
+            at[j] = mine;
+            mine += tiles[j] * ((units[j] + share - 1) / share) * p.heads;
+        }
+        int to = mine;
+#pragma unroll
+        for (int s = 1; s < 64; s *= 2) {
+            const int x = __shfl_up(to, s, 64);
+            if (lane >= s) to += x;
+        }
+        if (lane == 63) lds.sums[wave] = to;
+        __syncthreads();
+        int before = to - mine, all = 0;
+#pragma unroll
+        for (int z = 0; z < kFewWaves; ++z) {
+            if (z < wave) before += lds.sums[z];
+            all += lds.sums[z];
+        }
+        if (all <= groups) {
+            if (block >= all) {
+                if (threadIdx.x == 0) lds.piece = Piece{0, 0, 0, 1, 0};
+            } else if (before <= block && block < before + mine) {
+                int j = 0;
+#pragma unroll
+                for (int z = 1; z < kEvenPer; ++z)
+                    if (before + at[z] <= block) j = z;
+#pragma unroll
+                for (int z = 0; z < kEvenPer; ++z)
+                    if (z == j)
+                        lds.piece = piece_at(p, i0 + z, w[z].x, units[z], (units[z] + share - 1) / share,
+                                             block - before - at[z], block);
+            }
+        }
+        __syncthreads();
+        if (all <= groups) {
+            *o = lds.piece;
+            return true;
+        }
+    }
+    return false;
 }
 
 // The rows that unit x of the work belongs to, and its place among their units.
@@ -420,6 +499,7 @@ struct FewLds {
     // the wavefronts' sums; then a join's weights, largest maxima and sums
     __attribute__((aligned(16))) float o[kFewWaves][kRowTile * ROW];
     float m[kFewWaves][kRowTile], l[kFewWaves][kRowTile];
+    EvenLds even;
     int last;
     static_assert(kFewWaves * ROW >= kManyPieces + 2, "a join's numbers fit where the sums were");
 };
@@ -442,15 +522,21 @@ __device__ __forceinline__ void attend_few(const AttendArgs &p, FewLds<DIM> &lds
     int64_t x_first = (int64_t)block * share;
     int32_t x1 = x_first + share < work ? (int32_t)x_first + share : work;
     Piece cut;
-    const bool even = works.n <= 64 && share <= kFewEven &&
-                      (piece_of(p, works, share, few_groups<DIM>(), block, &cut) ||
-                       piece_of(p, works, share + 2, few_groups<DIM>(), block, &cut));
+    bool even = false;
+    if (share <= kFewEven) {
+        if (works.n <= 64)
+            even = piece_of(p, works, share, few_groups<DIM>(), block, &cut) ||
+                   piece_of(p, works, share + 2, few_groups<DIM>(), block, &cut);
+        else if (works.n <= kEvenRequests)
+            even = piece_of(p, works, share, few_groups<DIM>(), block, lds.even, &cut);
+    }
     if (even) x_first = cut.first, x1 = cut.last;
     if (x_first >= x1) return;
     const int64_t page_bytes = (int64_t)p.heads * 2 * p.page * DIM;
     const float scale2 = p.scale * kLog2e;
     int32_t x = (int32_t)x_first;
-    works.look(x / p.heads);
+    if (even) works.look_at(cut.request);
+    else works.look(x / p.heads);
     while (x < x1) {
         const Segment seg = segment_of(p, works, x);
         if (seg.units <= 0) break;
