@@ -68,7 +68,7 @@ __device__ __forceinline__ uint32_t add_sat(uint32_t a, uint32_t b) { return __b
 
 template <int THREADS>
 struct PlanLds {
-    uint32_t asked[2][THREADS / 64];
+    uint32_t asked[3][THREADS / 64];
     int32_t sums[kPlanSums][THREADS / 64];
     float cost[THREADS / 64];
 };
@@ -127,10 +127,21 @@ struct PlanPart {
     int32_t tiles[PER];                // tiles of many rows
     int32_t sums[kPlanSums][PER];      // sums over the chunk's earlier requests
     int32_t all[kPlanSums];                 // over the chunk
+    int32_t few_rows;                       // rows up to which a request counts as one of few
     uint32_t tokens;                        // asked by the chunk and all before it
 };
 
-// Prefix sums over a chunk, behind requests that ask for need0 pages and tok0 tokens.
+// Units, for one head, of a request of more than kFewRows and up to kMidRows rows,
+// if it gets what it asks for.
+__device__ __forceinline__ uint32_t mid_units(const PlanArgs &p, const Ask &a) {
+    const int64_t rows = (int64_t)a.tokens * p.group;
+    if (rows <= kFewRows || rows > kMidRows) return 0;
+    return ((uint32_t)(a.past + (int32_t)a.tokens + kUnit - 1) / kUnit) * (((uint32_t)rows + kRowTile - 1) / kRowTile);
+}
+
+// Prefix sums over a chunk, behind requests that ask for need0 pages and tok0
+// tokens.  (Requests of up to kMidRows rows are told apart by their work where
+// one chunk is all there is.)
 template <int THREADS>
 __device__ __forceinline__ void plan_chunk(const PlanArgs &p, int r0, uint32_t need0, uint32_t tok0, int32_t free_pages,
                                            PlanLds<THREADS> &lds, PlanPart<THREADS> &o) {
@@ -138,30 +149,34 @@ __device__ __forceinline__ void plan_chunk(const PlanArgs &p, int r0, uint32_t n
     const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
     const int i0 = r0 + threadIdx.x * PER;
     Ask a[PER];
-    uint32_t need = 0, tok = 0;
+    uint32_t need = 0, tok = 0, mid = 0;
 #pragma unroll
     for (int j = 0; j < PER; ++j) {
         const bool live = i0 + j < p.requests;
         a[j] = ask_of(p, live ? p.lengths[i0 + j] : 0, live ? p.add[i0 + j] : 0);
-        need = add_sat(need, a[j].need), tok = add_sat(tok, a[j].tokens);
+        need = add_sat(need, a[j].need), tok = add_sat(tok, a[j].tokens), mid = add_sat(mid, mid_units(p, a[j]));
     }
     uint32_t need_in = need, tok_in = tok;
 #pragma unroll
     for (int s = 1; s < 64; s *= 2) {
         const uint32_t x = __shfl_up(need_in, s, 64), y = __shfl_up(tok_in, s, 64);
+        mid = add_sat(mid, __shfl_xor(mid, s, 64));
         if (lane >= s) need_in = add_sat(need_in, x), tok_in = add_sat(tok_in, y);
     }
-    if (lane == 63) lds.asked[0][wave] = need_in, lds.asked[1][wave] = tok_in;
+    if (lane == 63) lds.asked[0][wave] = need_in, lds.asked[1][wave] = tok_in, lds.asked[2][wave] = mid;
     uint32_t need_at = __shfl_up(need_in, 1, 64), tok_at = __shfl_up(tok_in, 1, 64);
     if (lane == 0) need_at = 0, tok_at = 0;
     __syncthreads();
     need_at = add_sat(need_at, need0), tok_at = add_sat(tok_at, tok0);
     o.tokens = tok0;
+    mid = 0;
 #pragma unroll
     for (int w = 0; w < W; ++w) {
+        mid = add_sat(mid, lds.asked[2][w]);
         if (w < wave) need_at = add_sat(need_at, lds.asked[0][w]), tok_at = add_sat(tok_at, lds.asked[1][w]);
         o.tokens = add_sat(o.tokens, lds.asked[1][w]);
     }
+    o.few_rows = p.requests <= kPlanChunk && mid <= (uint32_t)(kMidUnits / p.heads) ? kMidRows : kFewRows;
     int32_t mine[kPlanSums] = {};
 #pragma unroll
     for (int j = 0; j < PER; ++j) {
@@ -178,7 +193,7 @@ __device__ __forceinline__ void plan_chunk(const PlanArgs &p, int r0, uint32_t n
         // what the window's kernels have to do for it
         const int32_t rows = last - o.first[j];                         // rows of the window's tensors
         const int64_t wide = (int64_t)rows * p.group;
-        const bool few = wide <= kFewRows;
+        const bool few = wide <= o.few_rows;
         o.tiles[j] = rows == 0 || few ? 0 : (int32_t)((wide + kTileRows - 1) / kTileRows);
         const int32_t v[kPlanSums] = {
             ok ? pages_of(o.after[j], p.page, p.shift) - (a[j].past >> p.shift) : 0,    // pages written to

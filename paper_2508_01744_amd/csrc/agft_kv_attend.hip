@@ -23,6 +23,7 @@ struct AttendArgs {
     int64_t q_token, q_head, out_token, out_head;   // numbers
     float scale;
     int32_t requests, row_pages, pages, page, shift, heads, group;
+    int32_t few_blocks;     // workgroups ahead of the tiles' that take few rows
 };
 
 typedef float float4v __attribute__((ext_vector_type(4)));
@@ -143,7 +144,7 @@ __device__ __forceinline__ float across_sum(float x) {
 // ---- few query rows: shared out over the cached tokens ----
 //
 // The work is the list of units (64 tokens of one request, for one head's 16
-// query rows) of the requests with at most 64 query rows per head, requests
+// query rows) of the requests with few query rows per head, requests
 // outermost, then heads, then rows; every workgroup
 // takes an equal stretch of it, so the split does not depend on how the lengths
 // are spread.  A stretch's part of one request's 16 rows (a segment) is cut among
@@ -1089,8 +1090,8 @@ __global__ __launch_bounds__(64 * kTileWaves, DIM > 128 ? 1 : 2) void agft_kv_ti
         FewLds<DIM> few;
         TileLds<DIM> many;
     } lds;
-    if (blockIdx.x < few_groups<DIM>()) attend_few<FORM, TYPE, DIM>(p, lds.few, blockIdx.x);
-    else attend_many<FORM, TYPE, DIM>(p, lds.many, blockIdx.x - few_groups<DIM>());
+    if ((int)blockIdx.x < p.few_blocks) attend_few<FORM, TYPE, DIM>(p, lds.few, blockIdx.x);
+    else attend_many<FORM, TYPE, DIM>(p, lds.many, blockIdx.x - p.few_blocks);
 }
 
 inline int log2_of(int32_t page) { return page == 16 ? 4 : page == 32 ? 5 : page == 64 ? 6 : 7; }
@@ -1143,11 +1144,14 @@ int agft_kv_attend(const agft_kv_config *cfg, const void *d_cache, size_t cache_
     if (tile_groups > INT32_MAX - kFewGroups) return AGFT_E_INVAL;
     const auto go = [&](auto form, auto type, auto dim) {
         const hipStream_t hs = static_cast<hipStream_t>(stream);
-        if ((int64_t)max_new * cfg->group <= kFewRows)
+        const int64_t rows = (int64_t)max_new * cfg->group;
+        p.few_blocks = rows > kMidRows ? few_groups<dim()>() : 0;
+        if (rows <= kMidRows) {
             agft_kv_few_kernel<form(), type(), dim()><<<few_groups<dim()>(), 64 * kFewWaves, 0, hs>>>(p);
-        else
-            agft_kv_tile_kernel<form(), type(), dim()>
-                <<<(unsigned)(few_groups<dim()>() + tile_groups), 64 * kTileWaves, 0, hs>>>(p);
+            const int code = launched();
+            if (code != AGFT_OK || rows <= kFewRows) return code;
+        }
+        agft_kv_tile_kernel<form(), type(), dim()><<<(unsigned)(p.few_blocks + tile_groups), 64 * kTileWaves, 0, hs>>>(p);
         return launched();
     };
     const auto dims = [&](auto form, auto type) {

@@ -19,7 +19,16 @@ constexpr int kBlockDims = 64;     // numbers of a layout block
 constexpr int kBlockBytes = kBlockTokens * kBlockDims;
 constexpr int kUnit = 64;          // tokens of a unit of attention work
 constexpr int kRowTile = 16;       // query rows (tokens x group) of a tile of the attention over few rows
-constexpr int kFewRows = 64;       // query rows of a request up to which that takes it
+// Query rows of a request up to which that takes it: kFewRows, or kMidRows while
+// the requests of more than kFewRows rows are little work in all.  Reading the
+// tokens again for every 16 rows is soon dearer than tiles of 128 that are part
+// empty, which are dearer for a few tokens (us, by rows / in tiles, 4 heads of
+// 128 numbers: 8 requests x 32 rows x 4,000 tokens, 4,032 units, 27.8 / 30.0;
+// 64 x 32 x 1,000, 8,192 units, 33.5 / 26.2; 200 x 64 x 2,000, 300 / 132; one head
+// of 64, 200 requests of 16 to 64 rows, 3,255 units, 18.9 / 27.9).
+constexpr int kFewRows = 16;
+constexpr int kMidRows = 64;
+constexpr int kMidUnits = 6144;    // units (for all heads) that are little work
 constexpr int kTileRows = 128;     // query rows of a tile of the attention over many rows
 constexpr int kFewGroups = 1024;   // workgroups, at most, that share the work of few rows
 constexpr int kTileSlots = 512;    // workgroups of the attention over many rows that run at once

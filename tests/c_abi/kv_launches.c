@@ -62,28 +62,31 @@ int main(void)
         CHECK(n ? n_ran == 1 && ran_grid[0] == (unsigned)(n + 63) / 64 : n_ran == 0);
     }
 
-    /* attention: one launch; requests of many rows only where a request may have more than 64 */
-    const void *few = NULL, *many = NULL;
-    for (int dim = 64; dim <= 256; dim *= 2)
+    /* attention: requests of at most 16 query rows in one launch, a second one
+       where a request may have up to 64, both kinds in one where it may have more */
+    for (int dim = 64; dim <= 256; dim *= 2) {
+        const void *few = NULL, *many = NULL;
         for (int max_new = 1; max_new <= 20; ++max_new) {
             agft_kv_config t = c;
             t.dim = dim;
             const unsigned groups = dim == 64 ? 1024 : dim == 128 ? 768 : 512;
+            /* 200 x 8 rows: 12 tiles of 128, one more for each of 64 requests, 512 / 4 shared ones; 4 heads */
+            const unsigned tiles = (12 + 64 + 128) * 4;
             start(0);
             CHECK(agft_kv_attend(&t, A, BIG, B, BIG, C, BIG, 200, max_new, &d, &d, NULL, 0.1f, W, BIG, NULL) == AGFT_OK);
-            CHECK(n_ran == 1 && ran_block[0] == 256);
+            CHECK(n_ran == (max_new > 2 && max_new <= 8 ? 2 : 1) && ran_block[0] == 256 && ran_block[n_ran - 1] == 256);
             if (max_new == 1) few = ran[0];
-            if (max_new == 20) many = ran[0];
-            if (max_new * 8 <= 64) {
-                CHECK(ran[0] == few && ran_grid[0] == groups);
-            } else {
-                /* 200 x 8 rows: 12 tiles of 128, up to 24 requests of more than 64, 512 / 4 shared ones; 4 heads */
-                CHECK(ran[0] != few && ran_grid[0] == groups + (12 + 24 + 128) * 4);
-            }
+            if (max_new == 3) many = ran[1];
+            if (max_new <= 8) CHECK(ran[0] == few && ran_grid[0] == groups);
+            if (max_new > 2) CHECK(ran[n_ran - 1] == many && ran_grid[n_ran - 1] == tiles + (max_new > 8 ? groups : 0));
         }
-    CHECK(few != many);
-    start(1);
-    CHECK(agft_kv_attend(&c, A, BIG, B, BIG, C, BIG, 200, 1, &d, &d, NULL, 0.1f, W, BIG, NULL) == AGFT_E_HIP);
+        CHECK(few != many);
+    }
+    for (int fail = 1; fail <= 2; ++fail) {
+        start(fail);
+        CHECK(agft_kv_attend(&c, A, BIG, B, BIG, C, BIG, 200, 5, &d, &d, NULL, 0.1f, W, BIG, NULL) == AGFT_E_HIP);
+        CHECK(n_ran == fail - 1);
+    }
 
     printf("%d failures\n", failures);
     return failures != 0;

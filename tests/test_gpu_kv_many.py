@@ -113,3 +113,20 @@ def test_out_and_queries_with_strides():
     cache.attend(tables, step, q, out=wide[:, :, 64:])
     assert torch.equal(wide[:69, :, 64:], packed[:69])
     assert (wide[:, :, :64] == 3.0).all() and (wide[69:] == 3.0).all()
+
+
+@pytest.mark.parametrize("requests", [20, 45])
+def test_some_rows_over_little_and_much_work(requests):
+    """17 to 64 query rows per request: the split over tokens while that is little
+    work in all (20 requests), tiles of rows beyond (45)."""
+    rng = np.random.default_rng(requests)
+    _, tables, cache, node = make(requests, 26, requests * 26, 128, 1, 8, 64, "e4m3")
+    lengths = [2500 + 7 * i for i in range(requests)]
+    step, want = fill(tables, cache, node, rng, lengths, "bf16")
+    tables.commit(step)
+    node.commit(want)
+    add = [3 + i % 6 for i in range(requests)]
+    units = sum(-(-(n + a) // 64) * -(-8 * a // 16) for n, a in zip(lengths, add))
+    assert (units <= 6144) == (requests == 20)
+    step, want = fill(tables, cache, node, rng, add, "bf16")
+    say("  worst share of the bound", attend_and_compare(tables, cache, node, step, want, rng, "bf16"))
