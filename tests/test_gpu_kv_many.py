@@ -115,10 +115,10 @@ def test_out_and_queries_with_strides():
     assert (wide[:, :, :64] == 3.0).all() and (wide[69:] == 3.0).all()
 
 
-@pytest.mark.parametrize("requests", [20, 45])
+@pytest.mark.parametrize("requests", [20, 60])
 def test_some_rows_over_little_and_much_work(requests):
     """17 to 64 query rows per request: the split over tokens while that is little
-    work in all (20 requests), tiles of rows beyond (45)."""
+    work in all (20 requests), tiles of rows beyond (60)."""
     rng = np.random.default_rng(requests)
     _, tables, cache, node = make(requests, 26, requests * 26, 128, 1, 8, 64, "e4m3")
     lengths = [2500 + 7 * i for i in range(requests)]
