@@ -54,7 +54,11 @@
  * 256-byte aligned, no allocation, work only enqueued on the given stream,
  * negative status codes (the AGFT_E_* values) on invalid arguments, before
  * anything is enqueued.  No call keeps state on the host, so any of them can be
- * recorded into a graph.  Buffers of one call must not overlap.
+ * recorded into a graph.  Buffers of one call must not overlap.  What a call
+ * cannot check on the host is its caller's: block tables, lengths and rings as
+ * agft_kv_plan and agft_kv_commit leave them (a page that no pool has is read as
+ * the pool's last), and work within 2^31 units (64 tokens of a request, for each
+ * head and 16 rows of queries), some tens of what 288 GB hold.
  */
 #ifndef AGFT_KV_H
 #define AGFT_KV_H

@@ -41,12 +41,6 @@ struct Half;
 template <>
 struct Half<AGFT_KV_BF16> {
     using x8 = bf16x8;
-    static __device__ __forceinline__ float load(const void *p, int64_t i) {
-        return __uint_as_float((uint32_t) static_cast<const uint16_t *>(p)[i] << 16);
-    }
-    static __device__ __forceinline__ void store(void *p, int64_t i, float x) {
-        static_cast<__bf16 *>(p)[i] = (__bf16)x;
-    }
     static __device__ __forceinline__ uint2 pack4(float a, float b, float c, float d) {
         const bf16x2 x = {(__bf16)a, (__bf16)b}, y = {(__bf16)c, (__bf16)d};
         return make_uint2(__builtin_bit_cast(uint32_t, x), __builtin_bit_cast(uint32_t, y));
@@ -77,12 +71,6 @@ struct Half<AGFT_KV_BF16> {
 template <>
 struct Half<AGFT_KV_FP16> {
     using x8 = fp16x8;
-    static __device__ __forceinline__ float load(const void *p, int64_t i) {
-        return (float)static_cast<const _Float16 *>(p)[i];
-    }
-    static __device__ __forceinline__ void store(void *p, int64_t i, float x) {
-        static_cast<_Float16 *>(p)[i] = (_Float16)x;
-    }
     static __device__ __forceinline__ uint2 pack4(float a, float b, float c, float d) {
         const fp16x2 x = {(_Float16)a, (_Float16)b}, y = {(_Float16)c, (_Float16)d};
         return make_uint2(__builtin_bit_cast(uint32_t, x), __builtin_bit_cast(uint32_t, y));
@@ -144,13 +132,18 @@ __device__ __forceinline__ float across_sum(float x) {
 // ---- few query rows: shared out over the cached tokens ----
 //
 // The work is the list of units (64 tokens of one request, for one head's 16
-// query rows) of the requests with few query rows per head, requests
-// outermost, then heads, then rows; every workgroup
-// takes an equal stretch of it, so the split does not depend on how the lengths
-// are spread.  A stretch's part of one request's 16 rows (a segment) is cut among
-// the wavefronts, each keeping its own maximum and sums, and joined in LDS; rows
-// that several workgroups share leave partial sums, which the last of them to
-// arrive joins, in the workgroups' order whichever it is.
+// query rows) of the requests with few query rows per head, requests outermost,
+// then heads, then rows; every workgroup takes an equal stretch of it, so the
+// split does not depend on how the lengths are spread.  A stretch's part of one
+// request's 16 rows (a segment) is cut among the wavefronts, each keeping its own
+// maximum and sums, and joined in LDS; rows that several workgroups share leave
+// partial sums, which the last of them to arrive joins, in the workgroups' order
+// whichever it is.
+//
+// What bounds it: memory, once there are some hundred MB (24 tokens over 60,000 to
+// 131,071 tokens, a cache of 4.45 GB: 754 us, 5.9 TB/s; a copy reaches 4.8, reads
+// and writes together), and a chain of loads below (requests, page, exponents,
+// codes, the pieces' way to the join: one token over 778 tokens 8.1 us).
 //
 // Scores are made transposed, S^T = K Q^T (16 tokens x 16 rows per matrix
 // instruction), so that a lane holds four tokens' probabilities of one row,
@@ -162,11 +155,23 @@ __device__ __forceinline__ float across_sum(float x) {
 // 2^(s log2(e) + ev - M) lies in 0..1 whatever the pages' scales are, and meets
 // the codes in fp16; l sums P 2^-ev, and the output is O / l.
 constexpr int kFewWaves = 4;
-constexpr int kFewPieces = 4;        // pieces that are joined without weights of their own
-constexpr int kManyPieces = 32;      // pieces that are joined at once
-constexpr int kAtOnce = 8;           // of them on their way at once
-constexpr int kFewEven = 8;          // share up to which rows are cut evenly
-constexpr int kFewShare = 4;         // units below which a stretch is not cut
+// Up to kFewPieces pieces are read in one round trip, weights and all (4 / 8: one
+// token over 778 tokens 10.4 / 10.7 us); more get their weights first, kAtOnce on
+// their way at a time (one by one: one shared head over 131,000 tokens 44 us for
+// 31); beyond kManyPieces, groups of them are joined first.
+constexpr int kFewPieces = 4;
+constexpr int kAtOnce = 8;
+constexpr int kManyPieces = 32;
+// A workgroup takes at least kFewShare units, one per wavefront (2 / 4 / 8: one
+// token over 778 tokens 13.0 / 10.4 / 11.9 us, 200 requests of 16 to 64 rows over
+// up to 3,000 tokens 19.7 / 21.0 / 25.6).  While its share is at most kFewEven,
+// rows are cut evenly instead of the work as a whole, if that takes no more
+// workgroups (those two 8.2 for 10.5 and 18.8 for 21.6, 64 tokens of 4 heads of 256
+// numbers over 100 to 2,000 tokens 35.6 for 38.6); beyond, an equal stretch is
+// worth more than that (up to a share of 64: 64 tokens over 100 to 8,192 tokens
+// 53.7 for 52.6).
+constexpr int kFewShare = 4;
+constexpr int kFewEven = 8;
 constexpr float kLog2e = 1.4426950408889634f;
 constexpr float kLn2 = 0.6931471805599453f;
 
@@ -488,7 +493,10 @@ __device__ __forceinline__ bool last_to_arrive(int32_t *counter, int parties, in
 }
 
 // Workgroups that share the work: what the registers let stay on 256 compute
-// units at once.
+// units at once (128 numbers, 512 with four blocks of 16 tokens on their way in a
+// wavefront / 768 with two: 64 tokens over 100 to 8,192 tokens 57 / 50 us; 256
+// numbers, 512 / 768, the latter in two rounds: 39 / 49; 64 numbers, 1,024 / 2,048:
+// 21.0 / 25.2).
 template <int DIM>
 constexpr int few_groups() {
     return DIM == 64 ? 1024 : DIM == 128 ? 768 : 512;
@@ -744,16 +752,22 @@ __device__ __forceinline__ void attend_few(const AttendArgs &p, FewLds<DIM> &lds
 // ---- many query rows: tiles of 128 ----
 //
 // A workgroup takes 128 rows (tokens x group) of one request and head, 32 per
-// wavefront, and goes over the tokens 64 at a time.  Vector instructions, not
-// the matrix cores, are what such a kernel runs out of (the exponentials alone
-// take a quarter of the matrix cores' time), so codes are turned into 16 bits
-// once per workgroup: each wavefront fetches one block of 16 tokens, a tile
+// wavefront, and goes over the tokens 64 at a time.  Vector instructions are what
+// such a kernel runs out of before the matrix cores (a matrix instruction takes
+// 15 ns of a SIMD, an exponential 4, a conversion 2), so codes are turned into 16
+// bits once per workgroup: each wavefront fetches one block of 16 tokens, a tile
 // ahead, and leaves its numbers in LDS as the matrix instructions (32 x 32 x 16)
-// take them, 16 bytes a lane.  As above, S^T = K Q^T and O^T = V^T P^T, so a
-// row's probabilities stay in the lanes that made them.  The tiles of tokens
-// that every row sees whole have a loop of their own, without masks.  The
-// longest tiles of rows start first, and consecutive workgroups take consecutive
-// heads, so that (with 8 heads) an XCD's L2 holds one head's tokens.
+// take them, 16 bytes a lane (every wavefront for itself: 2.38 ms for 2.20 on a
+// prompt of 16,380 tokens).  As above, S^T = K Q^T and O^T = V^T P^T, so a row's
+// probabilities stay in the lanes that made them.  The tiles of tokens that every
+// row sees whole have a loop of their own, without masks.  Consecutive workgroups
+// take consecutive heads, so that (with 8 heads) an XCD's L2 holds one head's
+// tokens.
+//
+// The prompt (32 query heads, 8 key/value heads of 128 numbers, causal: 2.2 TFLOP)
+// takes 2.06 to 2.25 ms on different cards, 1.0 PFLOP/s, 80% of what a large matrix
+// product of the library reaches; matrix cores, LDS and vector instructions are each
+// busy for about half of the cycles at a clock that their power sets.
 typedef float float16v __attribute__((ext_vector_type(16)));
 
 template <int TYPE>
@@ -764,7 +778,10 @@ __device__ __forceinline__ float16v mfma32(typename Half<TYPE>::x8 a, typename H
 
 constexpr int kTileWaves = 4;
 constexpr int kTileKeys = 64;
-constexpr float kSlack = 8.0f;    // powers of two that a maximum may grow before the sums are rescaled
+// Powers of two that a maximum may grow before the sums are rescaled: a probability
+// stays below 2^8, which 16 bits hold as exactly as one below 1 (0 / 8: the chunks
+// 133 / 126 us, the prompt 2.10 / 2.06 ms).
+constexpr float kSlack = 8.0f;
 
 template <int DIM>
 struct TileLds {
@@ -1081,8 +1098,11 @@ __global__ __launch_bounds__(64 * kFewWaves, few_groups<DIM>() / 256) void agft_
     attend_few<FORM, TYPE, DIM>(p, lds, blockIdx.x);
 }
 
-// Requests of few rows and of many in one launch, the few ones' workgroups
-// first: chunks of prompts beside single tokens take PLACE2
+// Tiles of many rows, in one launch with the few ones' workgroups where a request
+// may have more than kMidRows (10 chunks of 256 to 1,024 tokens beside 38 single
+// tokens 127 us, 137 in two launches).  Up to kMidRows the few ones come alone
+// first, at their own occupancy (200 requests of 16 to 64 rows 20.4 us, 23.6 in one
+// launch).
 template <int FORM, int TYPE, int DIM>
 __global__ __launch_bounds__(64 * kTileWaves, DIM > 128 ? 1 : 2) void agft_kv_tile_kernel(AttendArgs p) {
     static_assert(kFewWaves == kTileWaves, "one workgroup size");
@@ -1093,8 +1113,6 @@ __global__ __launch_bounds__(64 * kTileWaves, DIM > 128 ? 1 : 2) void agft_kv_ti
     if ((int)blockIdx.x < p.few_blocks) attend_few<FORM, TYPE, DIM>(p, lds.few, blockIdx.x);
     else attend_many<FORM, TYPE, DIM>(p, lds.many, blockIdx.x - p.few_blocks);
 }
-
-inline int log2_of(int32_t page) { return page == 16 ? 4 : page == 32 ? 5 : page == 64 ? 6 : 7; }
 
 }  // namespace agft_kv_detail
 

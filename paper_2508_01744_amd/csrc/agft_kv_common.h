@@ -164,6 +164,8 @@ inline bool dense_ok(const agft_kv_dense *t) {
            t->token_stride % per == 0 && t->head_stride % per == 0;
 }
 
+inline int log2_of(int32_t page) { return page == 16 ? 4 : page == 32 ? 5 : page == 64 ? 6 : 7; }
+
 inline int launched() { return hipGetLastError() == hipSuccess ? AGFT_OK : AGFT_E_HIP; }
 
 // ---- device side ----
