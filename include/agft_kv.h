@@ -58,7 +58,7 @@
  * cannot check on the host is its caller's: block tables, lengths and rings as
  * agft_kv_plan and agft_kv_commit leave them (a page that no pool has is read as
  * the pool's last), and work within 2^31 units (64 tokens of a request, for each
- * head and 16 rows of queries), some tens of what 288 GB hold.
+ * head and 16 rows of queries; 288 GB of cache make 2^26 of single tokens).
  */
 #ifndef AGFT_KV_H
 #define AGFT_KV_H
