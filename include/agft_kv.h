@@ -162,7 +162,9 @@ int agft_kv_append(const agft_kv_config *cfg, void *d_cache, size_t cache_bytes,
  * max_new: no request has more new tokens than this (1..max_tokens); short
  * bounds save launches, a bound that is too low leaves rows unwritten.
  * Products and sums are kept in fp32; probabilities meet the values in fp16,
- * relative to about the largest one's.
+ * relative to about the largest one's with its values' exponent; where the
+ * exponents of a request's pages lie more than 100 apart (values of 1e20 beside
+ * zeros), the smaller ones' share of the sum can be lost.
  * Calls that share a step or a workspace run one after another: partial sums
  * meet there.  The step's other parts stay as they are.
  */
