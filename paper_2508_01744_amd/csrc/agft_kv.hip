@@ -22,6 +22,7 @@ struct PlanArgs {
     Item *items;
     int64_t *slots;
     int32_t requests, row_pages, pages, page, shift, group, heads, max_tokens;
+    int32_t tile_units, tile_slots;    // of a head: compute units, workgroups that run at once
 };
 
 __device__ __forceinline__ int32_t pages_of(int32_t n, int32_t page, int32_t shift) { return (n + page - 1) >> shift; }
@@ -223,12 +224,16 @@ __device__ __forceinline__ void plan_chunk(const PlanArgs &p, int r0, uint32_t n
 
 // Many rows: in which order the workgroups take their tiles, the longest first
 // (by a factor of two), and which tiles several workgroups share, so that few
-// tiles over many tokens fill the chip.  A tile's parts cover at least
-// kPartTiles key tiles and at least an even share of all (8 / 16 / 32: 128 rows of
-// each of 8 requests over 4,000 tokens 52 / 46 / 64 us, of 64 over 1,000 tokens
-// 67 / 32 / 32).  (For up to kPlanChunk requests; beyond, tiles go by request, in
-// one part.)
-constexpr int kPartTiles = 16;
+// tiles over many tokens fill the chip.  Parts cover at least kPartTiles key
+// tiles where that gives every compute unit a workgroup (4 / 8 / 16: chunks of up
+// to 134 tokens of 14 requests over up to 3,341, 4 heads of 256 numbers, 58 / 52 /
+// 61 us; 128 rows of 8 requests over 4,000 tokens, 128 numbers, 33 / 33 / 35), and
+// at least kSecondTiles where it would give it a second one (8 / 16 / 24: 2,774
+// tokens of 7 query heads on one head of 64 36 / 28 / 32 us; 128 rows of 64
+// requests over 1,000 tokens, 256 tiles, 40 / 33 / 33).  (For up to kPlanChunk
+// requests; beyond, tiles go by request, in one part.)
+constexpr int kPartTiles = 8;
+constexpr int kSecondTiles = 16;
 constexpr int kMaxParts = 64;
 
 __device__ __forceinline__ void plan_order(const PlanArgs &p, const PlanPart<kPlanThreads> &o,
@@ -247,8 +252,8 @@ __device__ __forceinline__ void plan_order(const PlanArgs &p, const PlanPart<kPl
     cost = 0.0f;
 #pragma unroll
     for (int w = 0; w < kPlanThreads / 64; ++w) cost += lds.cost[w];
-    const float even = ceilf(cost / (float)tile_slots(p.heads));
-    const float least = even > (float)kPartTiles ? even : (float)kPartTiles;
+    const float once = ceilf(cost / (float)p.tile_units), even = ceilf(cost / (float)p.tile_slots);
+    const float least = fmaxf((float)kPartTiles, fminf(once, fmaxf((float)kSecondTiles, even)));
     int32_t mine[kPlanSums] = {}, at[PER], kind[PER];
 #pragma unroll
     for (int j = 0; j < PER; ++j) {
@@ -872,6 +877,9 @@ int agft_kv_plan(const agft_kv_config *cfg, void *d_tables, size_t tables_bytes,
     p.back = part(L.back), p.sums = part(L.sums), p.arrived = part(L.arrived), p.runs = part(L.runs), p.slots = sv.slots;
     p.requests = cfg->requests, p.row_pages = cfg->row_pages, p.pages = cfg->pages, p.page = cfg->page;
     p.shift = log2_of(cfg->page), p.group = cfg->group, p.heads = cfg->heads, p.max_tokens = max_tokens;
+    // (a compute unit has the registers for two such workgroups, of heads of 256 numbers for one)
+    p.tile_units = per_head(kTileUnits, cfg->heads);
+    p.tile_slots = cfg->dim > 128 ? p.tile_units : per_head(kTileSlots, cfg->heads);
     p.items = reinterpret_cast<Item *>(base + L.items);
     const hipStream_t hs = static_cast<hipStream_t>(stream);
     const int64_t by_tokens = ((int64_t)max_tokens + kPlanTokens - 1) / kPlanTokens;

@@ -22,16 +22,18 @@ constexpr int kRowTile = 16;       // query rows (tokens x group) of a tile of t
 // Query rows of a request up to which that takes it: kFewRows, or kMidRows while
 // the requests of more than kFewRows rows are little work in all.  Reading the
 // tokens again for every 16 rows is soon dearer than tiles of 128 that are part
-// empty, which are dearer for a few tokens (us, by rows / in tiles, 4 heads of
-// 128 numbers: 8 requests x 32 rows x 4,000 tokens, 4,032 units, 27.8 / 30.0;
-// 64 x 32 x 1,000, 8,192 units, 33.5 / 26.2; 200 x 64 x 2,000, 300 / 132; one head
-// of 64, 200 requests of 16 to 64 rows, 3,255 units, 18.9 / 27.9).
+// empty, which are dearer for a few tokens (us, by rows / in tiles: one head of 64
+// numbers, 200 requests of 16 to 64 rows, 2,230 units, 20.5 / 29.0; 2 heads of 256,
+// 9 requests of up to 20 rows over up to 3,726 tokens 22.5 / 46.2; 4 heads of 128,
+// 8 requests x 32 rows x 4,000 tokens, 4,032 units, 29.8 / 23.6; 64 x 32 x 1,000,
+// 8,192 units, 33.5 / 26.2; 200 x 64 x 2,000, 300 / 132).
 constexpr int kFewRows = 16;
 constexpr int kMidRows = 64;
-constexpr int kMidUnits = 6144;    // units (for all heads) that are little work
+constexpr int kMidUnits = 3584;    // units (for all heads) that are little work
 constexpr int kTileRows = 128;     // query rows of a tile of the attention over many rows
 constexpr int kFewGroups = 1024;   // workgroups, at most, that share the work of few rows
-constexpr int kTileSlots = 512;    // workgroups of the attention over many rows that run at once
+constexpr int kTileUnits = 256;    // compute units
+constexpr int kTileSlots = 2 * kTileUnits;  // workgroups, at most, of the attention over many rows that run at once
 constexpr int kTileParts = 2 * kTileSlots;  // of them, at most, that share rows with others
 constexpr int kArrivals = 3 * kFewGroups + kTileParts;   // counters of a window's joins
 constexpr int kPlanChunk = 1024;   // requests whose prefix sums one workgroup makes
@@ -96,12 +98,12 @@ inline int64_t tile_cap(const agft_kv_config *c, int64_t max_tokens) {
 }
 
 // Items run per head; a share of the chip's slots is a head's.
-__host__ __device__ inline int32_t tile_slots(int32_t heads) { return heads < kTileSlots ? kTileSlots / heads : 1; }
+inline int32_t per_head(int32_t slots, int32_t heads) { return heads < slots ? slots / heads : 1; }
 
 // (parts come to at most one per tile and one per slot)
 inline int64_t item_cap(const agft_kv_config *c, int64_t max_tokens) {
     const int64_t tiles = tile_cap(c, max_tokens);
-    return tiles == 0 ? 0 : tiles + tile_slots(c->heads);
+    return tiles == 0 ? 0 : tiles + per_head(kTileSlots, c->heads);
 }
 
 struct StepLayout {
