@@ -152,8 +152,17 @@ __device__ __forceinline__ float across_sum(float x) {
 // layout stores them.  Nothing moves between lanes but the maximum.
 //
 // With M the running maximum of s log2(e) + ev (ev the values' exponent), P =
-// 2^(s log2(e) + ev - M) lies in 0..1 whatever the pages' scales are, and meets
-// the codes in fp16; l sums P 2^-ev, and the output is O / l.
+// 2^(s log2(e) + ev - M) lies in 0..1 whatever the pages' scales are; l sums P
+// 2^-ev, and the output is O / l.  P meets the codes as 2^kRaise P in fp16.
+//
+// That rounding is what lets the second product run on matrix instructions: each
+// P keeps eleven bits (within 2^-11 of itself), what an fp16 output does.  Below 2^-14 fp16 keeps
+// fewer bits and below 2^-25 nothing, hence kRaise, which brings the largest near
+// the end of its range (65,504): what lies 2^-29 below the largest has its eleven
+// bits, and what is lost lies 2^-40 below (2^-25 without it: 131,000 tokens of
+// 2^-25.1 each beside one large one lost their 0.4% of the output).  l sums the P
+// that were not rounded: pages' exponents may lie so far apart that one's P vanish
+// beside another's larger values, and its tokens' weights must stay in l.
 constexpr int kFewWaves = 4;
 // Up to kFewPieces pieces are read in one round trip, weights and all (4 / 8: one
 // token over 778 tokens 10.4 / 10.7 us); more get their weights first, kAtOnce on
@@ -172,6 +181,7 @@ constexpr int kManyPieces = 32;
 // 53.7 for 52.6).
 constexpr int kFewShare = 4;
 constexpr int kFewEven = 8;
+constexpr int kRaise = 15;
 constexpr float kLog2e = 1.4426950408889634f;
 constexpr float kLn2 = 0.6931471805599453f;
 
@@ -365,10 +375,11 @@ constexpr int partial_floats() {
     return kRowTile * (DIM + 2);
 }
 
-template <int TYPE, int DIM>
+// o: the sums times 2^RAISE
+template <int TYPE, int DIM, int RAISE>
 __device__ __forceinline__ void store_row4(const AttendArgs &p, int first, int head, int r, int d, float4v o, float l) {
     const int t = first + r / p.group, hq = head * p.group + r % p.group;
-    const float f = l > 0.0f || l != l ? 1.0f / l : 0.0f;
+    const float f = l > 0.0f || l != l ? pow2(-RAISE) / l : 0.0f;
     uint2 *dst = reinterpret_cast<uint2 *>(p.out + (t * p.out_token + hq * p.out_head + d) * 2);
     *dst = Half<TYPE>::pack4(o[0] * f, o[1] * f, o[2] * f, o[3] * f);
 }
@@ -407,7 +418,7 @@ __device__ __forceinline__ void join_pieces(const AttendArgs &p, F piece, int pi
     const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, rows = seg.rows;
     const auto finish = [&](int r, int d, float4v o, float m, float l) {
         if (into == nullptr) {
-            store_row4<TYPE, DIM>(p, seg.first, seg.head, seg.row + r, d, o, l);
+            store_row4<TYPE, DIM, kRaise>(p, seg.first, seg.head, seg.row + r, d, o, l);
             if (d == 0) store_lse(p, seg.first, seg.head, seg.row + r, m, l);
         } else {
             put2(into + r * DIM + d, o[0], o[1]);
@@ -558,7 +569,7 @@ __device__ __forceinline__ void attend_few(const AttendArgs &p, FewLds<DIM> &lds
             // no slots, no keys
             for (int c = threadIdx.x; c < rows * DIM / 4; c += blockDim.x) {
                 const int r = c / (DIM / 4), d = c % (DIM / 4) * 4;
-                store_row4<TYPE, DIM>(p, first, head, row0 + r, d, (float4v){0, 0, 0, 0}, 0.0f);
+                store_row4<TYPE, DIM, 0>(p, first, head, row0 + r, d, (float4v){0, 0, 0, 0}, 0.0f);
                 if (d == 0) store_lse(p, first, head, row0 + r, -INFINITY, 0.0f);
             }
             continue;
@@ -681,7 +692,7 @@ __device__ __forceinline__ void attend_few(const AttendArgs &p, FewLds<DIM> &lds
                     for (int j = 0; j < 4; ++j) e[j] = __builtin_amdgcn_exp2f(t[s][j] - off);
                     l = fmaf((e[0] + e[1]) + (e[2] + e[3]), back[s], l);
 #pragma unroll
-                    for (int j = 0; j < 4; ++j) pr[s][j] = (_Float16)e[j];
+                    for (int j = 0; j < 4; ++j) pr[s][j] = (_Float16)(e[j] * pow2(kRaise));
                 }
 #pragma unroll
                 for (int s = 0; s < BLK; s += 2) {
@@ -720,7 +731,7 @@ __device__ __forceinline__ void attend_few(const AttendArgs &p, FewLds<DIM> &lds
                 ll = fmaf(s_l[w][r], f, ll);
             }
             if (whole) {
-                store_row4<TYPE, DIM>(p, first, head, row0 + r, d, oo, ll);
+                store_row4<TYPE, DIM, kRaise>(p, first, head, row0 + r, d, oo, ll);
                 if (d == 0) store_lse(p, first, head, row0 + r, mm, ll);
             } else {
                 put2(part + r * DIM + d, oo[0], oo[1]);
@@ -778,10 +789,12 @@ __device__ __forceinline__ float16v mfma32(typename Half<TYPE>::x8 a, typename H
 
 constexpr int kTileWaves = 4;
 constexpr int kTileKeys = 64;
-// Powers of two that a maximum may grow before the sums are rescaled: a probability
-// stays below 2^8, which 16 bits hold as exactly as one below 1 (0 / 8: the chunks
-// 133 / 126 us, the prompt 2.10 / 2.06 ms).
-constexpr float kSlack = 8.0f;
+// Powers of two that a maximum may grow before the sums are rescaled (0 / 8: the
+// chunks 133 / 126 us, the prompt 2.10 / 2.06 ms; 4 / 8: no difference).
+// Probabilities meet the codes as 2^kTileRaise P, so that they stay within fp16's
+// range where the maximum has grown; what is lost lies 2^-36 below the largest.
+constexpr int kSlack = 4;
+constexpr int kTileRaise = kRaise - kSlack;
 
 template <int DIM>
 struct TileLds {
@@ -815,7 +828,7 @@ __device__ __forceinline__ void attend_many(const AttendArgs &p, TileLds<DIM> &l
         if (item.part > 0) return;
         for (int c = threadIdx.x; c < rows * DIM / 4; c += blockDim.x) {
             const int r = c / (DIM / 4), d = c % (DIM / 4) * 4;
-            store_row4<TYPE, DIM>(p, first, head, row0 + r, d, (float4v){0, 0, 0, 0}, 0.0f);
+            store_row4<TYPE, DIM, 0>(p, first, head, row0 + r, d, (float4v){0, 0, 0, 0}, 0.0f);
             if (d == 0) store_lse(p, first, head, row0 + r, -INFINITY, 0.0f);
         }
         return;
@@ -959,7 +972,7 @@ __device__ __forceinline__ void attend_many(const AttendArgs &p, TileLds<DIM> &l
             for (int j = 0; j < 16; ++j) top = fmaxf(top, s[half][j]);
         top = halves_max(top);
         // the maximum that the sums are relative to follows the real one at some distance
-        if (__builtin_expect(__any(top > kSlack || m == -INFINITY), 0)) {
+        if (__builtin_expect(__any(top > (float)kSlack || m == -INFINITY), 0)) {
             const float m1 = fmaxf(m, off + top);
             float fall = m == -INFINITY ? 0.0f : exp2f(m - m1), shift = m1 == -INFINITY ? 0.0f : off - m1;
             m = m1;
@@ -1000,7 +1013,7 @@ __device__ __forceinline__ void attend_many(const AttendArgs &p, TileLds<DIM> &l
             for (int x = c * 32 / N; x < (c + 1) * 32 / N; ++x) {
                 const float e = __builtin_amdgcn_exp2f(s[x >> 4][x & 15]);
                 sum = (x & 7) == 0 ? e : sum + e;
-                pr[x >> 3][x & 7] = (_Float16)e;
+                pr[x >> 3][x & 7] = (_Float16)(e * pow2(kTileRaise));
                 if ((x & 7) == 7) l = fmaf(sum, pow_back[x >> 3], l);
             }
             __builtin_amdgcn_sched_barrier(0);
@@ -1097,7 +1110,7 @@ __device__ __forceinline__ void attend_many(const AttendArgs &p, TileLds<DIM> &l
     for (int c = 0; c < DG * 2; ++c)
 #pragma unroll
         for (int z = 0; z < 4; ++z)
-            store_row4<TYPE, DIM>(p, first, head, row, number(c, z),
+            store_row4<TYPE, DIM, kTileRaise>(p, first, head, row, number(c, z),
                                   (float4v){o[c][4 * z], o[c][4 * z + 1], o[c][4 * z + 2], o[c][4 * z + 3]}, l);
     if (h == 0) store_lse(p, first, head, row, m, l);
 }
