@@ -54,12 +54,22 @@ def _device(device):
 
 
 class _OnStream:
-    """What the front ends share: a configuration, a device, a stream."""
+    """What the front ends share: a configuration, a device, a stream.  Tables,
+    steps and caches that meet in a call have to have one configuration (a layer's
+    dim and form are its own)."""
 
     def _init(self, cfg, device, stream):
-        self.cfg, self.device, self.stream = cfg, _device(device), stream
-        self._cfg = ctypes.byref(cfg)
+        # (a copy: sizes and layouts follow from it)
+        self.cfg, self.device, self.stream = type(cfg).from_buffer_copy(cfg), _device(device), stream
+        self._cfg = ctypes.byref(self.cfg)
         self._lib = L.lib()
+        # where the parts of tables and steps lie; layers may differ in dim and form
+        self._shape = (cfg.requests, cfg.row_pages, cfg.pages, cfg.page, cfg.heads, cfg.group)
+
+    def _same(self, other, what):
+        if other._shape != self._shape:
+            raise ValueError(f"{what} of another configuration: (requests, row_pages, pages, page, heads, group) "
+                             f"{other._shape}, not {self._shape}")
 
     def set_stream(self, stream):
         """Enqueue on `stream` from now on (None: on the stream current at each call)."""
@@ -196,9 +206,10 @@ class KvTables(_OnStream):
         self._ints(add, (self.cfg.requests,), "add")
         if step is None:
             step = KvStep(self.cfg, max_tokens, max_new, self.device, self.stream)
-        elif step.max_tokens != max_tokens:
-            raise ValueError(f"step is for {step.max_tokens} tokens, not {max_tokens}")
         else:
+            self._same(step, "step")
+            if step.max_tokens != max_tokens:
+                raise ValueError(f"step is for {step.max_tokens} tokens, not {max_tokens}")
             step.set_max_new(max_new)
         code = self._lib.agft_kv_plan(self._cfg, self.ptr, self.nbytes, add.data_ptr(), step.ptr, step.nbytes,
                                       step.max_tokens, self._s())
@@ -208,6 +219,7 @@ class KvTables(_OnStream):
 
     def commit(self, step):
         """The planned window's lengths and free pages become the tables'."""
+        self._same(step, "step")
         L.check("agft_kv_commit", self._lib.agft_kv_commit(self._cfg, self.ptr, self.nbytes, step.ptr, step.nbytes,
                                                            step.max_tokens, self._s()))
 
@@ -274,6 +286,7 @@ class KvCache(_OnStream):
         """Store the window's keys and values, [max_tokens][heads][dim] each
         (bf16, fp16 or fp32), rows as in step.starts."""
         H, n = self.cfg.heads, step.max_tokens
+        self._same(step, "step")
         if k.dtype != v.dtype:
             raise ValueError("k and v must have one type")
         self._dense(self._d0, k, H, n, "k")
@@ -291,6 +304,8 @@ class KvCache(_OnStream):
         scale: 1 / sqrt(dim) if None."""
         c, n = self.cfg, step.max_tokens
         hq = c.heads * c.group
+        self._same(step, "step")
+        self._same(tables, "tables")
         if out is None:
             out = self._empty(n, hq, c.dim, dtype=q.dtype)
         elif out.dtype != q.dtype:

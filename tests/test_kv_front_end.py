@@ -1,0 +1,78 @@
+"""What the cache's front end refuses before anything is enqueued (CPU: calls
+that would launch are noted by kv_stub.py instead)."""
+import pytest
+import torch
+
+import kv_stub
+from paper_2508_01744_amd import KvCache, KvStep, KvTables, kv_config
+
+
+@pytest.fixture
+def lib(monkeypatch):
+    return kv_stub.install(monkeypatch)
+
+
+BASE = dict(requests=64, row_tokens=512, pages=200, page=16, heads=8, group=4, dim=64, form="e4m3")
+
+
+def tensors(cfg, n=32, dtype=torch.bfloat16):
+    k = torch.zeros(n, cfg.heads, cfg.dim, dtype=dtype)
+    return k, torch.zeros(n, cfg.heads * cfg.group, cfg.dim, dtype=dtype)
+
+
+def refused(lib, call, match):
+    before = list(lib.calls)
+    with pytest.raises(ValueError, match=match):
+        call()
+    assert lib.calls == before
+
+
+@pytest.mark.parametrize("other", [dict(heads=16), dict(heads=4), dict(group=8), dict(group=2), dict(page=32),
+                                   dict(requests=65), dict(requests=63), dict(pages=201), dict(row_tokens=528),
+                                   dict(row_tokens=256)])
+def test_objects_of_other_configurations(lib, other):
+    """A step's and the tables' parts lie where their configuration puts them."""
+    cfg, cfg2 = kv_config(**BASE), kv_config(**{**BASE, **other})
+    tables, tables2, cache, cache2 = KvTables(cfg), KvTables(cfg2), KvCache(cfg), KvCache(cfg2)
+    add, add2 = (torch.ones(c.requests, dtype=torch.int32) for c in (cfg, cfg2))
+    step = tables.plan(add, 32)
+    tables2.plan(add2, 32)
+    k2, q2 = tensors(cfg2)
+    k, q = tensors(cfg)
+    refused(lib, lambda: cache2.append(step, k2, k2), "configuration")
+    refused(lib, lambda: cache2.attend(tables2, step, q2), "configuration")
+    refused(lib, lambda: cache2.attend(tables, step, q2), "configuration")
+    refused(lib, lambda: cache.attend(tables2, step, q), "configuration")
+    refused(lib, lambda: tables2.plan(add2, 32, step=step), "configuration")
+    refused(lib, lambda: tables2.commit(step), "configuration")
+    del lib.calls[:]
+    cache.append(step, k, k)
+    cache.attend(tables, step, q)
+    tables.commit(step)
+    assert lib.calls == ["append", "attend", "commit"]
+
+
+def test_layers_may_differ_in_what_the_tables_do_not_hold(lib):
+    """One set of tables and one step for layers of other forms and smaller heads."""
+    cfg = kv_config(**{**BASE, "dim": 256})
+    tables = KvTables(cfg)
+    step = tables.plan(torch.ones(64, dtype=torch.int32), 32)
+    for kw in (dict(dim=256, form="int8"), dict(dim=128), dict(dim=64, form="int8")):
+        other = kv_config(**{**BASE, **kw})
+        k, q = tensors(other)
+        cache = KvCache(other)
+        cache.append(step, k, k)
+        cache.attend(tables, step, q)
+
+
+def test_a_configuration_that_is_changed_later(lib):
+    """Objects keep the configuration that they were made with."""
+    cfg = kv_config(**BASE)
+    tables, cache = KvTables(cfg), KvCache(cfg)
+    cfg.heads, cfg.requests = 16, 9
+    assert tables.cfg.heads == cache.cfg.heads == 8
+    step = tables.plan(torch.ones(64, dtype=torch.int32), 32)
+    assert isinstance(step, KvStep) and step.cfg.requests == 64
+    k, q = tensors(cache.cfg)
+    cache.append(step, k, k)
+    cache.attend(tables, step, q)
