@@ -10,7 +10,7 @@ LAUNCHING = ("reset", "plan", "commit", "append", "attend", "export")
 
 class Lib:
     def __init__(self, real):
-        self.real, self.calls = real, []
+        self.real, self.calls, self.args = real, [], []
 
     def __getattr__(self, name):
         if not name.startswith("agft_kv_"):
@@ -20,6 +20,7 @@ class Lib:
 
         def note(*args):
             self.calls.append(name[8:])
+            self.args.append(args)
             return L.AGFT_OK
         return note
 

@@ -76,3 +76,18 @@ def test_a_configuration_that_is_changed_later(lib):
     k, q = tensors(cache.cfg)
     cache.append(step, k, k)
     cache.attend(tables, step, q)
+
+
+def test_the_workspace_fits_the_largest_layer(lib):
+    """Layers of growing heads on one step: each gets a workspace as large as it needs."""
+    cfg = kv_config(**BASE)
+    tables = KvTables(cfg)
+    step = tables.plan(torch.ones(64, dtype=torch.int32), 32)
+    seen = []
+    for dim in (64, 256, 128, 256):
+        cache = KvCache(kv_config(**{**BASE, "dim": dim}))
+        cache.attend(tables, step, tensors(cache.cfg)[1])
+        work, nbytes = lib.args[-1][-3:-1]
+        assert nbytes >= lib.real.agft_kv_attend_bytes(cache._cfg, 32)
+        seen.append(work)
+    assert seen[1] == seen[2] == seen[3]
