@@ -57,8 +57,8 @@
  * recorded into a graph.  Buffers of one call must not overlap.  What a call
  * cannot check on the host is its caller's: block tables, lengths and rings as
  * agft_kv_plan and agft_kv_commit leave them (a page that no pool has is read as
- * the pool's last), steps and tables under the configuration that they were
- * written with (layers may differ in dim and form; with other requests, row_pages,
+ * the pool's last), steps that agft_kv_plan has written, and steps and tables
+ * under the configuration that they were written with (layers may differ in dim and form; with other requests, row_pages,
  * pages, page, heads or group their parts are looked for in the wrong places, out
  * of the buffers too), and work within 2^31 units (64 tokens of a request, for each
  * head and 16 rows of queries; 288 GB of cache make 2^26 of single tokens).

@@ -71,6 +71,11 @@ class _OnStream:
             raise ValueError(f"{what} of another configuration: (requests, row_pages, pages, page, heads, group) "
                              f"{other._shape}, not {self._shape}")
 
+    def _planned(self, step):
+        self._same(step, "step")
+        if not step.planned:
+            raise ValueError("the step has not been planned: its memory holds nothing yet")
+
     def set_stream(self, stream):
         """Enqueue on `stream` from now on (None: on the stream current at each call)."""
         self.stream = stream
@@ -112,7 +117,7 @@ def _view(buf, ptr, dtype, shape):
 
 
 class KvStep(_OnStream):
-    """A planned window, on the GPU:
+    """A window that KvTables.plan writes, on the GPU (`planned` once it has):
 
     counters [8]  after the window: ring's head, free pages; the window's
                   tokens, requests refused, pages taken, pages given back
@@ -140,6 +145,7 @@ class KvStep(_OnStream):
         self.starts = _view(self.buffer, v.starts, torch.int32, (R + 1,))
         self.slots = _view(self.buffer, v.slots, torch.int64, (self.max_tokens,))
         self._work, self._work_dim = None, 0
+        self.planned = False
 
     def set_max_new(self, max_new):
         """No request brings more new tokens than this (None: max_tokens)."""
@@ -218,11 +224,12 @@ class KvTables(_OnStream):
                                       step.max_tokens, self._s())
         if code != L.AGFT_OK:
             L.check("agft_kv_plan", code)
+        step.planned = True
         return step
 
     def commit(self, step):
         """The planned window's lengths and free pages become the tables'."""
-        self._same(step, "step")
+        self._planned(step)
         L.check("agft_kv_commit", self._lib.agft_kv_commit(self._cfg, self.ptr, self.nbytes, step.ptr, step.nbytes,
                                                            step.max_tokens, self._s()))
 
@@ -289,7 +296,7 @@ class KvCache(_OnStream):
         """Store the window's keys and values, [max_tokens][heads][dim] each
         (bf16, fp16 or fp32), rows as in step.starts."""
         H, n = self.cfg.heads, step.max_tokens
-        self._same(step, "step")
+        self._planned(step)
         if k.dtype != v.dtype:
             raise ValueError("k and v must have one type")
         self._dense(self._d0, k, H, n, "k")
@@ -307,7 +314,7 @@ class KvCache(_OnStream):
         scale: 1 / sqrt(dim) if None."""
         c, n = self.cfg, step.max_tokens
         hq = c.heads * c.group
-        self._same(step, "step")
+        self._planned(step)
         self._same(tables, "tables")
         if out is None:
             out = self._empty(n, hq, c.dim, dtype=q.dtype)

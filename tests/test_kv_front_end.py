@@ -91,3 +91,21 @@ def test_the_workspace_fits_the_largest_layer(lib):
         assert nbytes >= lib.real.agft_kv_attend_bytes(cache._cfg, 32)
         seen.append(work)
     assert seen[1] == seen[2] == seen[3]
+
+
+def test_a_step_that_was_never_planned(lib):
+    """Its memory holds anything, and the kernels take indices from it."""
+    cfg = kv_config(**BASE)
+    tables, cache = KvTables(cfg), KvCache(cfg)
+    k, q = tensors(cfg)
+    step = KvStep(cfg, 32)
+    refused(lib, lambda: cache.append(step, k, k), "planned")
+    refused(lib, lambda: cache.attend(tables, step, q), "planned")
+    refused(lib, lambda: tables.commit(step), "planned")
+    with pytest.raises(ValueError):
+        tables.plan(torch.ones(63, dtype=torch.int32), 32, step=step)
+    refused(lib, lambda: cache.append(step, k, k), "planned")
+    tables.plan(torch.ones(64, dtype=torch.int32), 32, step=step)
+    cache.append(step, k, k)
+    cache.attend(tables, step, q)
+    tables.commit(step)
