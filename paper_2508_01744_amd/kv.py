@@ -11,6 +11,7 @@ One window of a node with a KvTables `tables` and, per layer, a KvCache `cache`:
 
 Calls enqueue on the stream given to the object, or else on the stream that is
 current when they are called; nothing here waits for the GPU except load().
+Launches go to the calling thread's current device, which has to be the object's.
 Tensors of another stream are the caller's to order, as for any torch call.
 """
 import contextlib
@@ -45,6 +46,11 @@ except AttributeError:
     def _current_raw_stream(index):
         return torch.cuda.current_stream(index).cuda_stream
 
+try:
+    _current_device = torch._C._cuda_getDevice
+except AttributeError:
+    _current_device = torch.cuda.current_device
+
 
 def _device(device):
     device = torch.device(device)
@@ -60,13 +66,16 @@ class _OnStream:
 
     def _init(self, cfg, device, stream):
         # (a copy: sizes and layouts follow from it)
-        self.cfg, self.device, self.stream = type(cfg).from_buffer_copy(cfg), _device(device), stream
+        self.cfg, self.device = type(cfg).from_buffer_copy(cfg), _device(device)
+        self.set_stream(stream)
         self._cfg = ctypes.byref(self.cfg)
         self._lib = L.lib()
         # where the parts of tables and steps lie; layers may differ in dim and form
         self._shape = (cfg.requests, cfg.row_pages, cfg.pages, cfg.page, cfg.heads, cfg.group)
 
     def _same(self, other, what):
+        if other.device != self.device:
+            raise ValueError(f"{what} on {other.device}, not {self.device}")
         if other._shape != self._shape:
             raise ValueError(f"{what} of another configuration: (requests, row_pages, pages, page, heads, group) "
                              f"{other._shape}, not {self._shape}")
@@ -78,9 +87,14 @@ class _OnStream:
 
     def set_stream(self, stream):
         """Enqueue on `stream` from now on (None: on the stream current at each call)."""
+        if stream is not None and stream.device != self.device:
+            raise ValueError(f"a stream of {stream.device} for work on {self.device}")
         self.stream = stream
 
     def _s(self):
+        if _current_device() != self.device.index:
+            raise ValueError(f"work on {self.device} while the current device is {_current_device()}: launches go to "
+                             "the current device")
         # (the raw handle: a window's calls are short enough for the Stream object's microseconds to count)
         return _current_raw_stream(self.device.index) if self.stream is None else self.stream.cuda_stream
 

@@ -51,4 +51,5 @@ def install(monkeypatch):
     monkeypatch.setattr(kv, "_device", lambda device: Device())
     monkeypatch.setattr(kv._OnStream, "_empty", empty)
     monkeypatch.setattr(kv, "_current_raw_stream", lambda index: 0)
+    monkeypatch.setattr(kv, "_current_device", lambda: Device.index, raising=False)
     return lib

@@ -1,10 +1,12 @@
 """What the cache's front end refuses before anything is enqueued (CPU: calls
 that would launch are noted by kv_stub.py instead)."""
+from types import SimpleNamespace
+
 import pytest
 import torch
 
 import kv_stub
-from paper_2508_01744_amd import KvCache, KvStep, KvTables, kv_config
+from paper_2508_01744_amd import KvCache, KvStep, KvTables, kv, kv_config
 
 
 @pytest.fixture
@@ -109,3 +111,33 @@ def test_a_step_that_was_never_planned(lib):
     cache.append(step, k, k)
     cache.attend(tables, step, q)
     tables.commit(step)
+
+
+def test_launches_go_to_the_objects_device(lib, monkeypatch):
+    """A launch takes the calling thread's current device: with another one current
+    the kernels would run there, on memory of this one."""
+    cfg = kv_config(**BASE)
+    tables, cache = KvTables(cfg), KvCache(cfg)
+    add = torch.ones(64, dtype=torch.int32)
+    step = tables.plan(add, 32)
+    k, q = tensors(cfg)
+    slots = torch.zeros(5, dtype=torch.int64)
+    monkeypatch.setattr(kv, "_current_device", lambda: 3)
+    for call in (lambda: tables.plan(add, 32, step=step), lambda: cache.append(step, k, k),
+                 lambda: cache.attend(tables, step, q), lambda: tables.commit(step), lambda: cache.export(slots),
+                 tables.reset, lambda: KvTables(cfg)):
+        refused(lib, call, "current device")
+
+
+def test_objects_and_streams_of_other_devices(lib):
+    cfg = kv_config(**BASE)
+    tables, cache = KvTables(cfg), KvCache(cfg)
+    step = tables.plan(torch.ones(64, dtype=torch.int32), 32)
+    k, q = tensors(cfg)
+    stream = SimpleNamespace(device=torch.device("cuda", 3), cuda_stream=0)
+    refused(lib, lambda: cache.set_stream(stream), "cuda:3")
+    refused(lib, lambda: KvCache(cfg, stream=stream), "cuda:3")
+    tables.device = torch.device("cuda", 3)
+    refused(lib, lambda: cache.attend(tables, step, q), "cuda:3")
+    step.device = torch.device("cuda", 3)
+    refused(lib, lambda: cache.append(step, k, k), "cuda:3")
