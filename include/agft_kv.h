@@ -163,7 +163,8 @@ int agft_kv_append(const agft_kv_config *cfg, void *d_cache, size_t cache_bytes,
  * of the sums, or NULL.  Tokens that were not granted: out 0, log sum
  * -infinity.  Rows past the window's tokens are left alone.
  * max_new: no request has more new tokens than this (1..max_tokens); short
- * bounds save launches, a bound that is too low leaves rows unwritten.
+ * bounds save launches.  Where a request has more, the rows that only a saved
+ * launch would have made are NaN, in out and d_lse.
  * Products and sums are kept in fp32, the sum of the probabilities too;
  * probabilities meet the values in fp16: with 2^ev_j the scale of token j's
  * values, p_j 2^ev_j keeps eleven bits (within 2^-11 of itself) down to 2^-25 of

@@ -24,6 +24,7 @@ struct AttendArgs {
     float scale;
     int32_t requests, row_pages, pages, page, shift, heads, group;
     int32_t few_blocks;     // workgroups ahead of the tiles' that take few rows
+    bool alone;             // no launch for tiles of many rows
 };
 
 typedef float float4v __attribute__((ext_vector_type(4)));
@@ -524,7 +525,27 @@ struct FewLds {
     static_assert(kFewWaves * ROW >= kManyPieces + 2, "a join's numbers fit where the sums were");
 };
 
-template <int FORM, int TYPE, int DIM>
+// Rows of tiles that no launch makes, because a request brings more tokens than
+// the caller's bound: NaN, not what the memory held.
+template <int TYPE, int DIM>
+__device__ __forceinline__ void leave_nan(const AttendArgs &p, int items) {
+    const int64_t all = (int64_t)items * p.heads;
+    for (int64_t x = blockIdx.x; x < all; x += gridDim.x) {
+        const Item item = p.items[x / p.heads];
+        if (item.part > 0) continue;
+        const int head = (int)(x % p.heads), first = p.works[item.request].start, row0 = item.tile * kTileRows;
+        int rows = (p.works[item.request + 1].start - first) * p.group - row0;
+        if (rows > kTileRows) rows = kTileRows;
+        for (int c = threadIdx.x; c < rows * (DIM / 4); c += blockDim.x) {
+            const int r = c / (DIM / 4), d = c % (DIM / 4) * 4;
+            store_row4<TYPE, DIM, 0>(p, first, head, row0 + r, d, (float4v){0, 0, 0, 0}, NAN);
+            if (d == 0) store_lse(p, first, head, row0 + r, 0.0f, NAN);
+        }
+    }
+}
+
+// BESIDE: in a launch that makes the tiles of many rows too
+template <int FORM, int TYPE, int DIM, bool BESIDE>
 __device__ __forceinline__ void attend_few(const AttendArgs &p, FewLds<DIM> &lds, int block) {
     constexpr int DG = DIM / kBlockDims;
     constexpr int BLK = 2;                        // blocks of 16 tokens at a time
@@ -536,6 +557,8 @@ __device__ __forceinline__ void attend_few(const AttendArgs &p, FewLds<DIM> &lds
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     const int g = lane >> 4, n = lane & 15;
     Works works(p.works, p.requests);
+    if constexpr (!BESIDE)
+        if (__builtin_expect(p.alone && works.total.y > 0, 0)) leave_nan<TYPE, DIM>(p, works.total.y);
     const int32_t work = works.total.x * p.heads;
     int32_t share = (work + few_groups<DIM>() - 1) / few_groups<DIM>();
     if (share < kFewShare) share = kFewShare;
@@ -1120,7 +1143,7 @@ __device__ __forceinline__ void attend_many(const AttendArgs &p, TileLds<DIM> &l
 template <int FORM, int TYPE, int DIM>
 __global__ __launch_bounds__(64 * kFewWaves, few_groups<DIM>() / 256) void agft_kv_few_kernel(AttendArgs p) {
     __shared__ FewLds<DIM> lds;
-    attend_few<FORM, TYPE, DIM>(p, lds, blockIdx.x);
+    attend_few<FORM, TYPE, DIM, false>(p, lds, blockIdx.x);
 }
 
 // Tiles of many rows, in one launch with the few ones' workgroups where a request
@@ -1135,7 +1158,7 @@ __global__ __launch_bounds__(64 * kTileWaves, DIM > 128 ? 1 : 2) void agft_kv_ti
         FewLds<DIM> few;
         TileLds<DIM> many;
     } lds;
-    if ((int)blockIdx.x < p.few_blocks) attend_few<FORM, TYPE, DIM>(p, lds.few, blockIdx.x);
+    if ((int)blockIdx.x < p.few_blocks) attend_few<FORM, TYPE, DIM, true>(p, lds.few, blockIdx.x);
     else attend_many<FORM, TYPE, DIM>(p, lds.many, blockIdx.x - p.few_blocks);
 }
 
@@ -1189,6 +1212,7 @@ int agft_kv_attend(const agft_kv_config *cfg, const void *d_cache, size_t cache_
         const hipStream_t hs = static_cast<hipStream_t>(stream);
         const int64_t rows = (int64_t)max_new * cfg->group;
         p.few_blocks = rows > kMidRows ? few_groups<dim()>() : 0;
+        p.alone = rows <= kFewRows;
         if (rows <= kMidRows) {
             agft_kv_few_kernel<form(), type(), dim()><<<few_groups<dim()>(), 64 * kFewWaves, 0, hs>>>(p);
             const int code = launched();

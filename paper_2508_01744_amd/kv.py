@@ -162,7 +162,8 @@ class KvStep(_OnStream):
         self.planned = False
 
     def set_max_new(self, max_new):
-        """No request brings more new tokens than this (None: max_tokens)."""
+        """No request brings more new tokens than this (None: max_tokens); rows
+        of requests that do may come back from attend as NaN."""
         self.max_new = self.max_tokens if max_new is None else int(max_new)
         if not 1 <= self.max_new <= self.max_tokens:
             raise ValueError("max_new must be in 1..max_tokens")
