@@ -167,8 +167,8 @@ int agft_kv_append(const agft_kv_config *cfg, void *d_cache, size_t cache_bytes,
  * launch would have made are NaN, in out and d_lse.
  * Products and sums are kept in fp32, the sum of the probabilities too;
  * probabilities meet the values in fp16: with 2^ev_j the scale of token j's
- * values, p_j 2^ev_j keeps eleven bits (within 2^-11 of itself) down to 2^-25 of
- * the row's largest, fewer below, and is lost 2^-36 below it.  Where the exponents
+ * values, p_j 2^ev_j keeps eleven bits (within 2^-11 of itself) down to 2^-21 of
+ * the row's largest, fewer below, and is lost 2^-32 below it.  Where the exponents
  * of a request's pages lie more than 100 apart (values of 1e20 beside zeros), the
  * smaller ones' share of the sum can be lost.
  * Calls that share a step or a workspace run one after another: partial sums

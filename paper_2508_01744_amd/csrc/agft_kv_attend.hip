@@ -813,10 +813,14 @@ __device__ __forceinline__ float16v mfma32(typename Half<TYPE>::x8 a, typename H
 constexpr int kTileWaves = 4;
 constexpr int kTileKeys = 64;
 // Powers of two that a maximum may grow before the sums are rescaled (0 / 8: the
-// chunks 133 / 126 us, the prompt 2.10 / 2.06 ms; 4 / 8: no difference).
-// Probabilities meet the codes as 2^kTileRaise P, so that they stay within fp16's
-// range where the maximum has grown; what is lost lies 2^-36 below the largest.
-constexpr int kSlack = 4;
+// chunks 133 / 126 us, the prompt 2.10 / 2.06 ms).  Here the exponential itself
+// makes 2^kTileRaise P, below the end of fp16's range where the maximum has grown (a
+// multiplication for each P, as the few rows have it: the chunks 123 for 120 us, the
+// prompt 2.15 for 2.08 ms); what is lost lies 2^-32 below the largest.  M is the
+// maximum to within 2^-21, so that M - kTileRaise is exact: an exponent s log2(e) +
+// ev - M + kTileRaise is then rounded once, by 2^-22 near the largest, which is a
+// power of two in fp16 as before.
+constexpr int kSlack = 8;
 constexpr int kTileRaise = kRaise - kSlack;
 
 template <int DIM>
@@ -971,7 +975,7 @@ __device__ __forceinline__ void attend_many(const AttendArgs &p, TileLds<DIM> &l
     const auto step = [&](int t, auto mask) {
         constexpr bool MASK = mask();
         const int buf = t & 1;
-        const float off = m == -INFINITY ? 0.0f : m;
+        const float off = m == -INFINITY ? 0.0f : m - (float)kTileRaise;
         float pow_back[4];
 #pragma unroll
         for (int b = 0; b < 4; ++b) {
@@ -995,9 +999,9 @@ __device__ __forceinline__ void attend_many(const AttendArgs &p, TileLds<DIM> &l
             for (int j = 0; j < 16; ++j) top = fmaxf(top, s[half][j]);
         top = halves_max(top);
         // the maximum that the sums are relative to follows the real one at some distance
-        if (__builtin_expect(__any(top > (float)kSlack || m == -INFINITY), 0)) {
-            const float m1 = fmaxf(m, off + top);
-            float fall = m == -INFINITY ? 0.0f : exp2f(m - m1), shift = m1 == -INFINITY ? 0.0f : off - m1;
+        if (__builtin_expect(__any(top > (float)kRaise || m == -INFINITY), 0)) {
+            const float m1 = (fmaxf(m, off + top) - (float)kTileRaise) + (float)kTileRaise;
+            float fall = m == -INFINITY ? 0.0f : exp2f(m - m1), shift = m1 == -INFINITY ? 0.0f : off - (m1 - (float)kTileRaise);
             m = m1;
             // (keeps the compiler from multiplying ahead of the branch, which is rarely taken)
             asm volatile("" : "+v"(fall), "+v"(shift));
@@ -1036,7 +1040,7 @@ __device__ __forceinline__ void attend_many(const AttendArgs &p, TileLds<DIM> &l
             for (int x = c * 32 / N; x < (c + 1) * 32 / N; ++x) {
                 const float e = __builtin_amdgcn_exp2f(s[x >> 4][x & 15]);
                 sum = (x & 7) == 0 ? e : sum + e;
-                pr[x >> 3][x & 7] = (_Float16)(e * pow2(kTileRaise));
+                pr[x >> 3][x & 7] = (_Float16)e;
                 if ((x & 7) == 7) l = fmaf(sum, pow_back[x >> 3], l);
             }
             __builtin_amdgcn_sched_barrier(0);
@@ -1133,9 +1137,9 @@ __device__ __forceinline__ void attend_many(const AttendArgs &p, TileLds<DIM> &l
     for (int c = 0; c < DG * 2; ++c)
 #pragma unroll
         for (int z = 0; z < 4; ++z)
-            store_row4<TYPE, DIM, kTileRaise>(p, first, head, row, number(c, z),
+            store_row4<TYPE, DIM, 0>(p, first, head, row, number(c, z),
                                   (float4v){o[c][4 * z], o[c][4 * z + 1], o[c][4 * z + 2], o[c][4 * z + 3]}, l);
-    if (h == 0) store_lse(p, first, head, row, m, l);
+    if (h == 0) store_lse(p, first, head, row, m, l * pow2(-kTileRaise));
 }
 
 // ---- launches ----

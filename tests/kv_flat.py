@@ -13,7 +13,7 @@ a power of two), w_j the weights of the softmax and A = sum w_j |v_j|, an output
                                     scaling, twice (over the quotient); smax is
                                     the largest sum |q_d k_d| scale
     2 (N / 16 + 32) 2^-24 A         sums of N keys, 16 at a time, and joins, in fp32
-    N 2^-36 max(w_j 2^ev_j) cmax    what fp16 loses of a probability 2^-36 below
+    N 2^-32 max(w_j 2^ev_j) cmax    what fp16 loses of a probability 2^-32 below
                                     the largest, cmax the largest |code|
 
 and the logarithm of the sum by e, the sums' part, and 2^-22 of its size."""
@@ -118,7 +118,7 @@ class Window:
                 ev = e[:, 1].repeat_interleave(self.page)[:N]
                 off = (D + 4) * 2.0 ** -24 * smax + 2.0 ** -23 * (1.45 * smax + ev.abs().max() + 64)
                 sums = 2 * (N / 16 + 32) * 2.0 ** -24
-                gone = N * 2.0 ** -36 * (w * torch.exp2(ev)).amax(1) * code[:, 1].abs().max()
+                gone = N * 2.0 ** -32 * (w * torch.exp2(ev)).amax(1) * code[:, 1].abs().max()
                 tol = u * (w @ v).abs() + (2.0 ** -11 + 2 * off + sums)[:, None] * A + gone[:, None] + z + 2.0 ** -40
                 at, heads = slice(first, first + n), slice(h * G, (h + 1) * G)
                 out[at, heads], room[at, heads] = o.view(n, G, D), tol.view(n, G, D)
