@@ -158,7 +158,7 @@ class KvStep(_OnStream):
         self.granted = _view(self.buffer, v.granted, torch.int32, (R,))
         self.starts = _view(self.buffer, v.starts, torch.int32, (R + 1,))
         self.slots = _view(self.buffer, v.slots, torch.int64, (self.max_tokens,))
-        self._work, self._work_dim = None, 0
+        self._works, self._work_dim = [], 0
         self.planned = False
 
     def set_max_new(self, max_new):
@@ -171,12 +171,13 @@ class KvStep(_OnStream):
     def work(self, owner=None):
         """The attention's workspace, shared by the layers, which run one after
         another; made for the stream of `owner` when it is first asked for, and
-        again for a layer of larger heads than those before."""
+        again for a layer of larger heads than those before (the older ones stay: a
+        recorded graph may hold them)."""
         owner = owner or self
         if owner.cfg.dim > self._work_dim:
-            self._work = owner._buffer(self._lib.agft_kv_attend_bytes(owner._cfg, self.max_tokens), "cache")
+            self._works.append(owner._buffer(self._lib.agft_kv_attend_bytes(owner._cfg, self.max_tokens), "cache"))
             self._work_dim = owner.cfg.dim
-        return self._work
+        return self._works[-1]
 
 
 class KvTables(_OnStream):

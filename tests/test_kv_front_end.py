@@ -1,5 +1,6 @@
 """What the cache's front end refuses before anything is enqueued (CPU: calls
 that would launch are noted by kv_stub.py instead)."""
+import weakref
 from types import SimpleNamespace
 
 import pytest
@@ -141,3 +142,13 @@ def test_objects_and_streams_of_other_devices(lib):
     refused(lib, lambda: cache.attend(tables, step, q), "cuda:3")
     step.device = torch.device("cuda", 3)
     refused(lib, lambda: cache.append(step, k, k), "cuda:3")
+
+
+def test_older_workspaces_stay(lib):
+    """A recorded graph may hold the one that a larger layer's replaced."""
+    cfg = kv_config(**BASE)
+    tables = KvTables(cfg)
+    step = tables.plan(torch.ones(64, dtype=torch.int32), 32)
+    small = weakref.ref(step.work(KvCache(cfg)))
+    big = step.work(KvCache(kv_config(**{**BASE, "dim": 256})))
+    assert small() is not None and step.work() is big
