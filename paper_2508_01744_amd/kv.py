@@ -269,13 +269,16 @@ class KvCache(_OnStream):
 
     def load(self, codes, exps):
         """Take over codes uint8 [pages][heads][2][page][dim] (keys, values) and
-        exponents int32 [pages][heads][2].  Set-up: waits for the GPU."""
+        exponents int32 [pages][heads][2] in -126..126.  Set-up: checks the
+        exponents, waits for the GPU."""
         c = self.cfg
         if codes.dtype != torch.uint8 or tuple(codes.shape) != (c.pages, c.heads, 2, c.page, c.dim):
             raise ValueError("codes must be uint8 [pages][heads][2][page][dim]")
         if exps.dtype != torch.int32 or tuple(exps.shape) != (c.pages, c.heads, 2):
             raise ValueError("exps must be int32 [pages][heads][2]")
         self._dev(codes), self._dev(exps)
+        if bool(((exps < -126) | (exps > 126)).any()):
+            raise ValueError("exponents out of range: -126..126")
         with self._settled():
             self.exps.copy_(exps)
             part = max(1, (1 << 28) // (c.heads * 2 * c.page * c.dim))

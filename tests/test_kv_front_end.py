@@ -1,5 +1,6 @@
 """What the cache's front end refuses before anything is enqueued (CPU: calls
 that would launch are noted by kv_stub.py instead)."""
+import contextlib
 import weakref
 from types import SimpleNamespace
 
@@ -152,3 +153,19 @@ def test_older_workspaces_stay(lib):
     small = weakref.ref(step.work(KvCache(cfg)))
     big = step.work(KvCache(kv_config(**{**BASE, "dim": 256})))
     assert small() is not None and step.work() is big
+
+
+@pytest.mark.parametrize("bad", [-127, -200, 127, 128, 2 ** 31 - 1, -2 ** 31])
+def test_exponents_that_are_none(lib, monkeypatch, bad):
+    """A scale of 2^e, and of 2^-e, has to be a number of fp32."""
+    monkeypatch.setattr(kv._OnStream, "_settled", lambda self: contextlib.nullcontext())
+    cfg = kv_config(**{**BASE, "pages": 3})
+    cache = KvCache(cfg)
+    codes = torch.randint(0, 100, (3, 8, 2, 16, 64), dtype=torch.uint8)
+    exps = torch.randint(-126, 127, (3, 8, 2), dtype=torch.int32)
+    exps[0, 0, 0], exps[0, 0, 1] = -126, 126
+    cache.load(codes, exps)
+    held = cache.buffer.clone()
+    exps[2, 5, 1] = bad
+    refused(lib, lambda: cache.load(codes + 1, exps), "exponents")
+    assert torch.equal(cache.buffer, held)
