@@ -11,6 +11,7 @@ One window of a node with a KvTables `tables` and, per layer, a KvCache `cache`:
 
 Calls enqueue on the stream given to the object, or else on the stream that is
 current when they are called; nothing here waits for the GPU except load().
+There is no backward pass: tensors that ask for a gradient are refused.
 Launches go to the calling thread's current device, which has to be the object's.
 Tensors of another stream are the caller's to order, as for any torch call.
 """
@@ -305,6 +306,9 @@ class KvCache(_OnStream):
         if n < rows or h != heads or dim != self.cfg.dim or one != 1 or t.get_device() != self.device.index:
             raise ValueError(f"{what} must be [{rows} or more][{heads}][{self.cfg.dim}] on {self.device}, "
                              f"{' or '.join(str(d) for d in types)}, with contiguous numbers of a head")
+        if t.requires_grad and torch.is_grad_enabled():
+            raise ValueError(f"{what} asks for a gradient, and these calls have none: detach it, or call under "
+                             "torch.no_grad()")
         ptr = t.data_ptr()
         per = 7 if kind != L.AGFT_KV_FP32 else 3
         if ptr & 15 or token & per or head & per:

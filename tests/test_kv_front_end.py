@@ -169,3 +169,25 @@ def test_exponents_that_are_none(lib, monkeypatch, bad):
     exps[2, 5, 1] = bad
     refused(lib, lambda: cache.load(codes + 1, exps), "exponents")
     assert torch.equal(cache.buffer, held)
+
+
+def test_no_gradient_is_lost_in_silence(lib):
+    """There is no backward pass: inputs that ask for one are refused."""
+    cfg = kv_config(**BASE)
+    tables, cache = KvTables(cfg), KvCache(cfg)
+    step = tables.plan(torch.ones(64, dtype=torch.int32), 32)
+    k, q = tensors(cfg)
+    for t in (k, q):
+        t.requires_grad_()
+    refused(lib, lambda: cache.append(step, k, k.detach()), "gradient")
+    refused(lib, lambda: cache.append(step, k.detach(), k), "gradient")
+    refused(lib, lambda: cache.attend(tables, step, q), "gradient")
+    refused(lib, lambda: cache.attend(tables, step, q * 1), "gradient")
+    refused(lib, lambda: cache.attend(tables, step, q.detach(), out=q), "gradient")
+    with torch.no_grad():
+        cache.append(step, k, k)
+        cache.attend(tables, step, q)
+    with torch.inference_mode():
+        cache.attend(tables, step, q)
+    cache.append(step, k.detach(), k.detach())
+    cache.attend(tables, step, q.detach())
