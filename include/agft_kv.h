@@ -141,7 +141,8 @@ int agft_kv_commit(const agft_kv_config *cfg, void *d_tables, size_t tables_byte
 
 /*
  * A dense tensor [tokens][heads][dim] of a window: numbers of a head are
- * contiguous, strides count numbers.  Base and strides: multiples of 16 bytes.
+ * contiguous, strides count numbers.  Base and strides: multiples of 16 bytes;
+ * strides of an output are not 0 (of an input they may be).
  */
 typedef struct agft_kv_dense {
     void *data;

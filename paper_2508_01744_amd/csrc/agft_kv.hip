@@ -952,6 +952,7 @@ int agft_kv_export(const agft_kv_config *cfg, const void *d_cache, size_t cache_
     if (n == 0) return AGFT_OK;
     if (d_slots == nullptr || reinterpret_cast<uintptr_t>(d_slots) % 8 != 0) return AGFT_E_INVAL;
     if (!dense_ok(k) || !dense_ok(v) || k->type != v->type) return AGFT_E_INVAL;
+    if (!apart(k, n, cfg->heads) || !apart(v, n, cfg->heads)) return AGFT_E_INVAL;
     ExportArgs p;
     p.codes = static_cast<const char *>(d_cache) + C.codes;
     p.exps = reinterpret_cast<const int32_t *>(static_cast<const char *>(d_cache) + C.exps);

@@ -1199,6 +1199,7 @@ int agft_kv_attend(const agft_kv_config *cfg, const void *d_cache, size_t cache_
     if (!buffer_ok(d_cache, cache_bytes, C.total)) return AGFT_E_INVAL;
     if (!buffer_ok(d_work, work_bytes, agft_kv_attend_bytes(cfg, max_tokens))) return AGFT_E_INVAL;
     if (!dense_ok(q) || !dense_ok(out) || q->type != out->type || q->type == AGFT_KV_FP32) return AGFT_E_INVAL;
+    if (!apart(out, max_tokens, (int64_t)cfg->heads * cfg->group)) return AGFT_E_INVAL;
     if (max_new < 1 || max_new > max_tokens || !std::isfinite(scale)) return AGFT_E_INVAL;
     if (reinterpret_cast<uintptr_t>(d_lse) % 4 != 0) return AGFT_E_INVAL;
     AttendArgs p;

@@ -166,6 +166,11 @@ inline bool dense_ok(const agft_kv_dense *t) {
            t->token_stride % per == 0 && t->head_stride % per == 0;
 }
 
+// and of which each has memory of its own
+inline bool apart(const agft_kv_dense *t, int64_t tokens, int64_t heads) {
+    return (t->token_stride > 0 || tokens == 1) && (t->head_stride > 0 || heads == 1);
+}
+
 inline int log2_of(int32_t page) { return page == 16 ? 4 : page == 32 ? 5 : page == 64 ? 6 : 7; }
 
 inline int launched() { return hipGetLastError() == hipSuccess ? AGFT_OK : AGFT_E_HIP; }
