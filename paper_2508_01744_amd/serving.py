@@ -33,6 +33,8 @@ class Batch:
     block table, and how many new tokens each brings to a window."""
 
     def __init__(self, rows, queue_cap, tokens, row_tokens, seed=0):
+        if rows < 1 or tokens < 1 or row_tokens < 32:
+            raise ValueError("a node has at least one row of 32 tokens or more, and windows of a token or more")
         self.rows, self.queue_cap, self.tokens, self.row_tokens = rows, queue_cap, tokens, row_tokens
         self.rng = np.random.default_rng(seed)
         self.queue = []                     # (prompt, outputs) of requests that wait
@@ -127,6 +129,8 @@ def features(arrivals, queue, running, latency, rows, used, clock):
 
 def run(windows=300, workload="cfg1", seed=0, **node_options):
     """Let one tuner run a measured node for some windows; a summary dict."""
+    if windows < 1:
+        raise ValueError("at least one window")
     wl = get_workload(workload, B=1, T=windows)
     if wl.d != 8:
         raise ValueError("the measured node's context has 8 features")
