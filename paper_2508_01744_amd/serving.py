@@ -4,7 +4,9 @@ through the window's cache and attention work, layer by layer, and a tuner sees
 the node that results (Sec. 4.1's collector, features and decision loop, Fig. 5).
 
 What is real: continuous batching of prompts (in chunks) and single tokens,
-block tables, cache writes, attention, their time on the GPU.  What is not: the
+block tables, cache writes, attention, and their time, from the first call to
+the end of the work on the GPU: a window of little work takes as long as the
+host needs for its calls (4 to 8 us each).  What is not: the
 numbers (queries, keys and values are drawn once), the rest of a model, and the
 clock: the card's own stays as it is.  A decision's clock f enters by the closed
 form that the simulator uses, power P0 + c f^3 and a latency of which the share
@@ -106,7 +108,9 @@ class ServingNode:
         self._times = torch.cuda.Event(enable_timing=True), torch.cuda.Event(enable_timing=True)
 
     def window(self, add):
-        """One window's work; the time it took on the GPU in milliseconds."""
+        """One window's work; the time in milliseconds from its first call to its
+        end on the GPU, the host's time for the calls included where the GPU waits
+        for them."""
         new = torch.tensor(add, dtype=torch.int32).to(self.device)
         first, last = self._times
         first.record()
