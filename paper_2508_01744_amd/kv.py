@@ -53,11 +53,14 @@ except AttributeError:
     _current_device = torch.cuda.current_device
 
 
+_one = {}       # devices and configurations' tuples, one object each: compared at every call
+
+
 def _device(device):
     device = torch.device(device)
     if device.type == "cuda" and device.index is None:
         device = torch.device("cuda", torch.cuda.current_device())
-    return device
+    return _one.setdefault(device, device)
 
 
 class _OnStream:
@@ -68,23 +71,23 @@ class _OnStream:
     def _init(self, cfg, device, stream):
         # (a copy: sizes and layouts follow from it)
         self.cfg, self.device = type(cfg).from_buffer_copy(cfg), _device(device)
+        self._index = self.device.index
         self.set_stream(stream)
         self._cfg = ctypes.byref(self.cfg)
         self._lib = L.lib()
         # where the parts of tables and steps lie; layers may differ in dim and form
-        self._shape = (cfg.requests, cfg.row_pages, cfg.pages, cfg.page, cfg.heads, cfg.group)
+        shape = cfg.requests, cfg.row_pages, cfg.pages, cfg.page, cfg.heads, cfg.group
+        self._shape = _one.setdefault(shape, shape)
 
-    def _same(self, other, what):
-        if other.device != self.device:
+    def _fits(self, other, what):
+        """Refuse tables and steps of other devices or configurations, and steps without a plan."""
+        if other.device is not self.device and other.device != self.device:
             raise ValueError(f"{what} on {other.device}, not {self.device}")
-        if other._shape != self._shape:
+        if other._shape is not self._shape:
             raise ValueError(f"{what} of another configuration: (requests, row_pages, pages, page, heads, group) "
                              f"{other._shape}, not {self._shape}")
-
-    def _planned(self, step):
-        self._same(step, "step")
-        if not step.planned:
-            raise ValueError("the step has not been planned: its memory holds nothing yet")
+        if not other.planned:
+            raise ValueError(f"the {what} has not been planned: its memory holds nothing yet")
 
     def set_stream(self, stream):
         """Enqueue on `stream` from now on (None: on the stream current at each call)."""
@@ -93,11 +96,11 @@ class _OnStream:
         self.stream = stream
 
     def _s(self):
-        if _current_device() != self.device.index:
+        if _current_device() != self._index:
             raise ValueError(f"work on {self.device} while the current device is {_current_device()}: launches go to "
                              "the current device")
         # (the raw handle: a window's calls are short enough for the Stream object's microseconds to count)
-        return _current_raw_stream(self.device.index) if self.stream is None else self.stream.cuda_stream
+        return _current_raw_stream(self._index) if self.stream is None else self.stream.cuda_stream
 
     @contextlib.contextmanager
     def _settled(self):
@@ -184,6 +187,7 @@ class KvStep(_OnStream):
 class KvTables(_OnStream):
     """Block tables, lengths and the ring of free pages of a node's requests:
     counters [8], lengths [R], table [R][row_pages], ring [pages] (int32)."""
+    planned = True      # (as a step's: their memory holds something from the start)
 
     def __init__(self, cfg, device="cuda", stream=None):
         self._init(cfg, device, stream)
@@ -233,7 +237,8 @@ class KvTables(_OnStream):
         if step is None:
             step = KvStep(self.cfg, max_tokens, max_new, self.device, self.stream)
         else:
-            self._same(step, "step")
+            if step.device != self.device or step._shape is not self._shape:
+                self._fits(step, "step")
             if step.max_tokens != max_tokens:
                 raise ValueError(f"step is for {step.max_tokens} tokens, not {max_tokens}")
             step.set_max_new(max_new)
@@ -246,7 +251,7 @@ class KvTables(_OnStream):
 
     def commit(self, step):
         """The planned window's lengths and free pages become the tables'."""
-        self._planned(step)
+        self._fits(step, "step")
         L.check("agft_kv_commit", self._lib.agft_kv_commit(self._cfg, self.ptr, self.nbytes, step.ptr, step.nbytes,
                                                            step.max_tokens, self._s()))
 
@@ -303,7 +308,7 @@ class KvCache(_OnStream):
             kind = types[t.dtype]
         except (ValueError, KeyError):
             n = h = dim = one = -1
-        if n < rows or h != heads or dim != self.cfg.dim or one != 1 or t.get_device() != self.device.index:
+        if n < rows or h != heads or dim != self.cfg.dim or one != 1 or t.get_device() != self._index:
             raise ValueError(f"{what} must be [{rows} or more][{heads}][{self.cfg.dim}] on {self.device}, "
                              f"{' or '.join(str(d) for d in types)}, with contiguous numbers of a head")
         if t.requires_grad and torch.is_grad_enabled():
@@ -319,7 +324,7 @@ class KvCache(_OnStream):
         """Store the window's keys and values, [max_tokens][heads][dim] each
         (bf16, fp16 or fp32), rows as in step.starts."""
         H, n = self.cfg.heads, step.max_tokens
-        self._planned(step)
+        self._fits(step, "step")
         if k.dtype != v.dtype:
             raise ValueError("k and v must have one type")
         self._dense(self._d0, k, H, n, "k")
@@ -337,8 +342,8 @@ class KvCache(_OnStream):
         scale: 1 / sqrt(dim) if None."""
         c, n = self.cfg, step.max_tokens
         hq = c.heads * c.group
-        self._planned(step)
-        self._same(tables, "tables")
+        self._fits(step, "step")
+        self._fits(tables, "tables")
         if out is None:
             out = self._empty(n, hq, c.dim, dtype=q.dtype)
         elif out.dtype != q.dtype:
