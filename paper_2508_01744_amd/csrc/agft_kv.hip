@@ -230,8 +230,10 @@ __device__ __forceinline__ void plan_chunk(const PlanArgs &p, int r0, uint32_t n
 // 61 us; 128 rows of 8 requests over 4,000 tokens, 128 numbers, 33 / 33 / 35), and
 // at least kSecondTiles where it would give it a second one (8 / 16 / 24: 2,774
 // tokens of 7 query heads on one head of 64 36 / 28 / 32 us; 128 rows of 64
-// requests over 1,000 tokens, 256 tiles, 40 / 33 / 33).  (For up to kPlanChunk
-// requests; beyond, tiles go by request, in one part.)
+// requests over 1,000 tokens, 256 tiles, 40 / 33 / 33).  For up to kPlanChunk
+// requests; beyond, tiles go by request, in one part (64 tokens of 16 query heads
+// over 131,000: 1,830 us in a table of 1,025 rows, 115 in one of 1,024; 10 chunks of
+// 512 over 3,000 316 and 326).
 constexpr int kPartTiles = 8;
 constexpr int kSecondTiles = 16;
 constexpr int kMaxParts = 64;
@@ -607,8 +609,9 @@ struct AppendArgs {
 // One workgroup per run (tokens of one page), head and side; one wavefront per
 // 16 tokens of the page.  Lane 16 g + m holds token m's numbers 16 g..16 g + 15
 // of each 64: the layout's key entry, and what a value entry is turned from.
-// Memory bounds it: 17,641 tokens of 8 heads of 128 numbers, bf16 to e4m3, 24.7 us,
-// 4.4 TB/s of numbers and codes; single tokens are a chain of loads, 4.5 us.
+// 17,641 tokens of 8 heads of 128 numbers, bf16 to e4m3, 24.8 us, 4.4 TB/s of
+// numbers and codes (reading and writing reach 6.2; the values' turn through LDS is
+// a byte at a time); single tokens are a chain of loads, 4.5 us.
 template <int FORM, int TYPE, int DIM>
 __global__ void agft_kv_append_kernel(AppendArgs p) {
     constexpr int DG = DIM / kBlockDims;
@@ -740,8 +743,8 @@ struct ExportArgs {
 // Four threads per slot, a head and a side per workgroup; a thread takes 16
 // numbers of each 64: one key entry, or one byte of each of 16 value entries
 // (which neighbouring slots' threads read too, from the same lines).
-// Memory bounds it: 17,800 slots of 8 heads of 128 numbers, e4m3 to bf16, 30.6 us,
-// 3.6 TB/s of codes and numbers (a thread per key and value: 87 us for the write and
+// 17,800 slots of 8 heads of 128 numbers, e4m3 to bf16, 30.6 us, 3.6 TB/s of codes
+// and numbers (reading and writing reach 6.2; a thread per key and value: 87 us for the write and
 // the export of such prompts, 55 so).
 constexpr int kExportSlots = 64;
 

@@ -142,8 +142,8 @@ __device__ __forceinline__ float across_sum(float x) {
 // whichever it is.
 //
 // What bounds it: memory, once there are some hundred MB (24 tokens over 60,000 to
-// 131,071 tokens, a cache of 4.45 GB: 754 us, 5.9 TB/s; a copy reaches 4.8, reads
-// and writes together), and a chain of loads below (requests, page, exponents,
+// 131,071 tokens, a cache of 4.45 GB: 757 us, 5.9 TB/s; reading alone reaches 7.1),
+// and a chain of loads below (requests, page, exponents,
 // codes, the pieces' way to the join: one token over 778 tokens 8.1 us).
 //
 // Scores are made transposed, S^T = K Q^T (16 tokens x 16 rows per matrix
@@ -804,7 +804,7 @@ __device__ __forceinline__ void attend_few(const AttendArgs &p, FewLds<DIM> &lds
 // tokens.
 //
 // The prompt (32 query heads, 8 key/value heads of 128 numbers, causal: 2.2 TFLOP)
-// takes 2.06 to 2.25 ms on different cards, 1.0 PFLOP/s, 80% of what a large matrix
+// takes 2.08 to 2.23 ms on different cards, 1.0 PFLOP/s, 80% of what a large matrix
 // product of the library reaches; matrix cores, LDS and vector instructions are each
 // busy for about half of the cycles at a clock that their power sets.
 typedef float float16v __attribute__((ext_vector_type(16)));
