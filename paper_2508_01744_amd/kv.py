@@ -337,7 +337,8 @@ class KvCache(_OnStream):
     def attend(self, tables, step, q, out=None, lse=None, scale=None):
         """softmax(scale q K^T) V of the window's tokens over their requests'
         tokens up to themselves.  q, out [max_tokens][heads * group][dim], bf16
-        or fp16 (out is allocated if None); lse float32
+        or fp16 (out is allocated if None; rows past the window's tokens stay as
+        they are, in a fresh one whatever its memory held); lse float32
         [max_tokens][heads * group] or None receives the logarithms of the sums;
         scale: 1 / sqrt(dim) if None."""
         c, n = self.cfg, step.max_tokens
