@@ -143,8 +143,8 @@ __device__ __forceinline__ float across_sum(float x) {
 //
 // What bounds it: memory, once there are some hundred MB (24 tokens over 60,000 to
 // 131,071 tokens, a cache of 4.45 GB: 757 us, 5.9 TB/s; reading alone reaches 7.1),
-// and a chain of loads below (requests, page, exponents,
-// codes, the pieces' way to the join: one token over 778 tokens 8.1 us).
+// and a chain of loads below (requests, page, exponents, codes, the pieces' way to
+// the join: one token over 778 tokens 8.1 us).
 //
 // Scores are made transposed, S^T = K Q^T (16 tokens x 16 rows per matrix
 // instruction), so that a lane holds four tokens' probabilities of one row,
@@ -157,13 +157,14 @@ __device__ __forceinline__ float across_sum(float x) {
 // 2^-ev, and the output is O / l.  P meets the codes as 2^kRaise P in fp16.
 //
 // That rounding is what lets the second product run on matrix instructions: each
-// P keeps eleven bits (within 2^-11 of itself), what an fp16 output does.  Below 2^-14 fp16 keeps
-// fewer bits and below 2^-25 nothing, hence kRaise, which brings the largest near
-// the end of its range (65,504): what lies 2^-29 below the largest has its eleven
-// bits, and what is lost lies 2^-40 below (2^-25 without it: 131,000 tokens of
-// 2^-25.1 each beside one large one lost their 0.4% of the output).  l sums the P
-// that were not rounded: pages' exponents may lie so far apart that one's P vanish
-// beside another's larger values, and its tokens' weights must stay in l.
+// P keeps eleven bits (within 2^-11 of itself), what an fp16 output does.  Below
+// 2^-14 fp16 keeps fewer bits and below 2^-25 nothing, hence kRaise, which brings
+// the largest near the end of its range (65,504): what lies 2^-29 below the largest
+// has its eleven bits, and what is lost lies 2^-40 below (2^-25 without it: of
+// tokens that a wavefront saw beside one 2^25.1 times as large, nothing was left,
+// which for 131,000 of them is 0.4% of the output).  l sums the P that were not
+// rounded: pages' exponents may lie so far apart that one's P vanish beside
+// another's larger values, and its tokens' weights must stay in l.
 constexpr int kFewWaves = 4;
 // Up to kFewPieces pieces are read in one round trip, weights and all (4 / 8: one
 // token over 778 tokens 10.4 / 10.7 us); more get their weights first, kAtOnce on
