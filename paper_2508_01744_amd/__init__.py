@@ -7,8 +7,8 @@ from ._lib import LIB_PATH, AgftError, lib
 from .tuner import Tuner, launch_shape, make_config, workload_config
 from .env import GpuEnv, env_config
 from .sim import run_closed_loop
-from .kv import KvCache, KvStep, KvTables, kv_config
+from .kv import KvCache, KvEdit, KvStep, KvTables, kv_config
 
 __all__ = ["LIB_PATH", "AgftError", "lib", "Tuner", "launch_shape", "make_config", "workload_config",
            "GpuEnv", "env_config", "run_closed_loop",
-           "KvCache", "KvStep", "KvTables", "kv_config"]
+           "KvCache", "KvEdit", "KvStep", "KvTables", "kv_config"]

@@ -1,13 +1,16 @@
 """Build libagft.so (HIP, gfx950) in-tree with hipcc."""
 import os
 import subprocess
+import tempfile
+from concurrent.futures import ThreadPoolExecutor
 
 PKG = os.path.dirname(os.path.abspath(__file__))
 ROOT = os.path.dirname(PKG)
 CSRC = os.path.join(PKG, "csrc")
 INCLUDE = os.path.join(ROOT, "include")
 LIB = os.path.join(PKG, "libagft.so")
-SOURCES = [os.path.join(CSRC, name) for name in ("agft_step.hip", "agft_env.hip", "agft_kv.hip", "agft_kv_attend.hip")]
+SOURCES = [os.path.join(CSRC, name) for name in ("agft_step.hip", "agft_env.hip", "agft_kv.hip", "agft_kv_attend.hip",
+                                               "agft_pages.hip")]
 
 HIPCC_FLAGS = [
     "--offload-arch=gfx950", "-O3", "-std=c++17", "-fPIC", "-shared",
@@ -18,13 +21,21 @@ HIPCC_FLAGS = [
 
 
 def build(verbose=False, extra_flags=()):
-    """Compile every HIP source into paper_2508_01744_amd/libagft.so."""
+    """Compile every HIP source, side by side, into paper_2508_01744_amd/libagft.so."""
     hipcc = os.environ.get("HIPCC", "/opt/rocm/bin/hipcc")
     tmp = LIB + ".tmp"
-    cmd = [hipcc, *HIPCC_FLAGS, *extra_flags, "-I", INCLUDE, *SOURCES, "-o", tmp]
-    if verbose:
-        print(" ".join(cmd), flush=True)
-    subprocess.run(cmd, check=True)
+    compile_flags = [f for f in HIPCC_FLAGS if f != "-shared"]
+
+    def run(cmd):
+        if verbose:
+            print(" ".join(cmd), flush=True)
+        subprocess.run(cmd, check=True)
+
+    with tempfile.TemporaryDirectory() as folder, ThreadPoolExecutor(len(SOURCES)) as pool:
+        objects = [os.path.join(folder, os.path.basename(s)[:-4] + ".o") for s in SOURCES]
+        list(pool.map(lambda s, o: run([hipcc, *compile_flags, *extra_flags, "-I", INCLUDE, "-c", s, "-o", o]), SOURCES,
+                      objects))
+        run([hipcc, "--offload-arch=gfx950", "-fPIC", "-shared", *extra_flags, *objects, "-o", tmp])
     os.replace(tmp, LIB)
     return LIB
 

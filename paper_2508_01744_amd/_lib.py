@@ -1,6 +1,7 @@
 """ctypes binding of libagft.so: argument marshalling only.
 
-The names mirror include/agft.h, include/agft_sim.h and include/agft_kv.h.  Loading fails loudly
+The names mirror include/agft.h, include/agft_sim.h, include/agft_kv.h and
+include/agft_pages.h.  Loading fails loudly
 when the library has not been built: there is no other implementation to
 fall back to.
 """
@@ -73,6 +74,10 @@ class agft_kv_dense(ctypes.Structure):
     _fields_ = [("data", _vp), ("token_stride", _i64), ("head_stride", _i64), ("type", _i32)]
 
 
+class agft_pages_view(ctypes.Structure):
+    _fields_ = [("counters", _vp), ("lengths", _vp), ("granted", _vp), ("moves", _vp)]
+
+
 AGFT_KV_E4M3, AGFT_KV_INT8 = 0, 1
 AGFT_KV_BF16, AGFT_KV_FP16, AGFT_KV_FP32 = 0, 1, 2
 
@@ -86,6 +91,10 @@ EXPORTED = ["agft_state_bytes", "agft_create", "agft_step", "agft_get_state", "a
 KV_EXPORTED = ["agft_kv_tables_bytes", "agft_kv_step_bytes", "agft_kv_cache_bytes", "agft_kv_attend_bytes",
                "agft_kv_tables_at", "agft_kv_step_at", "agft_kv_reset", "agft_kv_plan", "agft_kv_commit",
                "agft_kv_append", "agft_kv_attend", "agft_kv_export"]
+
+# of agft_pages.h
+PAGES_EXPORTED = ["agft_pages_edit_bytes", "agft_pages_edit_at", "agft_pages_owners_at", "agft_pages_fork",
+                  "agft_pages_trim", "agft_pages_compact", "agft_pages_copy", "agft_pages_commit"]
 
 _lib = None
 
@@ -142,6 +151,18 @@ def _declare(lib):
                                       _vp]),
             ("export", ctypes.c_int, [_vp, _sz, _vp, _i64, densep, densep, _vp])):
         fn = getattr(lib, "agft_kv_" + name)
+        fn.restype, fn.argtypes = restype, [kvp, *args]
+    edit = [_vp, _sz, _i32]
+    for name, restype, args in (
+            ("edit_bytes", _sz, [_i32]),
+            ("edit_at", ctypes.c_int, [_i32, _vp, _sz, ctypes.POINTER(agft_pages_view)]),
+            ("owners_at", ctypes.c_int, [_vp, _sz, ctypes.POINTER(_vp)]),
+            ("fork", ctypes.c_int, [_vp, _sz, _vp, _vp, _vp, _i32, *edit, _vp]),
+            ("trim", ctypes.c_int, [_vp, _sz, _vp, *edit, _vp]),
+            ("compact", ctypes.c_int, [_vp, _sz, *edit, _vp]),
+            ("copy", ctypes.c_int, [_vp, _sz, *edit, _vp]),
+            ("commit", ctypes.c_int, [_vp, _sz, *edit, _vp])):
+        fn = getattr(lib, "agft_pages_" + name)
         fn.restype, fn.argtypes = restype, [kvp, *args]
     return lib
 

@@ -51,12 +51,13 @@ struct Ask {
     bool wants, ends;
 };
 
-__device__ __forceinline__ Ask ask_of(const PlanArgs &p, int32_t past, int32_t add) {
+// (No request ends here while pages have several owners: agft_pages.h.)
+__device__ __forceinline__ Ask ask_of(const PlanArgs &p, int32_t past, int32_t add, bool shared) {
     Ask a;
     const int32_t cap = p.row_pages << p.shift;
     a.past = past < 0 ? 0 : past > cap ? cap : past;
-    a.wants = add > 0;
-    a.ends = add < 0;
+    a.wants = add > 0 || (add < 0 && shared);
+    a.ends = add < 0 && !shared;
     a.held = pages_of(a.past, p.page, p.shift);
     a.tokens = add > 0 && add <= cap - a.past ? add : 0;
     a.need = pages_of(a.past + (int32_t)a.tokens, p.page, p.shift) - a.held;
@@ -151,11 +152,12 @@ __device__ __forceinline__ void plan_chunk(const PlanArgs &p, int r0, uint32_t n
     const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
     const int i0 = r0 + threadIdx.x * PER;
     Ask a[PER];
+    const bool shared = p.counters[2] != 0;
     uint32_t need = 0, tok = 0, mid = 0;
 #pragma unroll
     for (int j = 0; j < PER; ++j) {
         const bool live = i0 + j < p.requests;
-        a[j] = ask_of(p, live ? p.lengths[i0 + j] : 0, live ? p.add[i0 + j] : 0);
+        a[j] = ask_of(p, live ? p.lengths[i0 + j] : 0, live ? p.add[i0 + j] : 0, shared);
         need = add_sat(need, a[j].need), tok = add_sat(tok, a[j].tokens), mid = add_sat(mid, mid_units(p, a[j]));
     }
     uint32_t need_in = need, tok_in = tok;
@@ -434,7 +436,7 @@ __global__ __launch_bounds__(kSumsThreads) void agft_kv_plan_sums_kernel(PlanArg
         }
 #pragma unroll
         for (int z = 0; z < AHEAD; ++z) {
-            const Ask a = ask_of(p, past[z], add[z]);
+            const Ask a = ask_of(p, past[z], add[z], false);
             need0 = add_sat(need0, a.need), tok0 = add_sat(tok0, a.tokens);
         }
     }
@@ -497,8 +499,8 @@ __global__ __launch_bounds__(kPlanThreads) void agft_kv_plan_slots_kernel(PlanAr
         const int i = r0 + lane;
         const bool live = lane < 16 && i < p.requests;
         if (live) p.works[i].few += s_off[1][i / kPlanChunk];
-        const bool ends = live && p.add[i] < 0;
-        const Ask a = ask_of(p, ends ? p.lengths[i] : 0, 0);
+        const bool ends = live && p.add[i] < 0 && p.counters[2] == 0;
+        const Ask a = ask_of(p, ends ? p.lengths[i] : 0, 0, false);
         plan_give_back(p, ends, i, a.held, ends ? p.back[i] + s_off[3][i / kPlanChunk] : 0, head, free_pages);
     }
     for (int64_t t0 = (int64_t)blockIdx.x * kPlanTokens; t0 < p.max_tokens; t0 += (int64_t)gridDim.x * kPlanTokens) {
@@ -525,7 +527,7 @@ __global__ __launch_bounds__(kPlanThreads) void agft_kv_plan_slots_kernel(PlanAr
                 plan_items(p, i, (int32_t)t - first, tiles, s_off[2][i / kPlanChunk] + p.tiles[i], 1);
             }
             if (t < total && p.granted[i] > 0)
-                plan_token(p, t, i, ask_of(p, p.lengths[i], 0).past, (int32_t)t - p.starts[i], p.need[i],
+                plan_token(p, t, i, ask_of(p, p.lengths[i], 0, false).past, (int32_t)t - p.starts[i], p.need[i],
                            p.touched[i] + s_off[0][i / kPlanChunk], head);
             else
                 p.slots[t] = -1;
@@ -534,14 +536,14 @@ __global__ __launch_bounds__(kPlanThreads) void agft_kv_plan_slots_kernel(PlanAr
 }
 
 __global__ __launch_bounds__(256) void agft_kv_reset_kernel(int32_t *counters, int32_t *lengths, int32_t *table,
-                                                            int32_t *ring, int32_t requests, int64_t entries,
-                                                            int32_t pages) {
+                                                            int32_t *ring, int32_t *owners, int64_t *marks,
+                                                            int32_t requests, int64_t entries, int32_t pages) {
     const int64_t stride = (int64_t)gridDim.x * blockDim.x;
     const int64_t id = (int64_t)blockIdx.x * blockDim.x + threadIdx.x;
     if (id < 8) counters[id] = id == 1 ? pages : 0;
     for (int64_t j = id; j < requests; j += stride) lengths[j] = 0;
     for (int64_t j = id; j < entries; j += stride) table[j] = 0;
-    for (int64_t j = id; j < pages; j += stride) ring[j] = (int32_t)j;
+    for (int64_t j = id; j < pages; j += stride) ring[j] = (int32_t)j, owners[j] = 0, marks[j] = 0;
 }
 
 __global__ __launch_bounds__(256) void agft_kv_commit_kernel(int32_t *counters, int32_t *lengths,
@@ -855,8 +857,11 @@ int agft_kv_reset(const agft_kv_config *cfg, void *d_tables, size_t tables_bytes
     agft_kv_tables_view v;
     const int st = agft_kv_tables_at(cfg, d_tables, tables_bytes, &v);
     if (st != AGFT_OK) return st;
+    const TablesLayout L = tables_layout(cfg);
+    char *base = static_cast<char *>(d_tables);
     hipLaunchKernelGGL(agft_kv_reset_kernel, dim3(1024), dim3(256), 0, static_cast<hipStream_t>(stream), v.counters,
-                       v.lengths, v.table, v.ring, cfg->requests, (int64_t)cfg->requests * cfg->row_pages, cfg->pages);
+                       v.lengths, v.table, v.ring, reinterpret_cast<int32_t *>(base + L.owners),
+                       reinterpret_cast<int64_t *>(base + L.marks), cfg->requests, (int64_t)cfg->requests * cfg->row_pages, cfg->pages);
     return launched();
 }
 

@@ -59,7 +59,7 @@ inline int config_status(const agft_kv_config *c) {
 inline bool tokens_ok(int32_t max_tokens) { return max_tokens >= 1 && max_tokens <= 1 << 30; }
 
 struct TablesLayout {
-    size_t counters, lengths, table, ring, total;
+    size_t counters, lengths, table, ring, owners, marks, total;
 };
 
 inline TablesLayout tables_layout(const agft_kv_config *c) {
@@ -69,6 +69,8 @@ inline TablesLayout tables_layout(const agft_kv_config *c) {
     L.lengths = at, at += align_up((size_t)c->requests * 4);
     L.table = at, at += align_up((size_t)c->requests * c->row_pages * 4);
     L.ring = at, at += align_up((size_t)c->pages * 4);
+    L.owners = at, at += align_up((size_t)c->pages * 4);    // of each page, beyond the first
+    L.marks = at, at += align_up((size_t)c->pages * 8);     // zeros between calls
     L.total = at;
     return L;
 }

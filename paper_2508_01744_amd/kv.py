@@ -1,4 +1,4 @@
-"""Python front end of the serving node's paged cache (agft_kv.h): torch
+"""Python front end of the serving node's paged cache (agft_kv.h, agft_pages.h): torch
 supplies device memory and streams, the work runs in the HIP kernels behind
 libagft.so.
 
@@ -8,6 +8,12 @@ One window of a node with a KvTables `tables` and, per layer, a KvCache `cache`:
     cache.append(step, k, v)                   # per layer
     out = cache.attend(tables, step, q)        # per layer
     tables.commit(step)                        # the new lengths become the tables'
+
+and between windows the tables can be edited (agft_pages.h):
+
+    edit = tables.fork(src, dst)               # or trim(keep), or compact()
+    cache.copy(edit)                           # per layer
+    tables.commit(edit)
 
 Calls enqueue on the stream given to the object, or else on the stream that is
 current when they are called; nothing here waits for the GPU except load().
@@ -88,6 +94,10 @@ class _OnStream:
                              f"{other._shape}, not {self._shape}")
         if not other.planned:
             raise ValueError(f"the {what} has not been planned: its memory holds nothing yet")
+        if other._of is not None and other._of._edits != other._at:
+            raise ValueError(f"the tables have been edited since the {what} was planned")
+
+    _of = None      # steps: the tables that they were planned from, when those had been edited _at times
 
     def set_stream(self, stream):
         """Enqueue on `stream` from now on (None: on the stream current at each call)."""
@@ -184,9 +194,39 @@ class KvStep(_OnStream):
         return self._works[-1]
 
 
+class KvEdit(_OnStream):
+    """An edit that KvTables.fork, trim or compact writes, on the GPU (`planned` once one has):
+
+    counters [8]         after the edit: ring's head, free pages, owners beyond the first of all pages;
+                         requests refused, pages taken, pages given back, entries of moves, kind
+    lengths [R]          after the edit
+    granted [max_moves]  of a fork: tokens that each one got
+    moves [max_moves][2] pages to copy, from and to; -1 where there is none
+    """
+
+    def __init__(self, cfg, max_moves, device="cuda", stream=None):
+        self._init(cfg, device, stream)
+        self.max_moves = int(max_moves)
+        if not 1 <= self.max_moves <= 1 << 27:
+            raise ValueError("max_moves must be in 1..2^27")
+        self.nbytes = self._lib.agft_pages_edit_bytes(self._cfg, self.max_moves)
+        self.buffer = self._buffer(self.nbytes, "cache")
+        self.ptr = self.buffer.data_ptr()
+        v = L.agft_pages_view()
+        L.check("agft_pages_edit_at", self._lib.agft_pages_edit_at(self._cfg, self.max_moves, self.ptr, self.nbytes,
+                                                                   ctypes.byref(v)))
+        self.counters = _view(self.buffer, v.counters, torch.int32, (8,))
+        self.lengths = _view(self.buffer, v.lengths, torch.int32, (cfg.requests,))
+        self.granted = _view(self.buffer, v.granted, torch.int32, (self.max_moves,))
+        self.moves = _view(self.buffer, v.moves, torch.int32, (self.max_moves, 2))
+        self.planned, self._by, self._when = False, None, -1
+
+
 class KvTables(_OnStream):
     """Block tables, lengths and the ring of free pages of a node's requests:
-    counters [8], lengths [R], table [R][row_pages], ring [pages] (int32)."""
+    counters [8], lengths [R], table [R][row_pages], ring [pages], owners [pages]
+    beyond a page's first (int32).  While a page has several owners, counters[2] is
+    not 0, and requests end by trim: a plan refuses to end them."""
     planned = True      # (as a step's: their memory holds something from the start)
 
     def __init__(self, cfg, device="cuda", stream=None):
@@ -200,15 +240,23 @@ class KvTables(_OnStream):
         self.lengths = _view(self.buffer, v.lengths, torch.int32, (cfg.requests,))
         self.table = _view(self.buffer, v.table, torch.int32, (cfg.requests, cfg.row_pages))
         self.ring = _view(self.buffer, v.ring, torch.int32, (cfg.pages,))
+        owners = ctypes.c_void_p()
+        L.check("agft_pages_owners_at", self._lib.agft_pages_owners_at(self._cfg, self.ptr, self.nbytes,
+                                                                       ctypes.byref(owners)))
+        self.owners = _view(self.buffer, owners.value, torch.int32, (cfg.pages,))
+        # changes of the tables, and edits among them: plans hold for the tables that they were made from
+        self._changes = self._edits = 0
         self.reset()
 
     def reset(self):
         """No request holds a token, every page is free."""
         L.check("agft_kv_reset", self._lib.agft_kv_reset(self._cfg, self.ptr, self.nbytes, self._s()))
+        self._changes += 1
 
-    def load(self, lengths, table, free):
+    def load(self, lengths, table, free, shared=False):
         """Take over the tables of a running node: lengths [R], table
         [R][row_pages] and the free pages in the order of their use (int32).
+        shared: requests may have pages in common, whose owners are counted.
         Set-up: checks the values, which waits for the GPU."""
         cfg = self.cfg
         self._ints(lengths, (cfg.requests,), "lengths")
@@ -222,12 +270,20 @@ class KvTables(_OnStream):
             if wrong:
                 raise ValueError(f"{what} out of range")
         counters = torch.tensor([0, free.numel(), 0, 0, 0, 0, 0, 0], dtype=torch.int32)
+        owners = None
+        if shared:
+            cols = torch.arange(cfg.row_pages, device=table.device)
+            used = cols < ((lengths + (cfg.page - 1)) // cfg.page)[:, None]
+            owners = (torch.bincount(table[used], minlength=cfg.pages) - 1).clamp_(min=0)
+            counters[2] = owners.sum()
         with self._settled():
+            self.owners.zero_() if owners is None else self.owners.copy_(owners)
             self.lengths.copy_(lengths)
             self.table.copy_(table)
             self.ring.zero_()
             self.ring[:free.numel()].copy_(free)
             self.counters.copy_(counters)
+        self._changes += 1
 
     def plan(self, add, max_tokens, max_new=None, step=None):
         """Plan a window: add [R] int32 new tokens per request (0: none, < 0: it
@@ -246,14 +302,73 @@ class KvTables(_OnStream):
                                       step.max_tokens, self._s())
         if code != L.AGFT_OK:
             L.check("agft_kv_plan", code)
-        step.planned = True
+        step.planned, step._of, step._at = True, self, self._edits
         return step
 
     def commit(self, step):
-        """The planned window's lengths and free pages become the tables'."""
+        """The planned window's lengths and free pages, or the planned edit, become the tables'."""
+        if isinstance(step, KvEdit):
+            return self._commit_edit(step)
         self._fits(step, "step")
         L.check("agft_kv_commit", self._lib.agft_kv_commit(self._cfg, self.ptr, self.nbytes, step.ptr, step.nbytes,
                                                            step.max_tokens, self._s()))
+        self._changes += 1
+
+    def _edit(self, name, edit, moves, *args):
+        """Plan an edit with room for `moves` moves."""
+        if edit is None:
+            edit = KvEdit(self.cfg, moves, self.device, self.stream)
+        elif edit.device != self.device or edit._shape is not self._shape:
+            raise ValueError("edit of another device or configuration")
+        code = getattr(self._lib, "agft_pages_" + name)(self._cfg, self.ptr, self.nbytes, *args, edit.ptr, edit.nbytes,
+                                                        edit.max_moves, self._s())
+        if code != L.AGFT_OK:
+            L.check("agft_pages_" + name, code)
+        edit.planned, edit._by, edit._when = True, self, self._changes
+        return edit
+
+    def fork(self, src, dst, tokens=None, edit=None):
+        """Plan forks: request dst[j] gets the first tokens[j] (all if None) tokens
+        of request src[j]; int32 [n], n in 1..65536.  Whole pages are shared, a
+        partly filled last one is copied (KvCache.copy).  dst[j] holds nothing and
+        is named once; edit.granted[j] is 0 where that is not so, or no page is
+        free.  edit: a KvEdit of max_moves n to write again."""
+        n = src.numel()
+        if src.dim() != 1 or not 1 <= n <= 65536:
+            raise ValueError("src must name 1 to 65536 requests")
+        for t, what in ((src, "src"), (dst, "dst"), (tokens, "tokens")):
+            if t is not None:
+                self._ints(t, (n,), what)
+        if edit is not None and edit.max_moves != n:
+            raise ValueError(f"edit is for {edit.max_moves} moves, not {n}")
+        return self._edit("fork", edit, n, src.data_ptr(), dst.data_ptr(), None if tokens is None else tokens.data_ptr(), n)
+
+    def trim(self, keep, edit=None):
+        """Plan that request i keeps its first keep[i] tokens (int32 [R]; 0 ends it,
+        a negative number or one not below its length keeps all).  Pages without an
+        owner are free after the commit.  A request that would end inside a page
+        with other owners stays as it is and counts as refused.  No pages to copy."""
+        self._ints(keep, (self.cfg.requests,), "keep")
+        return self._edit("trim", edit, 1, keep.data_ptr())
+
+    def compact(self, edit=None):
+        """Plan that the held pages go to the pool's lower end: afterwards the free
+        ones are its last, in ascending order.  The pages that move have to be
+        copied in every layer (KvCache.copy).  edit: one of max_moves
+        max(1, pages // 2) to write again."""
+        moves = max(1, self.cfg.pages // 2)
+        if edit is not None and edit.max_moves != moves:
+            raise ValueError(f"edit is for {edit.max_moves} moves, not {moves}")
+        return self._edit("compact", edit, moves)
+
+    def _commit_edit(self, edit):
+        self._fits(edit, "edit")
+        if edit._by is not self or edit._when != self._changes:
+            raise ValueError("the tables have changed since the edit was planned, or it is not theirs")
+        L.check("agft_pages_commit", self._lib.agft_pages_commit(self._cfg, self.ptr, self.nbytes, edit.ptr, edit.nbytes,
+                                                                 edit.max_moves, self._s()))
+        self._changes += 1
+        self._edits += 1
 
 
 class KvCache(_OnStream):
@@ -363,6 +478,13 @@ class KvCache(_OnStream):
         if code != L.AGFT_OK:
             L.check("agft_kv_attend", code)
         return out
+
+    def copy(self, edit):
+        """Copy the pages that a planned edit moves or fills."""
+        self._fits(edit, "edit")
+        code = self._lib.agft_pages_copy(self._cfg, self.ptr, self.nbytes, edit.ptr, edit.nbytes, edit.max_moves, self._s())
+        if code != L.AGFT_OK:
+            L.check("agft_pages_copy", code)
 
     def export(self, slots, dtype=torch.bfloat16):
         """Keys and values of the slots [n] (int64; -1 gives zeros) as two
