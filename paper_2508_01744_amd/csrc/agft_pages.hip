@@ -351,7 +351,8 @@ __device__ __forceinline__ void trim_chunk(const EditArgs &p, bool extra, TrimLd
         }
         const int32_t first = pages_of(p, to), gone = pages_of(p, past) - first, end = up_to(gone);
         lds.past[lane] = past, lds.to[lane] = to, lds.first[lane] = first, lds.at[lane + 1] = end;
-        if (lane == 0) lds.at[0] = 0, lds.refused = __popcll(__ballot(refused));
+        const int32_t all_refused = __popcll(__ballot(refused));
+        if (lane == 0) lds.at[0] = 0, lds.refused = all_refused;
     }
     __syncthreads();
 }

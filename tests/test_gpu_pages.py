@@ -161,6 +161,18 @@ def test_many_forks_at_once(n):
     both.window([5] * (n + 1))
 
 
+@pytest.mark.parametrize("requests", [6, 1500, 4000])
+def test_refused_trims_are_counted(requests):
+    """One in three requests would end inside a page that others hold, wherever it stands among the requests."""
+    both = Both(requests, 2, 2 * requests, 16, seed=requests)
+    third = requests // 3
+    both.window([17] * third + [0] * (requests - third))
+    both.edit("fork", list(range(third)) * 2, list(range(third, 3 * third)), None)
+    want = both.edit("trim", [int(x) for x in both.rng.choice([-1, 0, 5, 16], requests)])
+    assert want["counters"][3] > requests // 8 or requests < 9
+    both.same_tokens()
+
+
 def test_long_rows():
     """Rows of more entries than one workgroup copies or lets go at a time; pages go back by their last owner."""
     tables, cache, node = make(6, 2600, 6000)
