@@ -10,7 +10,7 @@ CSRC = os.path.join(PKG, "csrc")
 INCLUDE = os.path.join(ROOT, "include")
 LIB = os.path.join(PKG, "libagft.so")
 SOURCES = [os.path.join(CSRC, name) for name in ("agft_step.hip", "agft_env.hip", "agft_kv.hip", "agft_kv_attend.hip",
-                                               "agft_pages.hip")]
+                                               "agft_pages.hip", "agft_diff.hip")]
 
 HIPCC_FLAGS = [
     "--offload-arch=gfx950", "-O3", "-std=c++17", "-fPIC", "-shared",

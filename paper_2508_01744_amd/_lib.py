@@ -1,9 +1,8 @@
 """ctypes binding of libagft.so: argument marshalling only.
 
-The names mirror include/agft.h, include/agft_sim.h, include/agft_kv.h and
-include/agft_pages.h.  Loading fails loudly
-when the library has not been built: there is no other implementation to
-fall back to.
+The names mirror include/agft.h, include/agft_sim.h, include/agft_kv.h,
+include/agft_pages.h and include/agft_diff.h.  Loading fails loudly when the
+library has not been built: there is no other implementation to fall back to.
 """
 import ctypes
 import os
@@ -78,6 +77,11 @@ class agft_pages_view(ctypes.Structure):
     _fields_ = [("counters", _vp), ("lengths", _vp), ("granted", _vp), ("moves", _vp)]
 
 
+class agft_diff_args(ctypes.Structure):
+    _fields_ = [("lambda_", _vp), ("lambda_token", _i64), ("lambda_head", _i64), ("weight", _vp), ("eps", _f32),
+                ("gain", _f32)]
+
+
 AGFT_KV_E4M3, AGFT_KV_INT8 = 0, 1
 AGFT_KV_BF16, AGFT_KV_FP16, AGFT_KV_FP32 = 0, 1, 2
 
@@ -95,6 +99,9 @@ KV_EXPORTED = ["agft_kv_tables_bytes", "agft_kv_step_bytes", "agft_kv_cache_byte
 # of agft_pages.h
 PAGES_EXPORTED = ["agft_pages_edit_bytes", "agft_pages_edit_at", "agft_pages_owners_at", "agft_pages_fork",
                   "agft_pages_trim", "agft_pages_compact", "agft_pages_copy", "agft_pages_commit"]
+
+# of agft_diff.h
+DIFF_EXPORTED = ["agft_diff_attend_bytes", "agft_diff_attend"]
 
 _lib = None
 
@@ -164,6 +171,11 @@ def _declare(lib):
             ("commit", ctypes.c_int, [_vp, _sz, *edit, _vp])):
         fn = getattr(lib, "agft_pages_" + name)
         fn.restype, fn.argtypes = restype, [kvp, *args]
+    lib.agft_diff_attend_bytes.restype = _sz
+    lib.agft_diff_attend_bytes.argtypes = [kvp, _i32]
+    lib.agft_diff_attend.restype = ctypes.c_int
+    lib.agft_diff_attend.argtypes = [kvp, _vp, _sz, _vp, _sz, _vp, _sz, _i32, _i32, densep, ctypes.POINTER(agft_diff_args),
+                                     densep, _vp, _f32, _vp, _sz, _vp]
     return lib
 
 

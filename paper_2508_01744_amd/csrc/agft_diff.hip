@@ -1,0 +1,961 @@
+// agft_diff.hip -- differential attention over a serving node's 8-bit paged cache.
+// agft_diff.h states the rules, agft_kv.h the cache's.
+
+#include <hip/hip_runtime.h>
+
+#include <cmath>
+#include <cstdint>
+#include <type_traits>
+
+#include "agft_diff.h"
+#include "agft_kv_attend.h"
+
+namespace agft_diff_detail {
+
+using namespace agft_kv_detail;
+
+// (heads: the pairs, which the work is cut by)
+struct DiffArgs : AttendArgs {
+    const float *lambda, *weight;
+    int64_t lambda_token, lambda_head;
+    float eps, gain;
+};
+
+constexpr int kManyPieces = 32;            // more are joined in groups first
+constexpr int kFewShare = 4;               // units that a workgroup takes at least
+constexpr int kFewEven = 8;                // units up to which rows are cut evenly
+constexpr int kRaise = 15;
+
+// Two halves of a value row meet the same probabilities, and each page has a scale
+// for either.  The larger one, 2^e, goes into the probabilities' exponent as the
+// one scale of agft_kv_attend does; a half's codes come to fp16 times 2^(ev - e +
+// lift), lift being what fp16's range leaves above the largest code.
+template <int FORM>
+constexpr int lift() {
+    return FORM == AGFT_KV_E4M3 ? 7 : 5;   // 448 * 2^7; 1152 * 2^5 (the integers' offset below)
+}
+
+// Eight codes, the first four times 2^a and the others times 2^b, as fp16.
+template <int FORM>
+__device__ __forceinline__ fp16x8 decode_scaled(uint32_t lo, uint32_t hi, float a, float b) {
+    uint32_t w[4];
+    if constexpr (FORM == AGFT_KV_E4M3) {
+        w[0] = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_f16_fp8(lo, a, false));
+        w[1] = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_f16_fp8(lo, a, true));
+        w[2] = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_f16_fp8(hi, b, false));
+        w[3] = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_f16_fp8(hi, b, true));
+    } else {
+        // c + 128 as the low byte of 1024 + (c + 128), less 1152, in one fused step with the scale
+        lo ^= 0x80808080u, hi ^= 0x80808080u;
+        w[0] = __builtin_amdgcn_perm(0x64646464u, lo, 0x04010400u);
+        w[1] = __builtin_amdgcn_perm(0x64646464u, lo, 0x04030402u);
+        w[2] = __builtin_amdgcn_perm(0x64646464u, hi, 0x04010400u);
+        w[3] = __builtin_amdgcn_perm(0x64646464u, hi, 0x04030402u);
+        const fp16x2 f[2] = {{(_Float16)a, (_Float16)a}, {(_Float16)b, (_Float16)b}};
+        const fp16x2 base = {(_Float16)-1152.0f, (_Float16)-1152.0f};
+#pragma unroll
+        for (int j = 0; j < 4; ++j)
+            w[j] = __builtin_bit_cast(uint32_t, __builtin_elementwise_fma(__builtin_bit_cast(fp16x2, w[j]), f[j >> 1],
+                                                                          base * f[j >> 1]));
+    }
+    return __builtin_bit_cast(fp16x8, (uint4v){w[0], w[1], w[2], w[3]});
+}
+
+// 2^(ev - e + lift), e the larger of a page's two value exponents
+template <int FORM>
+__device__ __forceinline__ float value_scale(int ev, int e) {
+    const int k = ev - e + lift<FORM>();
+    return pow2(k < -126 ? -126 : k);
+}
+
+// gain weight / sqrt(mean(y^2) + eps) without the weight, of a row of WIDE numbers
+template <int WIDE>
+__device__ __forceinline__ float row_factor(const DiffArgs &p, float squares) {
+    return p.weight == nullptr ? p.gain : p.gain / sqrtf(squares * (1.0f / WIDE) + p.eps);
+}
+__device__ __forceinline__ float4v weight_at(const DiffArgs &p, int d) {
+    return p.weight == nullptr ? (float4v){1, 1, 1, 1} : *reinterpret_cast<const float4v *>(p.weight + d);
+}
+__device__ __forceinline__ float square4(float4v y) { return (y[0] * y[0] + y[1] * y[1]) + (y[2] * y[2] + y[3] * y[3]); }
+
+// a f - b, the product rounded as the other map's was: equal maps leave zero
+__device__ __forceinline__ float4v less(float4v a, float f, float4v b) {
+#pragma clang fp contract(off)
+    a *= f;
+    return a - b;
+}
+
+template <int TYPE>
+__device__ __forceinline__ void store4(const DiffArgs &p, int first, int pair, int r, int d, float4v o) {
+    const int t = first + r / p.group, h = pair * p.group + r % p.group;
+    uint2 *dst = reinterpret_cast<uint2 *>(p.out + (t * p.out_token + h * p.out_head + d) * 2);
+    *dst = Half<TYPE>::pack4(o[0], o[1], o[2], o[3]);
+}
+
+__device__ __forceinline__ void store_lse(const DiffArgs &p, int first, int pair, int map, int r, float m, float l) {
+    if (p.lse == nullptr) return;
+    const int t = first + r / p.group, hq = (2 * pair + map) * p.group + r % p.group;
+    p.lse[(int64_t)t * p.heads * 2 * p.group + hq] = m == -INFINITY ? -INFINITY : (m + __log2f(l)) * kLn2;
+}
+
+__device__ __forceinline__ float lambda_of(const DiffArgs &p, int first, int pair, int r) {
+    return p.lambda[(first + r / p.group) * p.lambda_token + (pair * p.group + r % p.group) * p.lambda_head];
+}
+
+// Rows that no map has keys for: x in out, `lse` in d_lse.
+template <int TYPE, int WIDE>
+__device__ __forceinline__ void fill_rows(const DiffArgs &p, int first, int pair, int row0, int rows, float x, float lse) {
+    for (int c = threadIdx.x; c < rows * (WIDE / 4); c += blockDim.x) {
+        const int r = c / (WIDE / 4), d = c % (WIDE / 4) * 4;
+        store4<TYPE>(p, first, pair, row0 + r, d, (float4v){x, x, x, x});
+        if (d == 0) store_lse(p, first, pair, 0, row0 + r, lse, 1.0f), store_lse(p, first, pair, 1, row0 + r, lse, 1.0f);
+    }
+}
+
+// ---- few query rows ----
+//
+// The work is cut as agft_kv_attend cuts it, a pair of heads in the place of a head:
+// units of 64 tokens of one request, for one pair's 16 query rows (tokens x group).
+// Of a workgroup's four wavefronts two take the first map and two the second, each
+// half of the tokens: a wavefront reads its own map's keys and both heads' values,
+// which the other map's wavefront beside it reads at the same time (from the L1).
+// Every wavefront keeps its map's maximum, sum and 16 rows of 2 dim sums; the two
+// of a map join in LDS, pieces of several workgroups through memory, and the
+// difference and its norm are made once, where everything has met.
+template <int DIM>
+constexpr int few_groups() {
+    return DIM == 64 ? 768 : 512;
+}
+
+template <int DIM>
+struct FewLds {
+    static constexpr int C = DIM / 8;              // blocks of 16 numbers of a value row
+    float4v o[2][C * 64];                          // a map's sums, as the lanes hold them
+    float m[2][kRowTile], l[2][kRowTile], squares[2][kRowTile];
+    EvenLds even;
+    int last;
+};
+
+// A piece: both maps' sums as the lanes hold them, their maxima, their sums of probabilities.
+template <int DIM>
+constexpr int piece_floats() {
+    return 2 * (FewLds<DIM>::C * 256 + 2 * kRowTile);
+}
+
+// The rows' results, from both maps' sums: NC blocks of 16 numbers from block c0 on
+// of one map in a wavefront that is busy.  All wavefronts come here.
+template <int FORM, int TYPE, int DIM, int NC>
+__device__ __forceinline__ void finish_rows(const DiffArgs &p, const Segment &seg, FewLds<DIM> &lds, bool busy, int map,
+                                            int c0, float4v *o, float m, float l) {
+    const int lane = threadIdx.x & 63, n = lane & 15, g = lane >> 4;
+    const int row = seg.row + (n < seg.rows ? n : 0);
+    float f = l > 0.0f || l != l ? pow2(-kRaise - lift<FORM>()) / l : 0.0f;
+    if (busy && map == 1) {
+        f *= lambda_of(p, seg.first, seg.head, row);
+#pragma unroll
+        for (int c = 0; c < NC; ++c) lds.o[1][(c0 + c) * 64 + lane] = o[c] * f;
+    }
+    if (busy && c0 == 0 && g == 0 && n < seg.rows) store_lse(p, seg.first, seg.head, map, row, m, l);
+    __syncthreads();
+    if (busy && map == 0) {
+        float squares = 0.0f;
+#pragma unroll
+        for (int c = 0; c < NC; ++c) {
+            o[c] = less(o[c], f, lds.o[1][(c0 + c) * 64 + lane]);
+            squares += square4(o[c]);
+        }
+        squares = across_sum(squares);
+        if (g == 0) lds.squares[c0 > 0][n] = squares;
+    }
+    __syncthreads();
+    if (busy && map == 0 && n < seg.rows) {
+        float squares = lds.squares[0][n];
+        if constexpr (NC < FewLds<DIM>::C) squares += lds.squares[1][n];
+        const float by = row_factor<2 * DIM>(p, squares);
+#pragma unroll
+        for (int c = 0; c < NC; ++c) {
+            const int d = (c0 + c) * 16 + 4 * g;
+            store4<TYPE>(p, seg.first, seg.head, row, d, o[c] * by * weight_at(p, d));
+        }
+    }
+}
+
+// Joins the pieces of the same 16 rows.  A wavefront takes half of the numbers of
+// one map.  into: where the joined piece goes, or NULL: it is the rows' result.
+template <int FORM, int TYPE, int DIM, typename F>
+__device__ __forceinline__ void join_pieces(const DiffArgs &p, F piece, int pieces, float *into, const Segment &seg,
+                                            FewLds<DIM> &lds) {
+    constexpr int C = FewLds<DIM>::C, HALF = C / 2, MAP = C * 256;
+    constexpr int AHEAD = DIM == 64 ? 1 : 2;   // pieces on their way at once
+    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    const int map = wave >> 1, half = wave & 1, n = lane & 15, g = lane >> 4;
+    const int maxima = 2 * MAP + map * kRowTile + n, at = map * MAP + half * HALF * 256 + lane * 4;
+    float m = -INFINITY, l = 0.0f;
+#pragma unroll 1
+    for (int w0 = 0; w0 < pieces; w0 += 8) {
+        float x[8];
+#pragma unroll
+        for (int z = 0; z < 8; ++z) x[z] = get(piece(w0 + z < pieces ? w0 + z : w0) + maxima);
+#pragma unroll
+        for (int z = 0; z < 8; ++z) m = fmaxf(m, x[z]);
+    }
+    float4v o[HALF];
+#pragma unroll
+    for (int c = 0; c < HALF; ++c) o[c] = (float4v){0, 0, 0, 0};
+#pragma unroll 1
+    for (int w0 = 0; w0 < pieces; w0 += AHEAD) {
+        float mw[AHEAD], lw[AHEAD];
+        float2 a[AHEAD][HALF], b[AHEAD][HALF];
+#pragma unroll
+        for (int z = 0; z < AHEAD; ++z) {
+            const float *src = piece(w0 + z < pieces ? w0 + z : w0);
+            mw[z] = get(src + maxima), lw[z] = get(src + maxima + 2 * kRowTile);
+#pragma unroll
+            for (int c = 0; c < HALF; ++c) a[z][c] = get2(src + at + c * 256), b[z][c] = get2(src + at + c * 256 + 2);
+        }
+#pragma unroll
+        for (int z = 0; z < AHEAD; ++z)
+            if (w0 + z < pieces) {
+                const float f = mw[z] == -INFINITY ? 0.0f : exp2f(mw[z] - m);
+                l = fmaf(lw[z], f, l);
+#pragma unroll
+                for (int c = 0; c < HALF; ++c) o[c] += (float4v){a[z][c].x, a[z][c].y, b[z][c].x, b[z][c].y} * f;
+            }
+    }
+    if (into == nullptr) {
+        finish_rows<FORM, TYPE, DIM, HALF>(p, seg, lds, true, map, half * HALF, o, m, l);
+        return;
+    }
+    // (into is the first of the pieces, which the other lanes of this wavefront have read too; the
+    // other wavefronts read other numbers of it, and the maxima only up to here)
+    __syncthreads();
+#pragma unroll
+    for (int c = 0; c < HALF; ++c) {
+        put2(into + at + c * 256, o[c][0], o[c][1]);
+        put2(into + at + c * 256 + 2, o[c][2], o[c][3]);
+    }
+    if (g == 0 && half == 0) put(into + maxima, m), put(into + maxima + 2 * kRowTile, l);
+}
+
+// Rows of tiles that no launch makes, because a request brings more tokens than
+// the caller's bound: NaN, not what the memory held.
+template <int TYPE, int WIDE>
+__device__ __forceinline__ void leave_nan(const DiffArgs &p, int items) {
+    const int64_t all = (int64_t)items * p.heads;
+    for (int64_t x = blockIdx.x; x < all; x += gridDim.x) {
+        const Item item = p.items[x / p.heads];
+        if (item.part > 0) continue;
+        const int pair = (int)(x % p.heads), first = p.works[item.request].start, row0 = item.tile * kTileRows;
+        int rows = (p.works[item.request + 1].start - first) * p.group - row0;
+        if (rows > kTileRows) rows = kTileRows;
+        fill_rows<TYPE, WIDE>(p, first, pair, row0, rows, NAN, NAN);
+    }
+}
+
+// BESIDE: in a launch that makes the tiles of many rows too
+template <int FORM, int TYPE, int DIM, bool BESIDE>
+__device__ __forceinline__ void attend_few(const DiffArgs &p, FewLds<DIM> &lds, int block) {
+    constexpr int DG = DIM / kBlockDims, C = FewLds<DIM>::C;
+    constexpr int BLK = 2;                        // blocks of 16 tokens at a time
+    using H = Half<TYPE>;
+    using F = Half<AGFT_KV_FP16>;
+    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    const int g = lane >> 4, n = lane & 15, part = wave & 1, map = wave >> 1;
+    Works works(p.works, p.requests);
+    if constexpr (!BESIDE)
+        if (__builtin_expect(p.alone && works.total.y > 0, 0)) leave_nan<TYPE, 2 * DIM>(p, works.total.y);
+    const int32_t work = works.total.x * p.heads;
+    int32_t share = (work + few_groups<DIM>() - 1) / few_groups<DIM>();
+    if (share < kFewShare) share = kFewShare;
+    int64_t x_first = (int64_t)block * share;
+    int32_t x1 = x_first + share < work ? (int32_t)x_first + share : work;
+    Piece cut;
+    bool even = false;
+    if (share <= kFewEven) {
+        if (works.n <= 64)
+            even = piece_of(p, works, share, few_groups<DIM>(), block, &cut) ||
+                   piece_of(p, works, share + 2, few_groups<DIM>(), block, &cut);
+        else if (works.n <= kEvenRequests)
+            even = piece_of(p, works, share, few_groups<DIM>(), block, lds.even, &cut);
+    }
+    if (even) x_first = cut.first, x1 = cut.last;
+    if (x_first >= x1) return;
+    const int64_t side = (int64_t)p.page * DIM, page_bytes = (int64_t)p.heads * 4 * side;
+    const float scale2 = p.scale * kLog2e;
+    int32_t x = (int32_t)x_first;
+    if (even) works.look_at(cut.request);
+    else works.look(x / p.heads);
+    while (x < x1) {
+        const Segment seg = segment_of(p, works, x);
+        if (seg.units <= 0) break;
+        const int i = seg.request, pair = seg.head, units = seg.units, u0 = seg.at, row0 = seg.row, rows = seg.rows;
+        const int first = seg.first;
+        const int count = units - u0 < x1 - x ? units - u0 : x1 - x;
+        x += count;
+        const int granted = seg.granted, len = seg.length;
+        if (granted <= 0) {
+            // no slots, no keys
+            fill_rows<TYPE, 2 * DIM>(p, first, pair, row0, rows, 0.0f, -INFINITY);
+            continue;
+        }
+        // right operand of the scores: row n's numbers 64 dg + 16 g + 8 e.. + 7
+        typename H::x8 q[DG * 2];
+        const bool row_here = n < rows;
+        {
+            const int tk = (row0 + n) / p.group, hq = (2 * pair + map) * p.group + (row0 + n) % p.group;
+            const char *src = p.q + ((int64_t)(first + tk) * p.q_token + hq * p.q_head) * 2;
+#pragma unroll
+            for (int c = 0; c < DG * 2; ++c) {
+                uint4v v = {0, 0, 0, 0};
+                if (row_here) v = *reinterpret_cast<const uint4v *>(src + ((c >> 1) * kBlockDims + 16 * g + 8 * (c & 1)) * 2);
+                q[c] = __builtin_bit_cast(typename H::x8, v);
+            }
+        }
+        int limit = row_here ? len - granted + (row0 + n) / p.group + 1 : len;   // keys that row n sees
+        int least = len - granted + row0 / p.group + 1;                          // keys that every row sees
+        const int blocks = (len + kBlockTokens - 1) / kBlockTokens;
+        const char *codes = p.codes + (int64_t)pair * 4 * side;
+        const int sub_mask = (p.page >> 4) - 1;
+
+        float m = -INFINITY, l = 0.0f;
+        float4v o[C];
+#pragma unroll
+        for (int c = 0; c < C; ++c) o[c] = (float4v){0, 0, 0, 0};
+
+        // this wavefront's blocks of the segment: a half, two of each unit
+        static_assert(kUnit == 4 * kBlockTokens, "a unit gives either half two blocks");
+        const int b_first = u0 * 4 + 2 * count * part;
+        const int b_last = b_first + 2 * count < blocks ? b_first + 2 * count : blocks;
+        limit = limit < b_last * kBlockTokens ? limit : b_last * kBlockTokens;
+        least = least < b_last * kBlockTokens ? least : b_last * kBlockTokens;
+        for (int b0 = b_first; b0 < b_last; b0 += 64) {
+            // a lane per block: its page, this map's keys' exponent, the values' larger one and
+            // what either head's codes are taken by
+            int id, ek, ev;
+            float up[2];
+            {
+                int b = b0 + lane;
+                if (b >= blocks) b = blocks - 1;
+                uint32_t z = (uint32_t)p.table[(int64_t)i * p.row_pages + ((b << 4) >> p.shift)];
+                if (z >= (uint32_t)p.pages) z = (uint32_t)p.pages - 1;
+                id = (int)z;
+                const int4 e = *reinterpret_cast<const int4 *>(p.exps + ((int64_t)id * p.heads + pair) * 4);
+                ek = map == 0 ? e.x : e.z;
+                ev = e.y > e.w ? e.y : e.w;
+                up[0] = value_scale<FORM>(e.y, ev), up[1] = value_scale<FORM>(e.w, ev);
+            }
+            const int b1 = b0 + 64 < b_last ? b0 + 64 : b_last;
+            const auto block_at = [&](int b) {
+                const int bb = b >= b_last ? b_last - 1 : b;
+                return codes + (int64_t)__builtin_amdgcn_readlane(id, bb - b0) * page_bytes + (bb & sub_mask) * (16 * DIM) + lane * 16;
+            };
+            const auto fetch_keys = [&](int b, uint4v (*dst)[DG]) {
+#pragma unroll
+                for (int s = 0; s < BLK; ++s) {
+                    const char *src = block_at(b + s) + map * 2 * side;
+#pragma unroll
+                    for (int dg = 0; dg < DG; ++dg) dst[s][dg] = *reinterpret_cast<const uint4v *>(src + dg * kBlockBytes);
+                }
+            };
+            const auto fetch_values = [&](int b, uint4v (*dst)[2 * DG]) {
+#pragma unroll
+                for (int s = 0; s < BLK; ++s) {
+                    const char *src = block_at(b + s) + side;
+#pragma unroll
+                    for (int dg = 0; dg < 2 * DG; ++dg)
+                        dst[s][dg] = *reinterpret_cast<const uint4v *>(src + (dg / DG) * 2 * side + (dg % DG) * kBlockBytes);
+                }
+            };
+            // codes are asked for as soon as their registers are free: the next
+            // keys after the scores, the next values after the sums
+            uint4v kc[BLK][DG], vc[BLK][2 * DG];
+            fetch_keys(b0, kc);
+            fetch_values(b0, vc);
+            for (int b = b0; b < b1; b += BLK) {
+                float4v t[BLK];
+                float back[BLK], by[BLK][2];
+#pragma unroll
+                for (int s = 0; s < BLK; ++s) {
+                    float4v acc = {0, 0, 0, 0};
+#pragma unroll
+                    for (int dg = 0; dg < DG; ++dg) {
+                        acc = H::mfma(H::template decode<FORM>(kc[s][dg][0], kc[s][dg][1]), q[2 * dg], acc);
+                        acc = H::mfma(H::template decode<FORM>(kc[s][dg][2], kc[s][dg][3]), q[2 * dg + 1], acc);
+                    }
+                    int bb = b + s;
+                    if (bb >= b_last) bb = b_last - 1;
+                    const int bek = __builtin_amdgcn_readlane(ek, bb - b0), bev = __builtin_amdgcn_readlane(ev, bb - b0);
+                    by[s][0] = __uint_as_float(__builtin_amdgcn_readlane(__float_as_uint(up[0]), bb - b0));
+                    by[s][1] = __uint_as_float(__builtin_amdgcn_readlane(__float_as_uint(up[1]), bb - b0));
+                    const float ks = scale2 * pow2(bek);
+                    back[s] = pow2(-bev);
+#pragma unroll
+                    for (int j = 0; j < 4; ++j) t[s][j] = fmaf(acc[j], ks, (float)bev);
+                }
+                if (b + BLK < b1) fetch_keys(b + BLK, kc);
+                if ((b + BLK) * kBlockTokens > least) {
+#pragma unroll
+                    for (int s = 0; s < BLK; ++s) {
+                        const int key = (b + s) * kBlockTokens + 4 * g;
+#pragma unroll
+                        for (int j = 0; j < 4; ++j)
+                            if (key + j >= limit) t[s][j] = -INFINITY;
+                        // codes past the request's tokens may be anything, NaN too
+                        const int valid = len - key;
+                        const uint32_t keep = valid >= 4 ? ~0u : valid <= 0 ? 0u : (1u << (8 * valid)) - 1u;
+#pragma unroll
+                        for (int dg = 0; dg < 2 * DG; ++dg) vc[s][dg] &= keep;
+                    }
+                }
+                float top = t[0][0];
+#pragma unroll
+                for (int s = 0; s < BLK; ++s)
+#pragma unroll
+                    for (int j = 0; j < 4; ++j) top = fmaxf(top, t[s][j]);
+                top = across_max(top);
+                if (__any(top > m)) {
+                    const float m1 = fmaxf(m, top);
+                    float fall = m == -INFINITY ? 0.0f : exp2f(m - m1);
+                    m = m1;
+                    asm volatile("" : "+v"(fall));
+                    l *= fall;
+#pragma unroll
+                    for (int c = 0; c < C; ++c) o[c] *= fall;
+                }
+                const float off = m == -INFINITY ? 0.0f : m;
+                fp16x4 pr[BLK];
+#pragma unroll
+                for (int s = 0; s < BLK; ++s) {
+                    float4v e;
+#pragma unroll
+                    for (int j = 0; j < 4; ++j) e[j] = __builtin_amdgcn_exp2f(t[s][j] - off);
+                    l = fmaf((e[0] + e[1]) + (e[2] + e[3]), back[s], l);
+#pragma unroll
+                    for (int j = 0; j < 4; ++j) pr[s][j] = (_Float16)(e[j] * pow2(kRaise));
+                }
+                const fp16x8 pp = __builtin_shufflevector(pr[0], pr[1], 0, 1, 2, 3, 4, 5, 6, 7);
+#pragma unroll
+                for (int c = 0; c < C; ++c)
+                    o[c] = F::mfma(decode_scaled<FORM>(vc[0][c >> 2][c & 3], vc[1][c >> 2][c & 3], by[0][c / (C / 2)],
+                                                       by[1][c / (C / 2)]), pp, o[c]);
+                if (b + BLK < b1) fetch_values(b + BLK, vc);
+            }
+        }
+        l = across_sum(l);
+        // the two wavefronts of a map meet
+        if (part == 1) {
+#pragma unroll
+            for (int c = 0; c < C; ++c) lds.o[map][c * 64 + lane] = o[c];
+            if (g == 0) lds.m[map][n] = m, lds.l[map][n] = l;
+        }
+        __syncthreads();
+        if (part == 0) {
+            const float m1 = lds.m[map][n], both = fmaxf(m, m1);
+            const float f0 = m == -INFINITY ? 0.0f : exp2f(m - both), f1 = m1 == -INFINITY ? 0.0f : exp2f(m1 - both);
+            l = fmaf(l, f0, lds.l[map][n] * f1);
+            m = both;
+#pragma unroll
+            for (int c = 0; c < C; ++c) o[c] = o[c] * f0 + lds.o[map][c * 64 + lane] * f1;
+        }
+        if (count == units) {
+            finish_rows<FORM, TYPE, DIM, C>(p, seg, lds, part == 0, map, 0, o, m, l);
+        } else {
+            const int32_t from = x - count - u0;                       // the rows' first unit
+            const int owner = even ? cut.owner : from / share;
+            const int pieces = even ? cut.pieces : (from + units - 1) / share - owner + 1;
+            if (part == 0) {
+                float *at = p.partial + ((int64_t)block * 2 + (u0 == 0 ? 1 : 0)) * piece_floats<DIM>();
+#pragma unroll
+                for (int c = 0; c < C; ++c) {
+                    put2(at + (map * C + c) * 256 + lane * 4, o[c][0], o[c][1]);
+                    put2(at + (map * C + c) * 256 + lane * 4 + 2, o[c][2], o[c][3]);
+                }
+                at += 2 * C * 256 + map * kRowTile + n;
+                if (g == 0) put(at, m), put(at + 2 * kRowTile, l);
+            }
+            // groups of kManyPieces first, each into its first piece's place
+            const int mine = block - owner, group0 = mine / kManyPieces * kManyPieces;
+            const int members = pieces - group0 < kManyPieces ? pieces - group0 : kManyPieces;
+            const int groups = (pieces + kManyPieces - 1) / kManyPieces;
+            // the first piece of the rows is its workgroup's second one
+            const auto piece = [&](int w) {
+                return p.partial + ((int64_t)(owner + w) * 2 + (w == 0 ? 1 : 0)) * piece_floats<DIM>();
+            };
+            int32_t *counter = p.arrived + kFewGroups + (owner + group0) * 2 + (group0 == 0 ? 1 : 0);
+            if (last_to_arrive(counter, members, &lds.last)) {
+                float *into = groups == 1 ? nullptr : piece(group0);
+                join_pieces<FORM, TYPE, DIM>(p, [&](int w) { return piece(group0 + w); }, members, into, seg, lds);
+                if (groups > 1 && last_to_arrive(p.arrived + owner, groups, &lds.last))
+                    join_pieces<FORM, TYPE, DIM>(p, [&](int w) { return piece(kManyPieces * w); }, groups, nullptr, seg, lds);
+            }
+        }
+        __syncthreads();
+    }
+}
+
+// ---- many query rows ----
+//
+// A tile of agft_kv_attend's plan, 128 query rows of one request, is two workgroups
+// here, of 64 rows each: two wavefronts take 32 rows' first map and two their second,
+// over the tokens 64 at a time.  Each wavefront fetches one block of 16 tokens, keys
+// and values of both heads, and leaves them in LDS as 16 bits; a wavefront reads its
+// map's keys there and all values.  The second map's sums go to the first's
+// wavefronts through LDS at the end.
+constexpr int kTileWaves = 4;
+constexpr int kTileKeys = 64;
+constexpr int kSubRows = 64;               // rows of a workgroup
+// Powers of two that a maximum may grow before the sums are rescaled; the
+// exponential itself makes 2^kTileRaise P, as in agft_kv_attend.
+constexpr int kSlack = 8;
+constexpr int kTileRaise = kRaise - kSlack;
+
+template <int DIM>
+struct TileLds {
+    static constexpr int HEAD = kTileKeys * DIM * 2;       // a head's keys (or values) of a tile in 16 bits
+    // operands of 1 KB, 16 bytes a lane; keys: [head][32 tokens][64 numbers][32][16], values: [16 tokens][32 numbers]
+    __attribute__((aligned(16))) char tile[2][2][2 * HEAD];
+    float4 scale[4][2][4];                                 // by tile % 4, map: a block's factor of the scores, e, 2^-e
+    int last;
+};
+
+template <int FORM, int TYPE, int DIM>
+__device__ __forceinline__ void attend_many(const DiffArgs &p, TileLds<DIM> &lds, int block) {
+    constexpr int DG = DIM / kBlockDims, WIDE = 2 * DIM;
+    using H = Half<TYPE>;
+    const auto s_tile = lds.tile;
+    const auto s_scale = lds.scale;
+    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    const int h = lane >> 5, n = lane & 31, map = wave >> 1;
+    const int pair = block % p.heads, sub = block / p.heads & 1, place = block / p.heads >> 1;
+    if (place >= p.works[p.requests].items) return;
+    const Item item = p.items[place];
+    const int i = item.request;
+    const int4 own = *reinterpret_cast<const int4 *>(p.works + i);
+    const int len = p.works[i].length;
+    const int first = own.z, granted = own.w, all_rows = (p.works[i + 1].start - first) * p.group;
+    const int row0 = item.tile * kTileRows + sub * kSubRows;
+    const int rows = all_rows - row0 < kSubRows ? all_rows - row0 : kSubRows;
+    if (rows <= 0) return;
+    if (granted <= 0) {
+        if (item.part == 0) fill_rows<TYPE, WIDE>(p, first, pair, row0, rows, 0.0f, -INFINITY);
+        return;
+    }
+    const int past = len - granted, at_row = 32 * (wave & 1);
+    const bool busy = at_row < rows, row_here = at_row + n < rows;
+    const int row = row_here ? row0 + at_row + n : row0 + rows - 1;
+    const int limit = past + row / p.group + 1;            // keys that this lane's row sees
+    const int all_tiles = (past + (row0 + rows - 1) / p.group + kTileKeys) / kTileKeys;
+    const int begin = (int)((int64_t)all_tiles * item.part / item.parts);   // this part's tiles
+    const int tiles = (int)((int64_t)all_tiles * (item.part + 1) / item.parts);
+    int whole = (past + row0 / p.group + 1) / kTileKeys;                    // tiles that every row sees whole
+    if (whole > tiles) whole = tiles;
+    const int blocks = (len + kBlockTokens - 1) / kBlockTokens;
+
+    typename H::x8 q[DG * 4];
+    {
+        const int tk = row / p.group, hq = (2 * pair + map) * p.group + row % p.group;
+        const char *src = p.q + ((int64_t)(first + tk) * p.q_token + hq * p.q_head) * 2;
+#pragma unroll
+        for (int c = 0; c < DG * 4; ++c)                   // numbers 64 dg + 16 (2 c + h) + 8 e.. + 7
+            q[c] = __builtin_bit_cast(typename H::x8, *reinterpret_cast<const uint4v *>(
+                       src + ((c >> 2) * kBlockDims + 16 * (2 * ((c >> 1) & 1) + h) + 8 * (c & 1)) * 2));
+    }
+    const float scale2 = p.scale * kLog2e;
+    const int64_t side = (int64_t)p.page * DIM, page_bytes = (int64_t)p.heads * 4 * side;
+    const char *codes = p.codes + (int64_t)pair * 4 * side;
+    const int sub_mask = (p.page >> 4) - 1;
+
+    // a lane per tile: the page and exponents of this wavefront's block of it
+    int id = 0;
+    int4 ee = make_int4(0, 0, 0, 0);
+    const auto look_up = [&](int t0) {
+        int b = (t0 + lane) * 4 + wave;
+        if (b >= blocks) b = blocks - 1;
+        uint32_t z = (uint32_t)p.table[(int64_t)i * p.row_pages + ((b << 4) >> p.shift)];
+        if (z >= (uint32_t)p.pages) z = (uint32_t)p.pages - 1;
+        id = (int)z;
+        ee = *reinterpret_cast<const int4 *>(p.exps + ((int64_t)id * p.heads + pair) * 4);
+    };
+    // Step t makes the scores of tile t + 1 beside the sums of tile t, so its
+    // operands are the keys of one tile and the values of the one before.
+    uint4v ahead[2][2 * DG];                               // codes of the next step on their way
+    const char *values = codes;                            // this wavefront's values of the tile whose keys were last
+    const auto load = [&](const char *src, uint4v *dst) {
+#pragma unroll
+        for (int dg = 0; dg < 2 * DG; ++dg)
+            dst[dg] = *reinterpret_cast<const uint4v *>(src + (dg / DG) * 2 * side + (dg % DG) * kBlockBytes);
+    };
+    const auto fetch = [&](int t, bool both) {             // keys of tile t, values of tile t - 1
+        if (both) load(values, ahead[1]);
+        if ((t & 63) == 0 || !both) look_up(t & ~63);
+        int b = t * 4 + wave;
+        if (b >= blocks) b = blocks - 1;
+        const int64_t page_id = __builtin_amdgcn_readlane(id, t & 63);
+        const char *src = codes + page_id * page_bytes + (b & sub_mask) * (16 * DIM) + lane * 16;
+        load(src, ahead[0]);
+        values = src + side;
+    };
+    // Entry 16 g + m of the codes to the lanes that take its numbers: token m's
+    // numbers 16 g.. as a row of the left operand of the scores, numbers m, 16 + m,
+    // .. of tokens 4 g.. as rows of the left operand of the sums.
+    const int g = lane >> 4, m16 = lane & 15;
+    const int to_key = (((wave >> 1) * DG * 4 + (g >> 1) * 2) * 64 + 32 * (g & 1) + 16 * (wave & 1) + m16) * 16;
+    const int to_value = (wave * DG * 4 * 64 + 32 * (g & 1) + 16 * (g >> 1) + m16) * 16;
+    float up[2] = {0.0f, 0.0f};                            // what the values of the tile whose keys were last are taken by
+    const auto stage = [&](int t, bool both) {             // what fetch(t, both) brought
+        const int buf = (t + 1) & 1;
+#pragma unroll
+        for (int dg = 0; dg < 2 * DG; ++dg) {
+            const uint4v k = ahead[0][dg];
+#pragma unroll
+            for (int e = 0; e < 2; ++e)
+                *reinterpret_cast<typename H::x8 *>(&s_tile[buf][0][to_key + (dg / DG) * TileLds<DIM>::HEAD +
+                                                                    ((dg % DG) * 4 + e) * 1024]) =
+                    H::template decode<FORM>(k[2 * e], k[2 * e + 1]);
+        }
+        const int ev0 = __builtin_amdgcn_readlane(ee.y, t & 63), ev1 = __builtin_amdgcn_readlane(ee.w, t & 63);
+        const int ev = ev0 > ev1 ? ev0 : ev1;
+        if (lane == (t & 63)) {
+            s_scale[t & 3][0][wave] = make_float4(scale2 * pow2(ee.x), (float)ev, pow2(-ev), 0.0f);
+            s_scale[t & 3][1][wave] = make_float4(scale2 * pow2(ee.z), (float)ev, pow2(-ev), 0.0f);
+        }
+        if (both) {
+            if (((t - 1) * 4 + wave + 1) * kBlockTokens > len) {
+                // codes past the request's tokens may be anything, NaN too
+                const int valid = len - ((t - 1) * kTileKeys + 16 * wave + 4 * g);
+                const uint32_t keep = valid >= 4 ? ~0u : valid <= 0 ? 0u : (1u << (8 * valid)) - 1u;
+#pragma unroll
+                for (int dg = 0; dg < 2 * DG; ++dg) ahead[1][dg] &= keep;
+            }
+#pragma unroll
+            for (int dg = 0; dg < 2 * DG; ++dg) {
+                // words 0, 1 (2, 3) of the entries 16 g + m and 16 (g + 2) + m come
+                // together in the lower (upper) half: rows m (16 + m) of two operands
+#pragma unroll
+                for (int z = 0; z < 2; ++z) {
+                    const auto w = __builtin_amdgcn_permlane32_swap(ahead[1][dg][z], ahead[1][dg][2 + z], false, false);
+                    *reinterpret_cast<fp16x8 *>(&s_tile[buf][1][to_value + (dg * 2 + z) * 1024]) =
+                        decode_scaled<FORM>(w[0], w[1], up[dg / DG], up[dg / DG]);
+                }
+            }
+        }
+        up[0] = value_scale<FORM>(ev0, ev), up[1] = value_scale<FORM>(ev1, ev);
+    };
+
+    float m = -INFINITY, l = 0.0f;
+    float16v o[DG * 4];
+#pragma unroll
+    for (int c = 0; c < DG * 4; ++c)
+#pragma unroll
+        for (int j = 0; j < 16; ++j) o[c][j] = 0.0f;
+
+    float16v s[2];                                         // scores of the tile whose turn is next
+    const auto key_at = [&](int buf, int c) {
+        return reinterpret_cast<const uint4v *>(&s_tile[buf][0][map * TileLds<DIM>::HEAD + (c * 64 + lane) * 16]);
+    };
+    const auto scores = [&](int buf, float16v *z) {
+#pragma unroll
+        for (int half = 0; half < 2; ++half) {
+#pragma unroll
+            for (int j = 0; j < 16; ++j) z[half][j] = 0.0f;
+#pragma unroll
+            for (int c = 0; c < DG * 4; ++c)
+                z[half] = mfma32<TYPE>(__builtin_bit_cast(typename H::x8, *key_at(buf, half * DG * 4 + c)), q[c], z[half]);
+        }
+    };
+    // One step.  MASK: some row may not see all of the tile's keys.
+    const auto step = [&](int t, auto mask) {
+        constexpr bool MASK = mask();
+        const int buf = t & 1;
+        const float off = m == -INFINITY ? 0.0f : m - (float)kTileRaise;
+        float pow_back[4];
+#pragma unroll
+        for (int b = 0; b < 4; ++b) {
+            const float4 f = s_scale[t & 3][map][b];
+            const float ev = f.y - off;
+            pow_back[b] = f.z;
+#pragma unroll
+            for (int j = 0; j < 8; ++j) s[b >> 1][8 * (b & 1) + j] = fmaf(s[b >> 1][8 * (b & 1) + j], f.x, ev);
+        }
+        if constexpr (MASK) {
+#pragma unroll
+            for (int half = 0; half < 2; ++half)
+#pragma unroll
+                for (int j = 0; j < 16; ++j)
+                    if (t * kTileKeys + 32 * half + 8 * (j >> 2) + 4 * h + (j & 3) >= limit) s[half][j] = -INFINITY;
+        }
+        float top = s[0][0];
+#pragma unroll
+        for (int half = 0; half < 2; ++half)
+#pragma unroll
+            for (int j = 0; j < 16; ++j) top = fmaxf(top, s[half][j]);
+        top = halves_max(top);
+        // the maximum that the sums are relative to follows the real one at some distance
+        if (__builtin_expect(__any(top > (float)kRaise || m == -INFINITY), 0)) {
+            const float m1 = (fmaxf(m, off + top) - (float)kTileRaise) + (float)kTileRaise;
+            float fall = m == -INFINITY ? 0.0f : exp2f(m - m1), shift = m1 == -INFINITY ? 0.0f : off - (m1 - (float)kTileRaise);
+            m = m1;
+            // (keeps the compiler from multiplying ahead of the branch, which is rarely taken)
+            asm volatile("" : "+v"(fall), "+v"(shift));
+            l *= fall;
+#pragma unroll
+            for (int c = 0; c < DG * 4; ++c) o[c] *= fall;
+#pragma unroll
+            for (int half = 0; half < 2; ++half) s[half] += shift;
+        }
+        // Matrix instructions in the order of their operands in LDS, each of which
+        // is read AHEAD instructions before its use; the scores' instructions
+        // alternate between the two halves of the tile, with this tile's
+        // exponentials between them.
+        constexpr int N = DG * 8, ALL = DG * 24, AHEAD = 4;      // instructions of the scores, and with the sums
+        const auto operand = [&](int c) {
+            return c < N ? *key_at(buf, (c & 1) * (N / 2) + (c >> 1))
+                         : *reinterpret_cast<const uint4v *>(&s_tile[buf][1][((c - N) * 64 + lane) * 16]);
+        };
+        uint4v ring[AHEAD];
+        float16v z[2];
+#pragma unroll
+        for (int c = 0; c < AHEAD; ++c) ring[c] = operand(c);
+#pragma unroll
+        for (int half = 0; half < 2; ++half)
+#pragma unroll
+            for (int j = 0; j < 16; ++j) z[half][j] = 0.0f;
+        fp16x8 pr[4];
+        float sum = 0.0f;
+#pragma unroll
+        for (int c = 0; c < N; ++c) {
+            z[c & 1] = mfma32<TYPE>(__builtin_bit_cast(typename H::x8, ring[c % AHEAD]), q[c >> 1], z[c & 1]);
+            ring[c % AHEAD] = operand(c + AHEAD);
+#pragma unroll
+            for (int x = c * 32 / N; x < (c + 1) * 32 / N; ++x) {
+                const float e = __builtin_amdgcn_exp2f(s[x >> 4][x & 15]);
+                sum = (x & 7) == 0 ? e : sum + e;
+                pr[x >> 3][x & 7] = (_Float16)e;
+                if ((x & 7) == 7) l = fmaf(sum, pow_back[x >> 3], l);
+            }
+            __builtin_amdgcn_sched_barrier(0);
+        }
+#pragma unroll
+        for (int c = N; c < ALL; ++c) {
+            const int b = (c - N) / (DG * 4), y = (c - N) % (DG * 4);
+            o[y] = mfma32<AGFT_KV_FP16>(__builtin_bit_cast(fp16x8, ring[c % AHEAD]), pr[b], o[y]);
+            if (c + AHEAD < ALL) ring[c % AHEAD] = operand(c + AHEAD);
+            __builtin_amdgcn_sched_barrier(0);
+        }
+        s[0] = z[0], s[1] = z[1];
+    };
+
+    fetch(begin, false);
+    stage(begin, false);
+    fetch(begin + 1, true);
+    __syncthreads();
+    if (busy) scores((begin + 1) & 1, s);                  // of the first tile, whose keys lie in the buffer of the step before
+    stage(begin + 1, true);
+    if (!busy)                                             // no rows of its own: only fetches
+        for (int t = begin; t < tiles; ++t) {
+            __syncthreads();
+            if (t + 1 < tiles) fetch(t + 2, true), stage(t + 2, true);
+        }
+    int t = busy ? begin : tiles;
+    for (; t < whole; ++t) {
+        __syncthreads();                                   // this step's operands are in LDS, and the other buffer is read
+        if (t + 1 < tiles) fetch(t + 2, true);
+        step(t, std::false_type{});
+        if (t + 1 < tiles) stage(t + 2, true);
+    }
+    for (; t < tiles; ++t) {
+        __syncthreads();
+        if (t + 1 < tiles) fetch(t + 2, true);
+        step(t, std::true_type{});
+        if (t + 1 < tiles) stage(t + 2, true);
+    }
+    l = halves_sum(l);
+    // rows 8 z + 4 h.. of O^T: numbers 64 dg + 32 (z / 2) + 16 T + ..
+    const auto number = [&](int c, int z) { return 64 * (c >> 1) + 32 * (z >> 1) + 16 * (c & 1) + 8 * (z & 1) + 4 * h; };
+    if (item.parts > 1) {
+        // each part leaves its sums as its lanes hold them, and the last to arrive joins them the same way
+        constexpr int64_t PART = 2 * kSubRows * (WIDE + 2);
+        const int64_t stride = (int64_t)p.heads * 2 * PART;
+        const int64_t row_of = (int64_t)(place - item.part) * p.heads * 2 + pair * 2 + sub;
+        float *parts = p.partial + (int64_t)kFewGroups * 2 * piece_floats<DIM>() + row_of * PART;
+        const int mine = wave * (32 * WIDE) + lane * 2, own_row = 2 * kSubRows * WIDE + 32 * wave + n;
+        if (busy) {
+            float *at = parts + item.part * stride;
+#pragma unroll
+            for (int c = 0; c < DG * 4; ++c)
+#pragma unroll
+                for (int z = 0; z < 8; ++z) put2(at + mine + (c * 8 + z) * 128, o[c][2 * z], o[c][2 * z + 1]);
+            if (h == 0) put(at + own_row, m), put(at + own_row + 2 * kSubRows, l);
+        }
+        if (!last_to_arrive(p.arrived + 3 * kFewGroups + row_of, item.parts, &lds.last)) return;
+        if (busy) {
+            m = -INFINITY, l = 0.0f;
+            for (int w = 0; w < item.parts; ++w) m = fmaxf(m, get(parts + w * stride + own_row));
+#pragma unroll
+            for (int c = 0; c < DG * 4; ++c)
+#pragma unroll
+                for (int j = 0; j < 16; ++j) o[c][j] = 0.0f;
+            for (int w = 0; w < item.parts; ++w) {
+                const float *at = parts + w * stride;
+                const float mw = get(at + own_row), lw = get(at + own_row + 2 * kSubRows);
+                const float f = mw == -INFINITY ? 0.0f : exp2f(mw - m);
+                l = fmaf(lw, f, l);
+#pragma unroll
+                for (int c = 0; c < DG * 4; ++c) {
+                    float2 a[8];
+#pragma unroll
+                    for (int z = 0; z < 8; ++z) a[z] = get2(at + mine + (c * 8 + z) * 128);
+#pragma unroll
+                    for (int z = 0; z < 8; ++z)
+                        o[c][2 * z] = fmaf(a[z].x, f, o[c][2 * z]), o[c][2 * z + 1] = fmaf(a[z].y, f, o[c][2 * z + 1]);
+                }
+            }
+        }
+    }
+    // the second map's sums to the first's wavefronts, as the lanes hold them
+    __syncthreads();
+    float4v *other = reinterpret_cast<float4v *>(&s_tile[0][0][0]) + (wave & 1) * (DG * 16 * 64) + lane;
+    static_assert(sizeof(lds.tile) >= 2 * DG * 16 * 64 * sizeof(float4v), "two wavefronts' sums fit where the tiles were");
+    float f = l > 0.0f || l != l ? pow2(-lift<FORM>()) / l : 0.0f;
+    if (busy && map == 1) {
+        f *= lambda_of(p, first, pair, row);
+#pragma unroll
+        for (int c = 0; c < DG * 4; ++c)
+#pragma unroll
+            for (int z = 0; z < 4; ++z)
+                other[(c * 4 + z) * 64] = (float4v){o[c][4 * z], o[c][4 * z + 1], o[c][4 * z + 2], o[c][4 * z + 3]} * f;
+    }
+    __syncthreads();
+    if (!row_here) return;
+    if (h == 0) store_lse(p, first, pair, map, row, m, l * pow2(-kTileRaise));
+    if (map == 1) return;
+    float squares = 0.0f;
+#pragma unroll
+    for (int c = 0; c < DG * 4; ++c)
+#pragma unroll
+        for (int z = 0; z < 4; ++z) {
+            const float4v y = less((float4v){o[c][4 * z], o[c][4 * z + 1], o[c][4 * z + 2], o[c][4 * z + 3]}, f, other[(c * 4 + z) * 64]);
+            squares += square4(y);
+#pragma unroll
+            for (int j = 0; j < 4; ++j) o[c][4 * z + j] = y[j];
+        }
+    const float by = row_factor<WIDE>(p, halves_sum(squares));
+#pragma unroll
+    for (int c = 0; c < DG * 4; ++c)
+#pragma unroll
+        for (int z = 0; z < 4; ++z) {
+            const int d = number(c, z);
+            store4<TYPE>(p, first, pair, row, d,
+                         (float4v){o[c][4 * z], o[c][4 * z + 1], o[c][4 * z + 2], o[c][4 * z + 3]} * by * weight_at(p, d));
+        }
+}
+
+// ---- launches ----
+
+template <int FORM, int TYPE, int DIM>
+__global__ __launch_bounds__(64 * kFewWaves, few_groups<DIM>() / 256) void agft_diff_few_kernel(DiffArgs p) {
+    __shared__ FewLds<DIM> lds;
+    attend_few<FORM, TYPE, DIM, false>(p, lds, blockIdx.x);
+}
+
+// Tiles of many rows, in one launch with the few ones' workgroups where a request
+// may have more than kMidRows.
+template <int FORM, int TYPE, int DIM>
+__global__ __launch_bounds__(64 * kTileWaves, DIM > 64 ? 1 : 2) void agft_diff_tile_kernel(DiffArgs p) {
+    static_assert(kFewWaves == kTileWaves, "one workgroup size");
+    __shared__ union {
+        FewLds<DIM> few;
+        TileLds<DIM> many;
+    } lds;
+    if ((int)blockIdx.x < p.few_blocks) attend_few<FORM, TYPE, DIM, true>(p, lds.few, blockIdx.x);
+    else attend_many<FORM, TYPE, DIM>(p, lds.many, blockIdx.x - p.few_blocks);
+}
+
+inline int diff_status(const agft_kv_config *c) {
+    const int st = config_status(c);
+    if (st != AGFT_OK) return st;
+    return c->heads % 2 != 0 ? AGFT_E_INVAL : c->dim > 128 ? AGFT_E_UNSUPPORTED : AGFT_OK;
+}
+
+}  // namespace agft_diff_detail
+
+using namespace agft_diff_detail;
+
+extern "C" {
+
+size_t agft_diff_attend_bytes(const agft_kv_config *cfg, int32_t max_tokens) {
+    if (diff_status(cfg) != AGFT_OK || !tokens_ok(max_tokens)) return 0;
+    // pieces of few rows, and parts of many
+    const int64_t items = item_cap(cfg, max_tokens) * cfg->heads;
+    const size_t parts = (size_t)(items < kTileParts ? items : kTileParts);
+    const size_t piece = (size_t)(cfg->dim == 64 ? piece_floats<64>() : piece_floats<128>());
+    return align_up(((size_t)kFewGroups * 2 * piece + parts * 2 * kSubRows * (2 * (size_t)cfg->dim + 2)) * sizeof(float));
+}
+
+int agft_diff_attend(const agft_kv_config *cfg, const void *d_cache, size_t cache_bytes, const void *d_tables,
+                     size_t tables_bytes, void *d_step, size_t step_bytes, int32_t max_tokens, int32_t max_new,
+                     const agft_kv_dense *q, const agft_diff_args *diff, const agft_kv_dense *out, float *d_lse,
+                     float scale, void *d_work, size_t work_bytes, void *stream) {
+    int st = diff_status(cfg);
+    if (st != AGFT_OK) return st;
+    agft_kv_tables_view tv;
+    agft_kv_step_view sv;
+    st = agft_kv_tables_at(cfg, const_cast<void *>(d_tables), tables_bytes, &tv);
+    if (st != AGFT_OK) return st;
+    st = agft_kv_step_at(cfg, max_tokens, d_step, step_bytes, &sv);
+    if (st != AGFT_OK) return st;
+    const CacheLayout C = cache_layout(cfg);
+    if (!buffer_ok(d_cache, cache_bytes, C.total)) return AGFT_E_INVAL;
+    if (!buffer_ok(d_work, work_bytes, agft_diff_attend_bytes(cfg, max_tokens))) return AGFT_E_INVAL;
+    if (!dense_ok(q) || !dense_ok(out) || q->type != out->type || q->type == AGFT_KV_FP32) return AGFT_E_INVAL;
+    if (!apart(out, max_tokens, (int64_t)cfg->heads / 2 * cfg->group)) return AGFT_E_INVAL;
+    if (max_new < 1 || max_new > max_tokens || !std::isfinite(scale)) return AGFT_E_INVAL;
+    if (reinterpret_cast<uintptr_t>(d_lse) % 4 != 0) return AGFT_E_INVAL;
+    if (diff == nullptr || diff->lambda == nullptr || reinterpret_cast<uintptr_t>(diff->lambda) % 4 != 0) return AGFT_E_INVAL;
+    if (diff->lambda_token < 0 || diff->lambda_head < 0 || reinterpret_cast<uintptr_t>(diff->weight) % 16 != 0) return AGFT_E_INVAL;
+    if (!std::isfinite(diff->gain) || !std::isfinite(diff->eps) || diff->eps < 0) return AGFT_E_INVAL;
+    const StepLayout L = step_layout(cfg, max_tokens);
+    char *step = static_cast<char *>(d_step);
+    DiffArgs p;
+    p.codes = static_cast<const char *>(d_cache) + C.codes;
+    p.exps = reinterpret_cast<const int32_t *>(static_cast<const char *>(d_cache) + C.exps);
+    p.table = tv.table;
+    p.works = reinterpret_cast<const Work *>(step + L.works);
+    p.items = reinterpret_cast<const Item *>(step + L.items);
+    p.arrived = reinterpret_cast<int32_t *>(step + L.arrived);
+    p.partial = static_cast<float *>(d_work);
+    p.q = static_cast<const char *>(q->data), p.out = static_cast<char *>(out->data), p.lse = d_lse;
+    p.q_token = q->token_stride, p.q_head = q->head_stride;
+    p.out_token = out->token_stride, p.out_head = out->head_stride;
+    p.scale = scale;
+    p.requests = cfg->requests, p.row_pages = cfg->row_pages, p.pages = cfg->pages;
+    p.page = cfg->page, p.shift = log2_of(cfg->page), p.heads = cfg->heads / 2, p.group = cfg->group;
+    p.lambda = diff->lambda, p.lambda_token = diff->lambda_token, p.lambda_head = diff->lambda_head;
+    p.weight = diff->weight, p.eps = diff->eps, p.gain = diff->gain;
+    const int64_t tile_groups = item_cap(cfg, max_tokens) * cfg->heads;     // two of a tile and pair
+    if (tile_groups > INT32_MAX - kFewGroups) return AGFT_E_INVAL;
+    const auto go = [&](auto form, auto type, auto dim) {
+        const hipStream_t hs = static_cast<hipStream_t>(stream);
+        const int64_t rows = (int64_t)max_new * cfg->group;
+        p.few_blocks = rows > kMidRows ? few_groups<dim()>() : 0;
+        p.alone = rows <= kFewRows;
+        if (rows <= kMidRows) {
+            agft_diff_few_kernel<form(), type(), dim()><<<few_groups<dim()>(), 64 * kFewWaves, 0, hs>>>(p);
+            const int code = launched();
+            if (code != AGFT_OK || rows <= kFewRows) return code;
+        }
+        agft_diff_tile_kernel<form(), type(), dim()><<<(unsigned)(p.few_blocks + tile_groups), 64 * kTileWaves, 0, hs>>>(p);
+        return launched();
+    };
+    const auto dims = [&](auto form, auto type) {
+        return cfg->dim == 64 ? go(form, type, std::integral_constant<int, 64>{}) : go(form, type, std::integral_constant<int, 128>{});
+    };
+    const auto types = [&](auto form) {
+        return q->type == AGFT_KV_BF16 ? dims(form, std::integral_constant<int, AGFT_KV_BF16>{})
+                                       : dims(form, std::integral_constant<int, AGFT_KV_FP16>{});
+    };
+    return cfg->form == AGFT_KV_E4M3 ? types(std::integral_constant<int, AGFT_KV_E4M3>{})
+                                     : types(std::integral_constant<int, AGFT_KV_INT8>{});
+}
+
+}  // extern "C"

@@ -1,4 +1,4 @@
-"""Python front end of the serving node's paged cache (agft_kv.h, agft_pages.h): torch
+"""Python front end of the serving node's paged cache (agft_kv.h, agft_pages.h, agft_diff.h): torch
 supplies device memory and streams, the work runs in the HIP kernels behind
 libagft.so.
 
@@ -6,7 +6,7 @@ One window of a node with a KvTables `tables` and, per layer, a KvCache `cache`:
 
     step = tables.plan(add, max_tokens)        # pages and slots of the new tokens
     cache.append(step, k, v)                   # per layer
-    out = cache.attend(tables, step, q)        # per layer
+    out = cache.attend(tables, step, q)        # per layer (or attend_diff)
     tables.commit(step)                        # the new lengths become the tables'
 
 and between windows the tables can be edited (agft_pages.h):
@@ -173,6 +173,7 @@ class KvStep(_OnStream):
         self.starts = _view(self.buffer, v.starts, torch.int32, (R + 1,))
         self.slots = _view(self.buffer, v.slots, torch.int64, (self.max_tokens,))
         self._works, self._work_dim = [], 0
+        self._diff_works, self._diff_dim = [], 0
         self.planned = False
 
     def set_max_new(self, max_new):
@@ -192,6 +193,13 @@ class KvStep(_OnStream):
             self._works.append(owner._buffer(self._lib.agft_kv_attend_bytes(owner._cfg, self.max_tokens), "cache"))
             self._work_dim = owner.cfg.dim
         return self._works[-1]
+
+    def diff_work(self, owner):
+        """The same of the differential attention."""
+        if owner.cfg.dim > self._diff_dim:
+            self._diff_works.append(owner._buffer(self._lib.agft_diff_attend_bytes(owner._cfg, self.max_tokens), "cache"))
+            self._diff_dim = owner.cfg.dim
+        return self._diff_works[-1]
 
 
 class KvEdit(_OnStream):
@@ -379,6 +387,8 @@ class KvCache(_OnStream):
         # what calls tell the library of their tensors (a front end is not thread-safe, like a Tuner)
         self._d0, self._d1 = L.agft_kv_dense(), L.agft_kv_dense()
         self._b0, self._b1 = ctypes.byref(self._d0), ctypes.byref(self._d1)
+        self._diff = L.agft_diff_args()
+        self._bdiff = ctypes.byref(self._diff)
         self.nbytes = self._lib.agft_kv_cache_bytes(self._cfg)
         self.buffer = self._buffer(self.nbytes, "cache")
         self.ptr = self.buffer.data_ptr()
@@ -415,16 +425,18 @@ class KvCache(_OnStream):
         if t.device != self.device:
             raise ValueError(f"expected a tensor on {self.device}")
 
-    def _dense(self, d, t, heads, rows, what, types=TYPES):
+    def _dense(self, d, t, heads, rows, what, types=TYPES, dim=None):
         """Fill the agft_kv_dense d from a [tokens][heads][dim] tensor of at least `rows` tokens."""
+        if dim is None:
+            dim = self.cfg.dim
         try:
-            n, h, dim = t.shape
+            n, h, last = t.shape
             token, head, one = t.stride()
             kind = types[t.dtype]
         except (ValueError, KeyError):
-            n = h = dim = one = -1
-        if n < rows or h != heads or dim != self.cfg.dim or one != 1 or t.get_device() != self._index:
-            raise ValueError(f"{what} must be [{rows} or more][{heads}][{self.cfg.dim}] on {self.device}, "
+            n = h = last = one = -1
+        if n < rows or h != heads or last != dim or one != 1 or t.get_device() != self._index:
+            raise ValueError(f"{what} must be [{rows} or more][{heads}][{dim}] on {self.device}, "
                              f"{' or '.join(str(d) for d in types)}, with contiguous numbers of a head")
         if t.requires_grad and torch.is_grad_enabled():
             raise ValueError(f"{what} asks for a gradient, and these calls have none: detach it, or call under "
@@ -477,6 +489,55 @@ class KvCache(_OnStream):
                                         work.numel(), self._s())
         if code != L.AGFT_OK:
             L.check("agft_kv_attend", code)
+        return out
+
+    def attend_diff(self, tables, step, q, lam, weight=None, gain=1.0, eps=1e-5, out=None, lse=None, scale=None):
+        """Differential attention (agft_diff.h): heads 2 p and 2 p + 1 are a pair,
+        y = (softmax(scale q_0 K_0^T) - lam softmax(scale q_1 K_1^T)) [V_0 V_1], and out
+        is gain y, or with a weight (float32 [2 dim]) gain weight y / sqrt(mean(y^2) +
+        eps).  q [max_tokens][heads * group][dim], as for attend; lam float32
+        [heads / 2 * group], or [max_tokens][heads / 2 * group] with any strides; out
+        [max_tokens][heads / 2 * group][2 * dim]; lse, scale and rows past the window's
+        tokens as in attend."""
+        c, n = self.cfg, step.max_tokens
+        hq, ho = c.heads * c.group, c.heads // 2 * c.group
+        self._fits(step, "step")
+        self._fits(tables, "tables")
+        if c.heads % 2 or c.dim not in (64, 128):
+            raise ValueError(f"differential attention is of pairs of heads of 64 or 128 numbers, not {c.heads} of {c.dim}")
+        if out is None:
+            out = self._empty(n, ho, 2 * c.dim, dtype=q.dtype)
+        elif out.dtype != q.dtype:
+            raise ValueError("q and out must have one type")
+        self._dense(self._d0, q, hq, n, "q", HALVES)
+        self._dense(self._d1, out, ho, n, "out", HALVES, 2 * c.dim)
+        if lse is not None and (lse.device != self.device or lse.dtype != torch.float32 or
+                                lse.shape != (n, hq) or not lse.is_contiguous()):
+            raise ValueError(f"lse must be a contiguous float32 tensor [{n}][{hq}] on {self.device}")
+        rows = lam.shape[0] if lam.dim() == 2 else n
+        if lam.get_device() != self._index or lam.dtype != torch.float32 or lam.shape[-1:] != (ho,) or rows < n or \
+                lam.dim() > 2:
+            raise ValueError(f"lam must be float32 [{ho}] or [{n} or more][{ho}] on {self.device}")
+        if weight is not None and (weight.get_device() != self._index or weight.dtype != torch.float32 or
+                                   weight.shape != (2 * c.dim,) or not weight.is_contiguous() or weight.data_ptr() & 15):
+            raise ValueError(f"weight must be a contiguous float32 tensor [{2 * c.dim}] on {self.device}, from a multiple of "
+                             "16 bytes on")
+        if torch.is_grad_enabled() and (lam.requires_grad or weight is not None and weight.requires_grad):
+            raise ValueError("lam or weight asks for a gradient, and these calls have none: detach it, or call under "
+                             "torch.no_grad()")
+        d = self._diff
+        d.lambda_, d.lambda_head = lam.data_ptr(), lam.stride(-1)
+        d.lambda_token = lam.stride(0) if lam.dim() == 2 else 0
+        d.weight = None if weight is None else weight.data_ptr()
+        d.eps, d.gain = eps, gain
+        work = step.diff_work(self)
+        code = self._lib.agft_diff_attend(self._cfg, self.ptr, self.nbytes, tables.ptr, tables.nbytes, step.ptr,
+                                          step.nbytes, n, step.max_new, self._b0, self._bdiff, self._b1,
+                                          None if lse is None else lse.data_ptr(),
+                                          1.0 / math.sqrt(c.dim) if scale is None else float(scale), work.data_ptr(),
+                                          work.numel(), self._s())
+        if code != L.AGFT_OK:
+            L.check("agft_diff_attend", code)
         return out
 
     def copy(self, edit):
