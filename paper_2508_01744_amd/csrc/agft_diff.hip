@@ -22,8 +22,6 @@ struct DiffArgs : AttendArgs {
 };
 
 constexpr int kManyPieces = 32;            // more are joined in groups first
-constexpr int kFewShare = 4;               // units that a workgroup takes at least
-constexpr int kFewEven = 8;                // units up to which rows are cut evenly
 constexpr int kRaise = 15;
 
 // Two halves of a value row meet the same probabilities, and each page has a scale
@@ -122,119 +120,183 @@ __device__ __forceinline__ void fill_rows(const DiffArgs &p, int first, int pair
 // Every wavefront keeps its map's maximum, sum and 16 rows of 2 dim sums; the two
 // of a map join in LDS, pieces of several workgroups through memory, and the
 // difference and its norm are made once, where everything has met.
+//
+// What follows the loop over the tokens runs once a segment, over the rows that
+// there are, a thread for four numbers of a row of both maps: short code, since
+// code that has not run lately comes from memory as data does.
+//
+// What bounds it: memory for long contexts (24 tokens over 60,000 to 131,071 tokens, 8
+// heads of 128 numbers, 4.45 GB: 782 us, 5.7 TB/s), and below a chain of loads
+// (requests, page, codes) and of meetings (LDS, the pieces' way through memory): one
+// token over 778 tokens 12.9 us, 3 until the first codes are asked for, 4 in the loop,
+// 5 from there.  More on its way does not help: a third workgroup of 128 numbers
+// on a compute unit (queries in LDS, 17 registers spilled) 849 us for the long contexts,
+// two steps' codes ahead (30 spilled) 813, both maps in each wavefront, a value decoded
+// once, 816 (and one token 24).
+
+// Workgroups that share the work: what the registers let run at once.
 template <int DIM>
 constexpr int few_groups() {
     return DIM == 64 ? 768 : 512;
 }
 
+// A workgroup takes at least few_share units (64 numbers, 4 / 6: 200 requests of 16 to
+// 32 rows over up to 3,000 tokens 31.0 / 26.9 us; 128 numbers, 2 / 4 / 6: one token over
+// 778 tokens 12.4 / 12.9 / 13.8, 8 tokens over 500 to 4,000 24.2 / 18.2 / 18.9).  While its
+// share is at most kFewEven, rows are cut evenly if that takes no more workgroups; beyond,
+// up to 64 requests are cut by what their segments cost, kSegment units beside their own
+// (64 tokens over 100 to 8,192 tokens, 128 numbers: 63 us; by the units alone 77; in even
+// pieces, twice as many as run at once, 72).
+template <int DIM>
+constexpr int few_share() {
+    return DIM == 64 ? 6 : 4;
+}
+constexpr int kFewEven = 8;
+constexpr int kSegment = 2;
+
 template <int DIM>
 struct FewLds {
     static constexpr int C = DIM / 8;              // blocks of 16 numbers of a value row
-    float4v o[2][C * 64];                          // a map's sums, as the lanes hold them
-    float m[2][kRowTile], l[2][kRowTile], squares[2][kRowTile];
+    static constexpr int ROW = 2 * DIM + 4;        // off the banks
+    // the second half's sums of a map, as the lanes hold them; then the map's, by rows
+    union {
+        float4v half[2][C * 64];
+        float rows[2][kRowTile * ROW];
+    };
+    float m[2][2][kRowTile], l[2][2][kRowTile], lambda[kRowTile];   // [map][half]
     EvenLds even;
     int last;
 };
 
-// A piece: both maps' sums as the lanes hold them, their maxima, their sums of probabilities.
+// A piece: both maps' sums by rows, their maxima, their sums of probabilities.
 template <int DIM>
 constexpr int piece_floats() {
-    return 2 * (FewLds<DIM>::C * 256 + 2 * kRowTile);
+    return 2 * kRowTile * (2 * DIM + 2);
 }
 
-// The rows' results, from both maps' sums: NC blocks of 16 numbers from block c0 on
-// of one map in a wavefront that is busy.  All wavefronts come here.
-template <int FORM, int TYPE, int DIM, int NC>
-__device__ __forceinline__ void finish_rows(const DiffArgs &p, const Segment &seg, FewLds<DIM> &lds, bool busy, int map,
-                                            int c0, float4v *o, float m, float l) {
-    const int lane = threadIdx.x & 63, n = lane & 15, g = lane >> 4;
-    const int row = seg.row + (n < seg.rows ? n : 0);
-    float f = l > 0.0f || l != l ? pow2(-kRaise - lift<FORM>()) / l : 0.0f;
-    if (busy && map == 1) {
-        f *= lambda_of(p, seg.first, seg.head, row);
+// Four numbers of a row of either map, with the row's maxima and sums of probabilities.
+struct Both {
+    float4v o[2];
+    float m[2], l[2];
+};
+
+// The row's results from both maps' sums: all threads of a row, which lie side by side.
+template <int FORM, int TYPE, int DIM>
+__device__ __forceinline__ void finish(const DiffArgs &p, const Segment &seg, int r, int d, const Both &b, float lambda,
+                                       float4v weight) {
+    constexpr float unit = 1.0f / (1 << kRaise) / (1 << lift<FORM>());
+    float f[2];
 #pragma unroll
-        for (int c = 0; c < NC; ++c) lds.o[1][(c0 + c) * 64 + lane] = o[c] * f;
-    }
-    if (busy && c0 == 0 && g == 0 && n < seg.rows) store_lse(p, seg.first, seg.head, map, row, m, l);
-    __syncthreads();
-    if (busy && map == 0) {
-        float squares = 0.0f;
+    for (int a = 0; a < 2; ++a) f[a] = b.l[a] > 0.0f || b.l[a] != b.l[a] ? unit / b.l[a] : 0.0f;
+    float4v y = less(b.o[0], f[0], b.o[1] * (f[1] * lambda));
+    float squares = square4(y);
 #pragma unroll
-        for (int c = 0; c < NC; ++c) {
-            o[c] = less(o[c], f, lds.o[1][(c0 + c) * 64 + lane]);
-            squares += square4(o[c]);
-        }
-        squares = across_sum(squares);
-        if (g == 0) lds.squares[c0 > 0][n] = squares;
-    }
-    __syncthreads();
-    if (busy && map == 0 && n < seg.rows) {
-        float squares = lds.squares[0][n];
-        if constexpr (NC < FewLds<DIM>::C) squares += lds.squares[1][n];
-        const float by = row_factor<2 * DIM>(p, squares);
+    for (int s = 1; s < DIM / 2; s *= 2) squares += __shfl_xor(squares, s, 64);
+    const int row = seg.row + r;
+    store4<TYPE>(p, seg.first, seg.head, row, d, y * row_factor<2 * DIM>(p, squares) * weight);
+    if (d == 0) {
 #pragma unroll
-        for (int c = 0; c < NC; ++c) {
-            const int d = (c0 + c) * 16 + 4 * g;
-            store4<TYPE>(p, seg.first, seg.head, row, d, o[c] * by * weight_at(p, d));
-        }
+        for (int a = 0; a < 2; ++a) store_lse(p, seg.first, seg.head, a, row, b.m[a], b.l[a]);
     }
 }
 
-// Joins the pieces of the same 16 rows.  A wavefront takes half of the numbers of
-// one map.  into: where the joined piece goes, or NULL: it is the rows' result.
+template <int DIM>
+__device__ __forceinline__ void put_piece(float *to, int r, int d, const Both &b) {
+    constexpr int WIDE = 2 * DIM, MAP = kRowTile * WIDE;
+#pragma unroll
+    for (int a = 0; a < 2; ++a) {
+        put2(to + a * MAP + r * WIDE + d, b.o[a][0], b.o[a][1]);
+        put2(to + a * MAP + r * WIDE + d + 2, b.o[a][2], b.o[a][3]);
+        if (d == 0) put(to + 2 * MAP + a * kRowTile + r, b.m[a]), put(to + 2 * MAP + (2 + a) * kRowTile + r, b.l[a]);
+    }
+}
+
+// Joins the pieces of the same 16 rows.  into: where the joined piece goes, or NULL:
+// it is the rows' result.  (into is the first of them; a row is one wavefront's.)
 template <int FORM, int TYPE, int DIM, typename F>
 __device__ __forceinline__ void join_pieces(const DiffArgs &p, F piece, int pieces, float *into, const Segment &seg,
-                                            FewLds<DIM> &lds) {
-    constexpr int C = FewLds<DIM>::C, HALF = C / 2, MAP = C * 256;
-    constexpr int AHEAD = DIM == 64 ? 1 : 2;   // pieces on their way at once
-    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-    const int map = wave >> 1, half = wave & 1, n = lane & 15, g = lane >> 4;
-    const int maxima = 2 * MAP + map * kRowTile + n, at = map * MAP + half * HALF * 256 + lane * 4;
-    float m = -INFINITY, l = 0.0f;
+                                            const float *lambda, float4v weight) {
+    constexpr int WIDE = 2 * DIM, MAP = kRowTile * WIDE;
+    constexpr int AHEAD = 4;                   // pieces on their way at once, maxima and all
+    for (int c = threadIdx.x; c < seg.rows * (WIDE / 4); c += blockDim.x) {
+        const int r = c / (WIDE / 4), d = c % (WIDE / 4) * 4;
+        Both b;
+#pragma unroll
+        for (int a = 0; a < 2; ++a) b.m[a] = -INFINITY, b.l[a] = 0.0f, b.o[a] = (float4v){0, 0, 0, 0};
 #pragma unroll 1
-    for (int w0 = 0; w0 < pieces; w0 += 8) {
-        float x[8];
+        for (int w0 = 0; w0 < pieces; w0 += AHEAD) {
+            float m[AHEAD][2], l[AHEAD][2];
+            float2 x[AHEAD][2], y[AHEAD][2];
 #pragma unroll
-        for (int z = 0; z < 8; ++z) x[z] = get(piece(w0 + z < pieces ? w0 + z : w0) + maxima);
+            for (int z = 0; z < AHEAD; ++z) {
+                const float *src = piece(w0 + z < pieces ? w0 + z : w0);
 #pragma unroll
-        for (int z = 0; z < 8; ++z) m = fmaxf(m, x[z]);
-    }
-    float4v o[HALF];
-#pragma unroll
-    for (int c = 0; c < HALF; ++c) o[c] = (float4v){0, 0, 0, 0};
-#pragma unroll 1
-    for (int w0 = 0; w0 < pieces; w0 += AHEAD) {
-        float mw[AHEAD], lw[AHEAD];
-        float2 a[AHEAD][HALF], b[AHEAD][HALF];
-#pragma unroll
-        for (int z = 0; z < AHEAD; ++z) {
-            const float *src = piece(w0 + z < pieces ? w0 + z : w0);
-            mw[z] = get(src + maxima), lw[z] = get(src + maxima + 2 * kRowTile);
-#pragma unroll
-            for (int c = 0; c < HALF; ++c) a[z][c] = get2(src + at + c * 256), b[z][c] = get2(src + at + c * 256 + 2);
-        }
-#pragma unroll
-        for (int z = 0; z < AHEAD; ++z)
-            if (w0 + z < pieces) {
-                const float f = mw[z] == -INFINITY ? 0.0f : exp2f(mw[z] - m);
-                l = fmaf(lw[z], f, l);
-#pragma unroll
-                for (int c = 0; c < HALF; ++c) o[c] += (float4v){a[z][c].x, a[z][c].y, b[z][c].x, b[z][c].y} * f;
+                for (int a = 0; a < 2; ++a) {
+                    m[z][a] = get(src + 2 * MAP + a * kRowTile + r), l[z][a] = get(src + 2 * MAP + (2 + a) * kRowTile + r);
+                    x[z][a] = get2(src + a * MAP + r * WIDE + d), y[z][a] = get2(src + a * MAP + r * WIDE + d + 2);
+                }
             }
-    }
-    if (into == nullptr) {
-        finish_rows<FORM, TYPE, DIM, HALF>(p, seg, lds, true, map, half * HALF, o, m, l);
-        return;
-    }
-    // (into is the first of the pieces, which the other lanes of this wavefront have read too; the
-    // other wavefronts read other numbers of it, and the maxima only up to here)
-    __syncthreads();
 #pragma unroll
-    for (int c = 0; c < HALF; ++c) {
-        put2(into + at + c * 256, o[c][0], o[c][1]);
-        put2(into + at + c * 256 + 2, o[c][2], o[c][3]);
+            for (int a = 0; a < 2; ++a) {
+                float top = b.m[a];
+#pragma unroll
+                for (int z = 0; z < AHEAD; ++z) top = fmaxf(top, m[z][a]);
+                const float fall = b.m[a] == -INFINITY ? 0.0f : exp2f(b.m[a] - top);
+                b.m[a] = top, b.l[a] *= fall, b.o[a] *= fall;
+#pragma unroll
+                for (int z = 0; z < AHEAD; ++z)
+                    if (w0 + z < pieces) {
+                        const float f = m[z][a] == -INFINITY ? 0.0f : exp2f(m[z][a] - top);
+                        b.l[a] = fmaf(l[z][a], f, b.l[a]);
+                        b.o[a] += (float4v){x[z][a].x, x[z][a].y, y[z][a].x, y[z][a].y} * f;
+                    }
+            }
+        }
+        if (into == nullptr) finish<FORM, TYPE, DIM>(p, seg, r, d, b, lambda[r], weight);
+        else put_piece<DIM>(into, r, d, b);
     }
-    if (g == 0 && half == 0) put(into + maxima, m), put(into + maxima + 2 * kRowTile, l);
+}
+
+// Where a segment costs more than its units, the work is cut by that: a lane per
+// request, up to 64 of them.
+struct Costs {
+    int32_t tiles, units, to;   // of the lane's request: tiles of rows, units of each; the costs up to its end
+    int32_t all;
+};
+__device__ __forceinline__ Costs costs_of(const DiffArgs &p, const Works &works) {
+    const int lane = threadIdx.x & 63;
+    const int few_next = __shfl_down(works.a.x, 1, 64), start_next = __shfl_down(works.a.z, 1, 64);
+    const bool end = lane + 1 >= works.n;
+    Costs c;
+    tiles_of(p, works.a.x, works.a.z, end ? works.total.x : few_next, end ? works.total.z : start_next, c.tiles, c.units);
+    if (lane >= works.n) c.tiles = 0;
+    c.to = c.tiles * (c.units + kSegment) * p.heads;
+#pragma unroll
+    for (int s = 1; s < 64; s *= 2) {
+        const int x = __shfl_up(c.to, s, 64);
+        if (lane >= s) c.to += x;
+    }
+    c.all = __builtin_amdgcn_readlane(c.to, 63);
+    return c;
+}
+
+// The segment at place x of the costs; at: its unit there, or less than 0: so far ahead of its first.
+__device__ __forceinline__ Segment segment_at(const DiffArgs &p, const Works &works, const Costs &c, int32_t x) {
+    const auto at = [&](int v, int k) { return __builtin_amdgcn_readlane(v, k); };
+    Segment s;
+    const int i = __popcll(__ballot(c.to <= x));
+    if (i >= works.n) {
+        s.units = 0, s.at = 0;
+        return s;
+    }
+    const int tiles = at(c.tiles, i), one = at(c.units, i) + kSegment, rest = x - (at(c.to, i) - tiles * one * p.heads);
+    const int number = rest / one, tile = number % tiles;
+    const int start_next = i + 1 < works.n ? at(works.a.z, i + 1 < 64 ? i + 1 : 63) : works.total.z;
+    s.request = i, s.head = number / tiles, s.row = tile * kRowTile, s.units = one - kSegment, s.at = rest - number * one - kSegment;
+    s.first = at(works.a.z, i), s.granted = at(works.a.w, i), s.length = at(works.length, i);
+    const int rows = (start_next - s.first) * p.group - s.row;
+    s.rows = rows < kRowTile ? rows : kRowTile;
+    return s;
 }
 
 // Rows of tiles that no launch makes, because a request brings more tokens than
@@ -266,11 +328,12 @@ __device__ __forceinline__ void attend_few(const DiffArgs &p, FewLds<DIM> &lds, 
         if (__builtin_expect(p.alone && works.total.y > 0, 0)) leave_nan<TYPE, 2 * DIM>(p, works.total.y);
     const int32_t work = works.total.x * p.heads;
     int32_t share = (work + few_groups<DIM>() - 1) / few_groups<DIM>();
-    if (share < kFewShare) share = kFewShare;
+    if (share < few_share<DIM>()) share = few_share<DIM>();
     int64_t x_first = (int64_t)block * share;
     int32_t x1 = x_first + share < work ? (int32_t)x_first + share : work;
     Piece cut;
-    bool even = false;
+    Costs costs;
+    bool even = false, by_cost = false;
     if (share <= kFewEven) {
         if (works.n <= 64)
             even = piece_of(p, works, share, few_groups<DIM>(), block, &cut) ||
@@ -278,15 +341,33 @@ __device__ __forceinline__ void attend_few(const DiffArgs &p, FewLds<DIM> &lds, 
         else if (works.n <= kEvenRequests)
             even = piece_of(p, works, share, few_groups<DIM>(), block, lds.even, &cut);
     }
-    if (even) x_first = cut.first, x1 = cut.last;
+    if (even) {
+        x_first = cut.first, x1 = cut.last;
+    } else if (works.n <= 64 && work < 1 << 28) {
+        by_cost = true;
+        costs = costs_of(p, works);
+        share = (costs.all + few_groups<DIM>() - 1) / few_groups<DIM>();
+        x_first = (int64_t)block * share;
+        x1 = x_first + share < costs.all ? (int32_t)x_first + share : costs.all;
+    }
     if (x_first >= x1) return;
     const int64_t side = (int64_t)p.page * DIM, page_bytes = (int64_t)p.heads * 4 * side;
     const float scale2 = p.scale * kLog2e;
     int32_t x = (int32_t)x_first;
     if (even) works.look_at(cut.request);
-    else works.look(x / p.heads);
+    else if (!by_cost) works.look(x / p.heads);
     while (x < x1) {
-        const Segment seg = segment_of(p, works, x);
+        Segment seg;
+        if (by_cost) {
+            seg = segment_at(p, works, costs, x);
+            if (seg.at < 0) {
+                x -= seg.at;
+                seg.at = 0;
+                if (x >= x1) break;
+            }
+        } else {
+            seg = segment_of(p, works, x);
+        }
         if (seg.units <= 0) break;
         const int i = seg.request, pair = seg.head, units = seg.units, u0 = seg.at, row0 = seg.row, rows = seg.rows;
         const int first = seg.first;
@@ -301,6 +382,7 @@ __device__ __forceinline__ void attend_few(const DiffArgs &p, FewLds<DIM> &lds, 
         // right operand of the scores: row n's numbers 64 dg + 16 g + 8 e.. + 7
         typename H::x8 q[DG * 2];
         const bool row_here = n < rows;
+        const float lambda = lambda_of(p, first, pair, row_here ? row0 + n : row0);
         {
             const int tk = (row0 + n) / p.group, hq = (2 * pair + map) * p.group + (row0 + n) % p.group;
             const char *src = p.q + ((int64_t)(first + tk) * p.q_token + hq * p.q_head) * 2;
@@ -331,8 +413,7 @@ __device__ __forceinline__ void attend_few(const DiffArgs &p, FewLds<DIM> &lds, 
         for (int b0 = b_first; b0 < b_last; b0 += 64) {
             // a lane per block: its page, this map's keys' exponent, the values' larger one and
             // what either head's codes are taken by
-            int id, ek, ev;
-            float up[2];
+            int id, exps;
             {
                 int b = b0 + lane;
                 if (b >= blocks) b = blocks - 1;
@@ -340,9 +421,8 @@ __device__ __forceinline__ void attend_few(const DiffArgs &p, FewLds<DIM> &lds, 
                 if (z >= (uint32_t)p.pages) z = (uint32_t)p.pages - 1;
                 id = (int)z;
                 const int4 e = *reinterpret_cast<const int4 *>(p.exps + ((int64_t)id * p.heads + pair) * 4);
-                ek = map == 0 ? e.x : e.z;
-                ev = e.y > e.w ? e.y : e.w;
-                up[0] = value_scale<FORM>(e.y, ev), up[1] = value_scale<FORM>(e.w, ev);
+                // (exponents lie in -127..127)
+                exps = ((map == 0 ? e.x : e.z) & 255) | (e.y & 255) << 8 | (e.w & 255) << 16;
             }
             const int b1 = b0 + 64 < b_last ? b0 + 64 : b_last;
             const auto block_at = [&](int b) {
@@ -384,9 +464,9 @@ __device__ __forceinline__ void attend_few(const DiffArgs &p, FewLds<DIM> &lds, 
                     }
                     int bb = b + s;
                     if (bb >= b_last) bb = b_last - 1;
-                    const int bek = __builtin_amdgcn_readlane(ek, bb - b0), bev = __builtin_amdgcn_readlane(ev, bb - b0);
-                    by[s][0] = __uint_as_float(__builtin_amdgcn_readlane(__float_as_uint(up[0]), bb - b0));
-                    by[s][1] = __uint_as_float(__builtin_amdgcn_readlane(__float_as_uint(up[1]), bb - b0));
+                    const int e = __builtin_amdgcn_readlane(exps, bb - b0);
+                    const int bek = (int8_t)e, ev0 = (int8_t)(e >> 8), ev1 = (int8_t)(e >> 16), bev = ev0 > ev1 ? ev0 : ev1;
+                    by[s][0] = value_scale<FORM>(ev0, bev), by[s][1] = value_scale<FORM>(ev1, bev);
                     const float ks = scale2 * pow2(bek);
                     back[s] = pow2(-bev);
 #pragma unroll
@@ -441,38 +521,47 @@ __device__ __forceinline__ void attend_few(const DiffArgs &p, FewLds<DIM> &lds, 
                 if (b + BLK < b1) fetch_values(b + BLK, vc);
             }
         }
+        // (a thread's four numbers of a row are the same of every row)
+        const float4v weight = weight_at(p, (int)threadIdx.x % (DIM / 2) * 4);
+        // the two wavefronts of a map meet, and leave its sums by rows
         l = across_sum(l);
-        // the two wavefronts of a map meet
+        if (g == 0) lds.m[map][part][n] = m, lds.l[map][part][n] = l;
         if (part == 1) {
 #pragma unroll
-            for (int c = 0; c < C; ++c) lds.o[map][c * 64 + lane] = o[c];
-            if (g == 0) lds.m[map][n] = m, lds.l[map][n] = l;
+            for (int c = 0; c < C; ++c) lds.half[map][c * 64 + lane] = o[c];
         }
+        if (wave == 0 && g == 0) lds.lambda[n] = lambda;
         __syncthreads();
         if (part == 0) {
-            const float m1 = lds.m[map][n], both = fmaxf(m, m1);
+            const float m1 = lds.m[map][1][n], both = fmaxf(m, m1);
             const float f0 = m == -INFINITY ? 0.0f : exp2f(m - both), f1 = m1 == -INFINITY ? 0.0f : exp2f(m1 - both);
-            l = fmaf(l, f0, lds.l[map][n] * f1);
-            m = both;
 #pragma unroll
-            for (int c = 0; c < C; ++c) o[c] = o[c] * f0 + lds.o[map][c * 64 + lane] * f1;
+            for (int c = 0; c < C; ++c) o[c] = o[c] * f0 + lds.half[map][c * 64 + lane] * f1;
+            if (g == 0) lds.l[map][0][n] = fmaf(l, f0, lds.l[map][1][n] * f1), lds.m[map][0][n] = both;
         }
-        if (count == units) {
-            finish_rows<FORM, TYPE, DIM, C>(p, seg, lds, part == 0, map, 0, o, m, l);
-        } else {
-            const int32_t from = x - count - u0;                       // the rows' first unit
+        __syncthreads();
+        if (part == 0 && row_here) {
+#pragma unroll
+            for (int c = 0; c < C; ++c) *reinterpret_cast<float4v *>(&lds.rows[map][n * FewLds<DIM>::ROW + 16 * c + 4 * g]) = o[c];
+        }
+        __syncthreads();
+        const bool whole = count == units;
+        float *to = p.partial + ((int64_t)block * 2 + (u0 == 0 ? 1 : 0)) * piece_floats<DIM>();
+        for (int c = threadIdx.x; c < rows * (DIM / 2); c += blockDim.x) {
+            const int r = c / (DIM / 2), d = c % (DIM / 2) * 4;
+            Both b;
+#pragma unroll
+            for (int a = 0; a < 2; ++a) {
+                b.m[a] = lds.m[a][0][r], b.l[a] = lds.l[a][0][r];
+                b.o[a] = *reinterpret_cast<const float4v *>(&lds.rows[a][r * FewLds<DIM>::ROW + d]);
+            }
+            if (whole) finish<FORM, TYPE, DIM>(p, seg, r, d, b, lds.lambda[r], weight);
+            else put_piece<DIM>(to, r, d, b);
+        }
+        if (!whole) {
+            const int32_t from = x - count - u0;                       // the place of the rows' first unit
             const int owner = even ? cut.owner : from / share;
             const int pieces = even ? cut.pieces : (from + units - 1) / share - owner + 1;
-            if (part == 0) {
-                float *at = p.partial + ((int64_t)block * 2 + (u0 == 0 ? 1 : 0)) * piece_floats<DIM>();
-#pragma unroll
-                for (int c = 0; c < C; ++c) {
-                    put2(at + (map * C + c) * 256 + lane * 4, o[c][0], o[c][1]);
-                    put2(at + (map * C + c) * 256 + lane * 4 + 2, o[c][2], o[c][3]);
-                }
-                at += 2 * C * 256 + map * kRowTile + n;
-                if (g == 0) put(at, m), put(at + 2 * kRowTile, l);
-            }
             // groups of kManyPieces first, each into its first piece's place
             const int mine = block - owner, group0 = mine / kManyPieces * kManyPieces;
             const int members = pieces - group0 < kManyPieces ? pieces - group0 : kManyPieces;
@@ -482,11 +571,13 @@ __device__ __forceinline__ void attend_few(const DiffArgs &p, FewLds<DIM> &lds, 
                 return p.partial + ((int64_t)(owner + w) * 2 + (w == 0 ? 1 : 0)) * piece_floats<DIM>();
             };
             int32_t *counter = p.arrived + kFewGroups + (owner + group0) * 2 + (group0 == 0 ? 1 : 0);
-            if (last_to_arrive(counter, members, &lds.last)) {
-                float *into = groups == 1 ? nullptr : piece(group0);
-                join_pieces<FORM, TYPE, DIM>(p, [&](int w) { return piece(group0 + w); }, members, into, seg, lds);
-                if (groups > 1 && last_to_arrive(p.arrived + owner, groups, &lds.last))
-                    join_pieces<FORM, TYPE, DIM>(p, [&](int w) { return piece(kManyPieces * w); }, groups, nullptr, seg, lds);
+            // (one join in the code: of a group's pieces, then, by the last of all, of the groups')
+            int parties = members, step = 1, at = group0;
+            float *into = groups == 1 ? nullptr : piece(group0);
+            while (last_to_arrive(counter, parties, &lds.last)) {
+                join_pieces<FORM, TYPE, DIM>(p, [&](int w) { return piece(at + step * w); }, parties, into, seg, lds.lambda, weight);
+                if (into == nullptr) break;
+                counter = p.arrived + owner, parties = groups, step = kManyPieces, at = 0, into = nullptr;
             }
         }
         __syncthreads();
@@ -862,7 +953,7 @@ __global__ __launch_bounds__(64 * kFewWaves, few_groups<DIM>() / 256) void agft_
 // may have more than kMidRows.
 template <int FORM, int TYPE, int DIM>
 __global__ __launch_bounds__(64 * kTileWaves, DIM > 64 ? 1 : 2) void agft_diff_tile_kernel(DiffArgs p) {
-    static_assert(kFewWaves == kTileWaves, "one workgroup size");
+    static_assert(few_groups<DIM>() <= kFewGroups && kFewWaves == kTileWaves, "one workgroup size");
     __shared__ union {
         FewLds<DIM> few;
         TileLds<DIM> many;
