@@ -101,9 +101,9 @@ __device__ __forceinline__ float lambda_of(const DiffArgs &p, int first, int pai
 }
 
 // Rows that no map has keys for: x in out, `lse` in d_lse.
-template <int TYPE, int WIDE>
+template <int TYPE, int WIDE, int THREADS>
 __device__ __forceinline__ void fill_rows(const DiffArgs &p, int first, int pair, int row0, int rows, float x, float lse) {
-    for (int c = threadIdx.x; c < rows * (WIDE / 4); c += blockDim.x) {
+    for (int c = threadIdx.x; c < rows * (WIDE / 4); c += THREADS) {
         const int r = c / (WIDE / 4), d = c % (WIDE / 4) * 4;
         store4<TYPE>(p, first, pair, row0 + r, d, (float4v){x, x, x, x});
         if (d == 0) store_lse(p, first, pair, 0, row0 + r, lse, 1.0f), store_lse(p, first, pair, 1, row0 + r, lse, 1.0f);
@@ -218,7 +218,7 @@ __device__ __forceinline__ void join_pieces(const DiffArgs &p, F piece, int piec
                                             const float *lambda, float4v weight) {
     constexpr int WIDE = 2 * DIM, MAP = kRowTile * WIDE;
     constexpr int AHEAD = 4;                   // pieces on their way at once, maxima and all
-    for (int c = threadIdx.x; c < seg.rows * (WIDE / 4); c += blockDim.x) {
+    for (int c = threadIdx.x; c < seg.rows * (WIDE / 4); c += 64 * kFewWaves) {
         const int r = c / (WIDE / 4), d = c % (WIDE / 4) * 4;
         Both b;
 #pragma unroll
@@ -310,12 +310,11 @@ __device__ __forceinline__ void leave_nan(const DiffArgs &p, int items) {
         const int pair = (int)(x % p.heads), first = p.works[item.request].start, row0 = item.tile * kTileRows;
         int rows = (p.works[item.request + 1].start - first) * p.group - row0;
         if (rows > kTileRows) rows = kTileRows;
-        fill_rows<TYPE, WIDE>(p, first, pair, row0, rows, NAN, NAN);
+        fill_rows<TYPE, WIDE, 64 * kFewWaves>(p, first, pair, row0, rows, NAN, NAN);
     }
 }
 
-// BESIDE: in a launch that makes the tiles of many rows too
-template <int FORM, int TYPE, int DIM, bool BESIDE>
+template <int FORM, int TYPE, int DIM>
 __device__ __forceinline__ void attend_few(const DiffArgs &p, FewLds<DIM> &lds, int block) {
     constexpr int DG = DIM / kBlockDims, C = FewLds<DIM>::C;
     constexpr int BLK = 2;                        // blocks of 16 tokens at a time
@@ -324,8 +323,7 @@ __device__ __forceinline__ void attend_few(const DiffArgs &p, FewLds<DIM> &lds, 
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     const int g = lane >> 4, n = lane & 15, part = wave & 1, map = wave >> 1;
     Works works(p.works, p.requests);
-    if constexpr (!BESIDE)
-        if (__builtin_expect(p.alone && works.total.y > 0, 0)) leave_nan<TYPE, 2 * DIM>(p, works.total.y);
+    if (__builtin_expect(p.alone && works.total.y > 0, 0)) leave_nan<TYPE, 2 * DIM>(p, works.total.y);
     const int32_t work = works.total.x * p.heads;
     int32_t share = (work + few_groups<DIM>() - 1) / few_groups<DIM>();
     if (share < few_share<DIM>()) share = few_share<DIM>();
@@ -376,7 +374,7 @@ __device__ __forceinline__ void attend_few(const DiffArgs &p, FewLds<DIM> &lds, 
         const int granted = seg.granted, len = seg.length;
         if (granted <= 0) {
             // no slots, no keys
-            fill_rows<TYPE, 2 * DIM>(p, first, pair, row0, rows, 0.0f, -INFINITY);
+            fill_rows<TYPE, 2 * DIM, 64 * kFewWaves>(p, first, pair, row0, rows, 0.0f, -INFINITY);
             continue;
         }
         // right operand of the scores: row n's numbers 64 dg + 16 g + 8 e.. + 7
@@ -547,7 +545,7 @@ __device__ __forceinline__ void attend_few(const DiffArgs &p, FewLds<DIM> &lds, 
         __syncthreads();
         const bool whole = count == units;
         float *to = p.partial + ((int64_t)block * 2 + (u0 == 0 ? 1 : 0)) * piece_floats<DIM>();
-        for (int c = threadIdx.x; c < rows * (DIM / 2); c += blockDim.x) {
+        for (int c = threadIdx.x; c < rows * (DIM / 2); c += 64 * kFewWaves) {
             const int r = c / (DIM / 2), d = c % (DIM / 2) * 4;
             Both b;
 #pragma unroll
@@ -584,17 +582,44 @@ __device__ __forceinline__ void attend_few(const DiffArgs &p, FewLds<DIM> &lds, 
     }
 }
 
+// The lane, for what follows the loop over the tokens: nothing made from it is kept
+// in registers through that loop.
+__device__ __forceinline__ int lane_anew() {
+    int lane = threadIdx.x & 63;
+    asm volatile("" : "+v"(lane));
+    return lane;
+}
+
 // ---- many query rows ----
 //
-// A tile of agft_kv_attend's plan, 128 query rows of one request, is two workgroups
-// here, of 64 rows each: two wavefronts take 32 rows' first map and two their second,
-// over the tokens 64 at a time.  Each wavefront fetches one block of 16 tokens, keys
-// and values of both heads, and leaves them in LDS as 16 bits; a wavefront reads its
-// map's keys there and all values.  The second map's sums go to the first's
-// wavefronts through LDS at the end.
-constexpr int kTileWaves = 4;
+// A tile of agft_kv_attend's plan, 128 query rows of one request, is one workgroup of
+// eight wavefronts (128 numbers) or two of four (64 numbers): half of them take 32 rows'
+// first map each and half their second, over the tokens 64 at a time.  The wavefronts
+// fetch the tile's codes once between them, a tile ahead, and leave keys and values in
+// LDS as 16 bits; each reads its map's keys there and all values.  A step makes the
+// scores of the tokens that follow beside the exponentials and sums of those before
+// them, 64 tokens at a time, or 32 where the registers hold no more (128 numbers: 32
+// rows of 256 sums are 128 registers of 256, and two wavefronts share a SIMD).  The
+// second map's sums go to the first's wavefronts through LDS at the end.
+//
+// The prompt (10,001 tokens, 16 query heads of 128 numbers, two maps each, int8, causal:
+// 1.23 TFLOP) takes 1.23 ms, 1.0 PFLOP/s, 78% of what a large matrix product of the library
+// reaches (e4m3 1.17 ms; 64 numbers, 0.61 TFLOP, 0.68 to 0.72 ms).  Matrix instructions and
+// vector ones are each busy for a third to a half of the cycles, LDS for a quarter; what
+// counts is that they run beside one another.  Four wavefronts of 128 numbers, one on a
+// SIMD, 1.89 ms; eight without the scores ahead 1.47; with three operands on their way and
+// 12 registers spilled 1.38; pages and exponents in LDS instead, none spilled, 1.26, and the
+// sums at a raised wave priority 1.23.  64 numbers in steps of 32 tokens 0.81 ms (0.74 on
+// that card), eight wavefronts on tiles of 128 tokens the same as four on 64.
 constexpr int kTileKeys = 64;
-constexpr int kSubRows = 64;               // rows of a workgroup
+template <int DIM>
+constexpr int tile_span() {                // tokens of a step, in 32s
+    return DIM == 64 ? 2 : 1;
+}
+template <int DIM>
+constexpr int tile_waves() {
+    return DIM == 64 ? 4 : 8;
+}
 // Powers of two that a maximum may grow before the sums are rescaled; the
 // exponential itself makes 2^kTileRaise P, as in agft_kv_attend.
 constexpr int kSlack = 8;
@@ -605,33 +630,39 @@ struct TileLds {
     static constexpr int HEAD = kTileKeys * DIM * 2;       // a head's keys (or values) of a tile in 16 bits
     // operands of 1 KB, 16 bytes a lane; keys: [head][32 tokens][64 numbers][32][16], values: [16 tokens][32 numbers]
     __attribute__((aligned(16))) char tile[2][2][2 * HEAD];
-    float4 scale[4][2][4];                                 // by tile % 4, map: a block's factor of the scores, e, 2^-e
+    float4 scale[2][16];                                   // by map, block % 16: its factor of the scores, e, 2^-e
+    int2 look[tile_waves<DIM>()][2][64];                   // pages and exponents of the blocks that a wavefront fetches
     int last;
 };
 
 template <int FORM, int TYPE, int DIM>
 __device__ __forceinline__ void attend_many(const DiffArgs &p, TileLds<DIM> &lds, int block) {
-    constexpr int DG = DIM / kBlockDims, WIDE = 2 * DIM;
+    constexpr int DG = DIM / kBlockDims, WIDE = 2 * DIM, WAVES = tile_waves<DIM>(), BLOCKS = kTileKeys / kBlockTokens;
+    constexpr int SPAN = tile_span<DIM>(), SHIFT = 2 * SPAN;                           // of a step; blocks of it
+    constexpr int GROUPS = WAVES / 2, ROWS = 32 * GROUPS, SUBS = kTileRows / ROWS;   // of 32 rows; rows; workgroups of a tile
+    // heads of a block that a wavefront fetches: both, where there is a wavefront for each block
+    constexpr int HEADS = BLOCKS == WAVES ? 2 : 1;
+    static_assert(BLOCKS * 2 == WAVES * HEADS, "the wavefronts fetch a tile");
     using H = Half<TYPE>;
     const auto s_tile = lds.tile;
     const auto s_scale = lds.scale;
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-    const int h = lane >> 5, n = lane & 31, map = wave >> 1;
-    const int pair = block % p.heads, sub = block / p.heads & 1, place = block / p.heads >> 1;
+    const int h = lane >> 5, n = lane & 31, map = wave / GROUPS, own_rows = wave % GROUPS;
+    const int pair = block % p.heads, sub = block / p.heads % SUBS, place = block / p.heads / SUBS;
     if (place >= p.works[p.requests].items) return;
     const Item item = p.items[place];
     const int i = item.request;
     const int4 own = *reinterpret_cast<const int4 *>(p.works + i);
     const int len = p.works[i].length;
     const int first = own.z, granted = own.w, all_rows = (p.works[i + 1].start - first) * p.group;
-    const int row0 = item.tile * kTileRows + sub * kSubRows;
-    const int rows = all_rows - row0 < kSubRows ? all_rows - row0 : kSubRows;
+    const int row0 = item.tile * kTileRows + sub * ROWS;
+    const int rows = all_rows - row0 < ROWS ? all_rows - row0 : ROWS;
     if (rows <= 0) return;
     if (granted <= 0) {
-        if (item.part == 0) fill_rows<TYPE, WIDE>(p, first, pair, row0, rows, 0.0f, -INFINITY);
+        if (item.part == 0) fill_rows<TYPE, WIDE, 64 * WAVES>(p, first, pair, row0, rows, 0.0f, -INFINITY);
         return;
     }
-    const int past = len - granted, at_row = 32 * (wave & 1);
+    const int past = len - granted, at_row = 32 * own_rows;
     const bool busy = at_row < rows, row_here = at_row + n < rows;
     const int row = row_here ? row0 + at_row + n : row0 + rows - 1;
     const int limit = past + row / p.group + 1;            // keys that this lane's row sees
@@ -653,84 +684,108 @@ __device__ __forceinline__ void attend_many(const DiffArgs &p, TileLds<DIM> &lds
     }
     const float scale2 = p.scale * kLog2e;
     const int64_t side = (int64_t)p.page * DIM, page_bytes = (int64_t)p.heads * 4 * side;
-    const char *codes = p.codes + (int64_t)pair * 4 * side;
+    // what this wavefront fetches: a block, of one head or both
+    const int part = wave & (BLOCKS - 1), head = HEADS == 2 ? 0 : wave / BLOCKS;
+    const char *codes = p.codes + ((int64_t)pair * 2 + head) * 2 * side;
     const int sub_mask = (p.page >> 4) - 1;
 
-    // a lane per tile: the page and exponents of this wavefront's block of it
-    int id = 0;
-    int4 ee = make_int4(0, 0, 0, 0);
-    const auto look_up = [&](int t0) {
-        int b = (t0 + lane) * 4 + wave;
-        if (b >= blocks) b = blocks - 1;
+    // A step makes the scores of the tokens that follow beside the sums of those before
+    // them, so its operands are the values of tile t and the keys from a step on.  A lane
+    // per tile: page and exponents of this wavefront's blocks.
+    struct Look {
+        int id, exps;                                      // (exponents of keys and values, a byte each: they lie in -127..127)
+    };
+    constexpr bool KEPT = SPAN == 2;                       // in registers, where there is room; else in LDS
+    int2 kept[2];
+    const auto look_up = [&](int t0, int side_at) {
+        const int lane = lane_anew();
+        int b = (t0 + lane) * BLOCKS + part + (side_at == 0 ? SHIFT : 0);
+        b = b < 0 ? 0 : b >= blocks ? blocks - 1 : b;
         uint32_t z = (uint32_t)p.table[(int64_t)i * p.row_pages + ((b << 4) >> p.shift)];
         if (z >= (uint32_t)p.pages) z = (uint32_t)p.pages - 1;
-        id = (int)z;
-        ee = *reinterpret_cast<const int4 *>(p.exps + ((int64_t)id * p.heads + pair) * 4);
+        const int4 e = *reinterpret_cast<const int4 *>(p.exps + ((int64_t)z * p.heads + pair) * 4);
+        const int2 k = make_int2((int)z, (e.x & 255) | (e.y & 255) << 8 | (e.z & 255) << 16 | e.w << 24);
+        if constexpr (KEPT) kept[side_at] = k;
+        else lds.look[wave][side_at][lane] = k;
     };
-    // Step t makes the scores of tile t + 1 beside the sums of tile t, so its
-    // operands are the keys of one tile and the values of the one before.
-    uint4v ahead[2][2 * DG];                               // codes of the next step on their way
-    const char *values = codes;                            // this wavefront's values of the tile whose keys were last
-    const auto load = [&](const char *src, uint4v *dst) {
+    // (a wavefront reads what it wrote itself)
+    const auto look_at = [&](int t, int side_at) {
+        if constexpr (KEPT)
+            return Look{__builtin_amdgcn_readlane(kept[side_at].x, t & 63), __builtin_amdgcn_readlane(kept[side_at].y, t & 63)};
+        const int2 k = lds.look[wave][side_at][t & 63];
+        return Look{__builtin_amdgcn_readfirstlane(k.x), __builtin_amdgcn_readfirstlane(k.y)};
+    };
+    const auto block_at = [&](int t, int side_at) {
+        int b = t * BLOCKS + part + (side_at == 0 ? SHIFT : 0);
+        b = b < 0 ? 0 : b >= blocks ? blocks - 1 : b;
+        return codes + (int64_t)look_at(t, side_at).id * page_bytes + (b & sub_mask) * (16 * DIM) + side_at * side;
+    };
+    uint4v ahead[2][HEADS][DG];                            // codes of the next step on their way
+    const auto fetch = [&](int t, bool first) {
+        if ((t & 63) == 0 || first) look_up(t & ~63, 0), look_up(t & ~63, 1);
+        const char *k = block_at(t, 0), *v = block_at(t, 1);
+        const int at = lane_anew() * 16;
 #pragma unroll
-        for (int dg = 0; dg < 2 * DG; ++dg)
-            dst[dg] = *reinterpret_cast<const uint4v *>(src + (dg / DG) * 2 * side + (dg % DG) * kBlockBytes);
-    };
-    const auto fetch = [&](int t, bool both) {             // keys of tile t, values of tile t - 1
-        if (both) load(values, ahead[1]);
-        if ((t & 63) == 0 || !both) look_up(t & ~63);
-        int b = t * 4 + wave;
-        if (b >= blocks) b = blocks - 1;
-        const int64_t page_id = __builtin_amdgcn_readlane(id, t & 63);
-        const char *src = codes + page_id * page_bytes + (b & sub_mask) * (16 * DIM) + lane * 16;
-        load(src, ahead[0]);
-        values = src + side;
+        for (int a = 0; a < HEADS; ++a)
+#pragma unroll
+            for (int dg = 0; dg < DG; ++dg) {
+                ahead[0][a][dg] = *reinterpret_cast<const uint4v *>(k + a * 2 * side + dg * kBlockBytes + at);
+                ahead[1][a][dg] = *reinterpret_cast<const uint4v *>(v + a * 2 * side + dg * kBlockBytes + at);
+            }
     };
     // Entry 16 g + m of the codes to the lanes that take its numbers: token m's
     // numbers 16 g.. as a row of the left operand of the scores, numbers m, 16 + m,
     // .. of tokens 4 g.. as rows of the left operand of the sums.
-    const int g = lane >> 4, m16 = lane & 15;
-    const int to_key = (((wave >> 1) * DG * 4 + (g >> 1) * 2) * 64 + 32 * (g & 1) + 16 * (wave & 1) + m16) * 16;
-    const int to_value = (wave * DG * 4 * 64 + 32 * (g & 1) + 16 * (g >> 1) + m16) * 16;
-    float up[2] = {0.0f, 0.0f};                            // what the values of the tile whose keys were last are taken by
-    const auto stage = [&](int t, bool both) {             // what fetch(t, both) brought
-        const int buf = (t + 1) & 1;
+    const auto stage = [&](int t) {                        // what fetch(t) brought
+        const int buf = t & 1, lane = lane_anew(), g = lane >> 4, m16 = lane & 15;
+        const int to_key = head * TileLds<DIM>::HEAD +
+                           (((part >> 1) * DG * 4 + (g >> 1) * 2) * 64 + 32 * (g & 1) + 16 * (part & 1) + m16) * 16;
+        const int to_value = ((part * 2 + head) * DG * 2 * 64 + 32 * (g & 1) + 16 * (g >> 1) + m16) * 16;
 #pragma unroll
-        for (int dg = 0; dg < 2 * DG; ++dg) {
-            const uint4v k = ahead[0][dg];
+        for (int a = 0; a < HEADS; ++a)
 #pragma unroll
-            for (int e = 0; e < 2; ++e)
-                *reinterpret_cast<typename H::x8 *>(&s_tile[buf][0][to_key + (dg / DG) * TileLds<DIM>::HEAD +
-                                                                    ((dg % DG) * 4 + e) * 1024]) =
-                    H::template decode<FORM>(k[2 * e], k[2 * e + 1]);
-        }
-        const int ev0 = __builtin_amdgcn_readlane(ee.y, t & 63), ev1 = __builtin_amdgcn_readlane(ee.w, t & 63);
-        const int ev = ev0 > ev1 ? ev0 : ev1;
-        if (lane == (t & 63)) {
-            s_scale[t & 3][0][wave] = make_float4(scale2 * pow2(ee.x), (float)ev, pow2(-ev), 0.0f);
-            s_scale[t & 3][1][wave] = make_float4(scale2 * pow2(ee.z), (float)ev, pow2(-ev), 0.0f);
-        }
-        if (both) {
-            if (((t - 1) * 4 + wave + 1) * kBlockTokens > len) {
-                // codes past the request's tokens may be anything, NaN too
-                const int valid = len - ((t - 1) * kTileKeys + 16 * wave + 4 * g);
-                const uint32_t keep = valid >= 4 ? ~0u : valid <= 0 ? 0u : (1u << (8 * valid)) - 1u;
+            for (int dg = 0; dg < DG; ++dg) {
+                const uint4v k = ahead[0][a][dg];
 #pragma unroll
-                for (int dg = 0; dg < 2 * DG; ++dg) ahead[1][dg] &= keep;
+                for (int e = 0; e < 2; ++e)
+                    *reinterpret_cast<typename H::x8 *>(&s_tile[buf][0][to_key + a * TileLds<DIM>::HEAD + (dg * 4 + e) * 1024]) =
+                        H::template decode<FORM>(k[2 * e], k[2 * e + 1]);
             }
+        // (read by all lanes: what is made for one lane of them alone need not be there in the others)
+        const int x = look_at(t, 0).exps;
+        if (lane == 0) {
+            const int e0 = (int8_t)(x >> 8), e1 = x >> 24, e = e0 > e1 ? e0 : e1;
 #pragma unroll
-            for (int dg = 0; dg < 2 * DG; ++dg) {
+            for (int a = 0; a < HEADS; ++a)
+                s_scale[head + a][(t * BLOCKS + part + SHIFT) & 15] =
+                    make_float4(scale2 * pow2(head + a == 0 ? (int8_t)x : (int8_t)(x >> 16)), (float)e, pow2(-e), 0.0f);
+        }
+        if ((t * BLOCKS + part + 1) * kBlockTokens > len) {
+            // codes past the request's tokens may be anything, NaN too
+            const int valid = len - (t * kTileKeys + 16 * part + 4 * g);
+            const uint32_t keep = valid >= 4 ? ~0u : valid <= 0 ? 0u : (1u << (8 * valid)) - 1u;
+#pragma unroll
+            for (int a = 0; a < HEADS; ++a)
+#pragma unroll
+                for (int dg = 0; dg < DG; ++dg) ahead[1][a][dg] &= keep;
+        }
+        const int ve = look_at(t, 1).exps;
+        const int ev0 = (int8_t)(ve >> 8), ev1 = ve >> 24, ev = ev0 > ev1 ? ev0 : ev1;
+#pragma unroll
+        for (int a = 0; a < HEADS; ++a) {
+            const float up = value_scale<FORM>(head + a == 0 ? ev0 : ev1, ev);
+#pragma unroll
+            for (int dg = 0; dg < DG; ++dg) {
                 // words 0, 1 (2, 3) of the entries 16 g + m and 16 (g + 2) + m come
                 // together in the lower (upper) half: rows m (16 + m) of two operands
 #pragma unroll
                 for (int z = 0; z < 2; ++z) {
-                    const auto w = __builtin_amdgcn_permlane32_swap(ahead[1][dg][z], ahead[1][dg][2 + z], false, false);
-                    *reinterpret_cast<fp16x8 *>(&s_tile[buf][1][to_value + (dg * 2 + z) * 1024]) =
-                        decode_scaled<FORM>(w[0], w[1], up[dg / DG], up[dg / DG]);
+                    const auto w = __builtin_amdgcn_permlane32_swap(ahead[1][a][dg][z], ahead[1][a][dg][2 + z], false, false);
+                    *reinterpret_cast<fp16x8 *>(&s_tile[buf][1][to_value + ((a * DG + dg) * 2 + z) * 1024]) =
+                        decode_scaled<FORM>(w[0], w[1], up, up);
                 }
             }
         }
-        up[0] = value_scale<FORM>(ev0, ev), up[1] = value_scale<FORM>(ev1, ev);
     };
 
     float m = -INFINITY, l = 0.0f;
@@ -740,47 +795,69 @@ __device__ __forceinline__ void attend_many(const DiffArgs &p, TileLds<DIM> &lds
 #pragma unroll
         for (int j = 0; j < 16; ++j) o[c][j] = 0.0f;
 
-    float16v s[2];                                         // scores of the tile whose turn is next
+    constexpr int N = DG * 4;                              // instructions of 32 tokens' scores; their sums are 4 N
     const auto key_at = [&](int buf, int c) {
-        return reinterpret_cast<const uint4v *>(&s_tile[buf][0][map * TileLds<DIM>::HEAD + (c * 64 + lane) * 16]);
+        return *reinterpret_cast<const uint4v *>(&s_tile[buf][0][map * TileLds<DIM>::HEAD + (c * 64 + lane) * 16]);
     };
-    const auto scores = [&](int buf, float16v *z) {
-#pragma unroll
-        for (int half = 0; half < 2; ++half) {
-#pragma unroll
-            for (int j = 0; j < 16; ++j) z[half][j] = 0.0f;
-#pragma unroll
-            for (int c = 0; c < DG * 4; ++c)
-                z[half] = mfma32<TYPE>(__builtin_bit_cast(typename H::x8, *key_at(buf, half * DG * 4 + c)), q[c], z[half]);
-        }
-    };
-    // One step.  MASK: some row may not see all of the tile's keys.
-    const auto step = [&](int t, auto mask) {
+    float16v s[SPAN];                                      // scores of the tokens whose turn is next
+    // The tokens of a step: number `which` of tile t's.  MASK: some row may not see all of them.
+    const auto step = [&](int t, auto which, auto mask) {
         constexpr bool MASK = mask();
+        constexpr int AT = which() * SPAN;                 // in 32 tokens of the tile
         const int buf = t & 1;
-        const float off = m == -INFINITY ? 0.0f : m - (float)kTileRaise;
-        float pow_back[4];
+        // Matrix instructions in the order of their operands in LDS, each of which is read
+        // AHEAD instructions before its use: the next scores', then these tokens' sums'.
+        constexpr int SCORES = SPAN * N, ALL = 3 * SCORES, AHEAD = SPAN == 2 ? 4 : 2;
+        // scores beside the search for the maximum; exponentials beside the others (the rest: beside the sums)
+        constexpr int EARLY = SPAN == 2 ? 0 : 3, BESIDE = SPAN == 2 ? 32 : 8;
+        const auto operand = [&](int c) {
+            return c < SCORES ? key_at(buf, (AT + c % SPAN) * N + c / SPAN)
+                              : *reinterpret_cast<const uint4v *>(&s_tile[buf][1][((AT * 2 * N + c - SCORES) * 64 + lane) * 16]);
+        };
+        uint4v ring[AHEAD];
 #pragma unroll
-        for (int b = 0; b < 4; ++b) {
-            const float4 f = s_scale[t & 3][map][b];
+        for (int c = 0; c < AHEAD; ++c) ring[c] = operand(c);
+        float16v z[SPAN];
+#pragma unroll
+        for (int w = 0; w < SPAN; ++w)
+#pragma unroll
+            for (int j = 0; j < 16; ++j) z[w][j] = 0.0f;
+        const auto score = [&](int c) {
+            z[c % SPAN] = mfma32<TYPE>(__builtin_bit_cast(typename H::x8, ring[c % AHEAD]), q[c / SPAN], z[c % SPAN]);
+            ring[c % AHEAD] = operand(c + AHEAD);
+        };
+        if constexpr (EARLY > 0) score(0);
+        __builtin_amdgcn_sched_barrier(0);
+        const float off = m == -INFINITY ? 0.0f : m - (float)kTileRaise;
+        float pow_back[2 * SPAN];
+#pragma unroll
+        for (int b = 0; b < 2 * SPAN; ++b) {
+            const float4 f = s_scale[map][(t * BLOCKS + 2 * AT + b) & 15];
             const float ev = f.y - off;
             pow_back[b] = f.z;
 #pragma unroll
-            for (int j = 0; j < 8; ++j) s[b >> 1][8 * (b & 1) + j] = fmaf(s[b >> 1][8 * (b & 1) + j], f.x, ev);
+            for (int j = 8 * (b & 1); j < 8 * (b & 1) + 8; ++j) s[b >> 1][j] = fmaf(s[b >> 1][j], f.x, ev);
         }
         if constexpr (MASK) {
+            const int sees = limit - t * kTileKeys - 32 * AT - 4 * (lane_anew() >> 5);
 #pragma unroll
-            for (int half = 0; half < 2; ++half)
+            for (int w = 0; w < SPAN; ++w)
 #pragma unroll
                 for (int j = 0; j < 16; ++j)
-                    if (t * kTileKeys + 32 * half + 8 * (j >> 2) + 4 * h + (j & 3) >= limit) s[half][j] = -INFINITY;
+                    if (32 * w + 8 * (j >> 2) + (j & 3) >= sees) s[w][j] = -INFINITY;
         }
+        __builtin_amdgcn_sched_barrier(0);
+        if constexpr (EARLY > 1) score(1);
+        __builtin_amdgcn_sched_barrier(0);
         float top = s[0][0];
 #pragma unroll
-        for (int half = 0; half < 2; ++half)
+        for (int w = 0; w < SPAN; ++w)
 #pragma unroll
-            for (int j = 0; j < 16; ++j) top = fmaxf(top, s[half][j]);
+            for (int j = 0; j < 16; ++j) top = fmaxf(top, s[w][j]);
         top = halves_max(top);
+        __builtin_amdgcn_sched_barrier(0);
+        if constexpr (EARLY > 2) score(2);
+        __builtin_amdgcn_sched_barrier(0);
         // the maximum that the sums are relative to follows the real one at some distance
         if (__builtin_expect(__any(top > (float)kRaise || m == -INFINITY), 0)) {
             const float m1 = (fmaxf(m, off + top) - (float)kTileRaise) + (float)kTileRaise;
@@ -792,91 +869,98 @@ __device__ __forceinline__ void attend_many(const DiffArgs &p, TileLds<DIM> &lds
 #pragma unroll
             for (int c = 0; c < DG * 4; ++c) o[c] *= fall;
 #pragma unroll
-            for (int half = 0; half < 2; ++half) s[half] += shift;
+            for (int w = 0; w < SPAN; ++w) s[w] += shift;
         }
-        // Matrix instructions in the order of their operands in LDS, each of which
-        // is read AHEAD instructions before its use; the scores' instructions
-        // alternate between the two halves of the tile, with this tile's
-        // exponentials between them.
-        constexpr int N = DG * 8, ALL = DG * 24, AHEAD = 4;      // instructions of the scores, and with the sums
-        const auto operand = [&](int c) {
-            return c < N ? *key_at(buf, (c & 1) * (N / 2) + (c >> 1))
-                         : *reinterpret_cast<const uint4v *>(&s_tile[buf][1][((c - N) * 64 + lane) * 16]);
-        };
-        uint4v ring[AHEAD];
-        float16v z[2];
-#pragma unroll
-        for (int c = 0; c < AHEAD; ++c) ring[c] = operand(c);
-#pragma unroll
-        for (int half = 0; half < 2; ++half)
-#pragma unroll
-            for (int j = 0; j < 16; ++j) z[half][j] = 0.0f;
-        fp16x8 pr[4];
+        fp16x8 pr[2 * SPAN];
         float sum = 0.0f;
+        const auto exponential = [&](int x) {
+            const float e = __builtin_amdgcn_exp2f(s[x >> 4][x & 15]);
+            sum = (x & 7) == 0 ? e : sum + e;
+            pr[x >> 3][x & 7] = (_Float16)e;
+            if ((x & 7) == 7) l = fmaf(sum, pow_back[x >> 3], l);
+        };
 #pragma unroll
-        for (int c = 0; c < N; ++c) {
-            z[c & 1] = mfma32<TYPE>(__builtin_bit_cast(typename H::x8, ring[c % AHEAD]), q[c >> 1], z[c & 1]);
-            ring[c % AHEAD] = operand(c + AHEAD);
+        for (int c = EARLY; c < SCORES; ++c) {
+            score(c);
 #pragma unroll
-            for (int x = c * 32 / N; x < (c + 1) * 32 / N; ++x) {
-                const float e = __builtin_amdgcn_exp2f(s[x >> 4][x & 15]);
-                sum = (x & 7) == 0 ? e : sum + e;
-                pr[x >> 3][x & 7] = (_Float16)e;
-                if ((x & 7) == 7) l = fmaf(sum, pow_back[x >> 3], l);
+            for (int x = (c - EARLY) * BESIDE / (SCORES - EARLY); x < (c - EARLY + 1) * BESIDE / (SCORES - EARLY); ++x) exponential(x);
+            __builtin_amdgcn_sched_barrier(0);
+        }
+        if constexpr (SPAN == 1) __builtin_amdgcn_s_setprio(1);
+#pragma unroll
+        for (int c = SCORES; c < ALL; ++c) {
+            const int b = (c - SCORES) / N, y = (c - SCORES) % N;
+            o[y] = mfma32<AGFT_KV_FP16>(__builtin_bit_cast(fp16x8, ring[c % AHEAD]), pr[b], o[y]);
+            if (c + AHEAD < ALL) ring[c % AHEAD] = operand(c + AHEAD);
+            if (BESIDE < 16 * SPAN && b == 0) {
+#pragma unroll
+                for (int x = 8 + y * 8 / N; x < 8 + (y + 1) * 8 / N; ++x) exponential(x);
             }
             __builtin_amdgcn_sched_barrier(0);
         }
 #pragma unroll
-        for (int c = N; c < ALL; ++c) {
-            const int b = (c - N) / (DG * 4), y = (c - N) % (DG * 4);
-            o[y] = mfma32<AGFT_KV_FP16>(__builtin_bit_cast(fp16x8, ring[c % AHEAD]), pr[b], o[y]);
-            if (c + AHEAD < ALL) ring[c % AHEAD] = operand(c + AHEAD);
-            __builtin_amdgcn_sched_barrier(0);
-        }
-        s[0] = z[0], s[1] = z[1];
+        for (int w = 0; w < SPAN; ++w) s[w] = z[w];
+        if constexpr (SPAN == 1) __builtin_amdgcn_s_setprio(0);
+    };
+    const auto steps = [&](int t, auto mask) {
+        step(t, std::integral_constant<int, 0>{}, mask);
+        if constexpr (SPAN == 1) step(t, std::integral_constant<int, 1>{}, mask);
     };
 
-    fetch(begin, false);
-    stage(begin, false);
-    fetch(begin + 1, true);
+    fetch(begin - 1, true);
+    stage(begin - 1);
+    fetch(begin, true);
     __syncthreads();
-    if (busy) scores((begin + 1) & 1, s);                  // of the first tile, whose keys lie in the buffer of the step before
-    stage(begin + 1, true);
+    if (busy) {                                            // the first tokens' scores: keys of the step before
+#pragma unroll
+        for (int w = 0; w < SPAN; ++w) {
+#pragma unroll
+            for (int j = 0; j < 16; ++j) s[w][j] = 0.0f;
+#pragma unroll
+            for (int c = 0; c < N; ++c)
+                s[w] = mfma32<TYPE>(__builtin_bit_cast(typename H::x8, key_at((begin - 1) & 1, (2 - SPAN + w) * N + c)), q[c], s[w]);
+        }
+    }
+    stage(begin);
     if (!busy)                                             // no rows of its own: only fetches
         for (int t = begin; t < tiles; ++t) {
             __syncthreads();
-            if (t + 1 < tiles) fetch(t + 2, true), stage(t + 2, true);
+            if (t + 1 < tiles) fetch(t + 1, false), stage(t + 1);
         }
     int t = busy ? begin : tiles;
     for (; t < whole; ++t) {
         __syncthreads();                                   // this step's operands are in LDS, and the other buffer is read
-        if (t + 1 < tiles) fetch(t + 2, true);
-        step(t, std::false_type{});
-        if (t + 1 < tiles) stage(t + 2, true);
+        if (t + 1 < tiles) fetch(t + 1, false);
+        steps(t, std::false_type{});
+        if (t + 1 < tiles) stage(t + 1);
     }
     for (; t < tiles; ++t) {
         __syncthreads();
-        if (t + 1 < tiles) fetch(t + 2, true);
-        step(t, std::true_type{});
-        if (t + 1 < tiles) stage(t + 2, true);
+        if (t + 1 < tiles) fetch(t + 1, false);
+        steps(t, std::true_type{});
+        if (t + 1 < tiles) stage(t + 1);
     }
     l = halves_sum(l);
-    // rows 8 z + 4 h.. of O^T: numbers 64 dg + 32 (z / 2) + 16 T + ..
-    const auto number = [&](int c, int z) { return 64 * (c >> 1) + 32 * (z >> 1) + 16 * (c & 1) + 8 * (z & 1) + 4 * h; };
+    // (made anew from the lane: not kept through the loop)
+    const int lane1 = lane_anew(), h1 = lane1 >> 5, n1 = lane1 & 31;
+    const bool row_here1 = at_row + n1 < rows;
+    const int row1 = row_here1 ? row0 + at_row + n1 : row0 + rows - 1;
+    // rows 8 z + 4 h1.. of O^T: numbers 64 dg + 32 (z / 2) + 16 T + ..
+    const auto number = [&](int c, int z) { return 64 * (c >> 1) + 32 * (z >> 1) + 16 * (c & 1) + 8 * (z & 1) + 4 * h1; };
     if (item.parts > 1) {
         // each part leaves its sums as its lanes hold them, and the last to arrive joins them the same way
-        constexpr int64_t PART = 2 * kSubRows * (WIDE + 2);
-        const int64_t stride = (int64_t)p.heads * 2 * PART;
-        const int64_t row_of = (int64_t)(place - item.part) * p.heads * 2 + pair * 2 + sub;
+        constexpr int64_t PART = 2 * ROWS * (WIDE + 2);
+        const int64_t stride = p.heads * SUBS * PART;
+        const int64_t row_of = ((int64_t)(place - item.part) * p.heads + pair) * SUBS + sub;
         float *parts = p.partial + (int64_t)kFewGroups * 2 * piece_floats<DIM>() + row_of * PART;
-        const int mine = wave * (32 * WIDE) + lane * 2, own_row = 2 * kSubRows * WIDE + 32 * wave + n;
+        const int mine = wave * (32 * WIDE) + lane1 * 2, own_row = 2 * ROWS * WIDE + 32 * wave + n1;
         if (busy) {
             float *at = parts + item.part * stride;
 #pragma unroll
             for (int c = 0; c < DG * 4; ++c)
 #pragma unroll
                 for (int z = 0; z < 8; ++z) put2(at + mine + (c * 8 + z) * 128, o[c][2 * z], o[c][2 * z + 1]);
-            if (h == 0) put(at + own_row, m), put(at + own_row + 2 * kSubRows, l);
+            if (h1 == 0) put(at + own_row, m), put(at + own_row + 2 * ROWS, l);
         }
         if (!last_to_arrive(p.arrived + 3 * kFewGroups + row_of, item.parts, &lds.last)) return;
         if (busy) {
@@ -888,7 +972,7 @@ __device__ __forceinline__ void attend_many(const DiffArgs &p, TileLds<DIM> &lds
                 for (int j = 0; j < 16; ++j) o[c][j] = 0.0f;
             for (int w = 0; w < item.parts; ++w) {
                 const float *at = parts + w * stride;
-                const float mw = get(at + own_row), lw = get(at + own_row + 2 * kSubRows);
+                const float mw = get(at + own_row), lw = get(at + own_row + 2 * ROWS);
                 const float f = mw == -INFINITY ? 0.0f : exp2f(mw - m);
                 l = fmaf(lw, f, l);
 #pragma unroll
@@ -905,11 +989,11 @@ __device__ __forceinline__ void attend_many(const DiffArgs &p, TileLds<DIM> &lds
     }
     // the second map's sums to the first's wavefronts, as the lanes hold them
     __syncthreads();
-    float4v *other = reinterpret_cast<float4v *>(&s_tile[0][0][0]) + (wave & 1) * (DG * 16 * 64) + lane;
-    static_assert(sizeof(lds.tile) >= 2 * DG * 16 * 64 * sizeof(float4v), "two wavefronts' sums fit where the tiles were");
+    float4v *other = reinterpret_cast<float4v *>(&s_tile[0][0][0]) + own_rows * (DG * 16 * 64) + lane1;
+    static_assert(sizeof(lds.tile) >= GROUPS * DG * 16 * 64 * sizeof(float4v), "a map's sums fit where the tiles were");
     float f = l > 0.0f || l != l ? pow2(-lift<FORM>()) / l : 0.0f;
     if (busy && map == 1) {
-        f *= lambda_of(p, first, pair, row);
+        f *= lambda_of(p, first, pair, row1);
 #pragma unroll
         for (int c = 0; c < DG * 4; ++c)
 #pragma unroll
@@ -917,8 +1001,8 @@ __device__ __forceinline__ void attend_many(const DiffArgs &p, TileLds<DIM> &lds
                 other[(c * 4 + z) * 64] = (float4v){o[c][4 * z], o[c][4 * z + 1], o[c][4 * z + 2], o[c][4 * z + 3]} * f;
     }
     __syncthreads();
-    if (!row_here) return;
-    if (h == 0) store_lse(p, first, pair, map, row, m, l * pow2(-kTileRaise));
+    if (!row_here1) return;
+    if (h1 == 0) store_lse(p, first, pair, map, row1, m, l * pow2(-kTileRaise));
     if (map == 1) return;
     float squares = 0.0f;
 #pragma unroll
@@ -936,7 +1020,7 @@ __device__ __forceinline__ void attend_many(const DiffArgs &p, TileLds<DIM> &lds
 #pragma unroll
         for (int z = 0; z < 4; ++z) {
             const int d = number(c, z);
-            store4<TYPE>(p, first, pair, row, d,
+            store4<TYPE>(p, first, pair, row1, d,
                          (float4v){o[c][4 * z], o[c][4 * z + 1], o[c][4 * z + 2], o[c][4 * z + 3]} * by * weight_at(p, d));
         }
 }
@@ -946,20 +1030,28 @@ __device__ __forceinline__ void attend_many(const DiffArgs &p, TileLds<DIM> &lds
 template <int FORM, int TYPE, int DIM>
 __global__ __launch_bounds__(64 * kFewWaves, few_groups<DIM>() / 256) void agft_diff_few_kernel(DiffArgs p) {
     __shared__ FewLds<DIM> lds;
-    attend_few<FORM, TYPE, DIM, false>(p, lds, blockIdx.x);
+    attend_few<FORM, TYPE, DIM>(p, lds, blockIdx.x);
 }
 
-// Tiles of many rows, in one launch with the few ones' workgroups where a request
-// may have more than kMidRows.
+// Tiles of many rows; of 64 numbers in one launch with the few ones' workgroups, which
+// are as large (chunks of 256 to 1,024 tokens beside single ones: 124 us, 141 apart).
+template <int DIM>
+constexpr bool one_launch() {
+    return tile_waves<DIM>() == kFewWaves;
+}
 template <int FORM, int TYPE, int DIM>
-__global__ __launch_bounds__(64 * kTileWaves, DIM > 64 ? 1 : 2) void agft_diff_tile_kernel(DiffArgs p) {
-    static_assert(few_groups<DIM>() <= kFewGroups && kFewWaves == kTileWaves, "one workgroup size");
-    __shared__ union {
-        FewLds<DIM> few;
-        TileLds<DIM> many;
-    } lds;
-    if ((int)blockIdx.x < p.few_blocks) attend_few<FORM, TYPE, DIM, true>(p, lds.few, blockIdx.x);
-    else attend_many<FORM, TYPE, DIM>(p, lds.many, blockIdx.x - p.few_blocks);
+__global__ __launch_bounds__(64 * tile_waves<DIM>(), 2) void agft_diff_tile_kernel(DiffArgs p) {
+    if constexpr (one_launch<DIM>()) {
+        __shared__ union {
+            FewLds<DIM> few;
+            TileLds<DIM> many;
+        } lds;
+        if ((int)blockIdx.x < p.few_blocks) attend_few<FORM, TYPE, DIM>(p, lds.few, blockIdx.x);
+        else attend_many<FORM, TYPE, DIM>(p, lds.many, blockIdx.x - p.few_blocks);
+    } else {
+        __shared__ TileLds<DIM> lds;
+        attend_many<FORM, TYPE, DIM>(p, lds, blockIdx.x);
+    }
 }
 
 inline int diff_status(const agft_kv_config *c) {
@@ -980,7 +1072,7 @@ size_t agft_diff_attend_bytes(const agft_kv_config *cfg, int32_t max_tokens) {
     const int64_t items = item_cap(cfg, max_tokens) * cfg->heads;
     const size_t parts = (size_t)(items < kTileParts ? items : kTileParts);
     const size_t piece = (size_t)(cfg->dim == 64 ? piece_floats<64>() : piece_floats<128>());
-    return align_up(((size_t)kFewGroups * 2 * piece + parts * 2 * kSubRows * (2 * (size_t)cfg->dim + 2)) * sizeof(float));
+    return align_up(((size_t)kFewGroups * 2 * piece + parts * kTileRows * (2 * (size_t)cfg->dim + 2)) * sizeof(float));
 }
 
 int agft_diff_attend(const agft_kv_config *cfg, const void *d_cache, size_t cache_bytes, const void *d_tables,
@@ -1023,19 +1115,21 @@ int agft_diff_attend(const agft_kv_config *cfg, const void *d_cache, size_t cach
     p.page = cfg->page, p.shift = log2_of(cfg->page), p.heads = cfg->heads / 2, p.group = cfg->group;
     p.lambda = diff->lambda, p.lambda_token = diff->lambda_token, p.lambda_head = diff->lambda_head;
     p.weight = diff->weight, p.eps = diff->eps, p.gain = diff->gain;
-    const int64_t tile_groups = item_cap(cfg, max_tokens) * cfg->heads;     // two of a tile and pair
-    if (tile_groups > INT32_MAX - kFewGroups) return AGFT_E_INVAL;
+    const int64_t tile_groups = item_cap(cfg, max_tokens) * p.heads;
+    if (tile_groups > (INT32_MAX - kFewGroups) / 2) return AGFT_E_INVAL;
     const auto go = [&](auto form, auto type, auto dim) {
         const hipStream_t hs = static_cast<hipStream_t>(stream);
         const int64_t rows = (int64_t)max_new * cfg->group;
-        p.few_blocks = rows > kMidRows ? few_groups<dim()>() : 0;
+        const bool beside = one_launch<dim()>() && rows > kMidRows;
         p.alone = rows <= kFewRows;
-        if (rows <= kMidRows) {
+        p.few_blocks = beside ? few_groups<dim()>() : 0;
+        if (!beside) {
             agft_diff_few_kernel<form(), type(), dim()><<<few_groups<dim()>(), 64 * kFewWaves, 0, hs>>>(p);
             const int code = launched();
             if (code != AGFT_OK || rows <= kFewRows) return code;
         }
-        agft_diff_tile_kernel<form(), type(), dim()><<<(unsigned)(p.few_blocks + tile_groups), 64 * kTileWaves, 0, hs>>>(p);
+        constexpr int waves = tile_waves<dim()>(), subs = 8 / waves;     // workgroups of a tile
+        agft_diff_tile_kernel<form(), type(), dim()><<<(unsigned)(p.few_blocks + tile_groups * subs), 64 * waves, 0, hs>>>(p);
         return launched();
     };
     const auto dims = [&](auto form, auto type) {
