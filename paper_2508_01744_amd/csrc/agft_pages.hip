@@ -120,6 +120,27 @@ __device__ __forceinline__ int32_t before_me(int32_t x, int32_t *all, int32_t *l
     return before;
 }
 
+// N sums over all threads.
+template <int THREADS, int N>
+__device__ __forceinline__ void sums_of(int32_t *x, int32_t *lds) {
+    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+#pragma unroll
+    for (int s = 1; s < 64; s *= 2)
+#pragma unroll
+        for (int k = 0; k < N; ++k) x[k] += __shfl_xor(x[k], s, 64);
+    __syncthreads();                        // (an earlier scan's sums have been read)
+#pragma unroll
+    for (int k = 0; k < N; ++k)
+        if (lane == 0) lds[k * (THREADS / 64) + wave] = x[k];
+    __syncthreads();
+#pragma unroll
+    for (int k = 0; k < N; ++k) {
+        x[k] = 0;
+#pragma unroll
+        for (int w = 0; w < THREADS / 64; ++w) x[k] += lds[k * (THREADS / 64) + w];
+    }
+}
+
 // Lengths before and after an edit that leaves them.
 __device__ __forceinline__ void keep_lengths(const EditArgs &p, const uint32_t *but) {
     for (int32_t i = blockIdx.x * blockDim.x + threadIdx.x; i < p.requests; i += gridDim.x * blockDim.x) {
@@ -418,15 +439,13 @@ __global__ __launch_bounds__(kThreads) void agft_pages_trim_give_kernel(EditArgs
     const int32_t head = p.counters[kHead], free_pages = free_of(p), extra = p.counters[kExtra];
     trim_chunk<true>(p, extra != 0, lds);
     const int32_t total = lds.at[kChunkRequests];
-    int32_t part[4] = {};                   // given back before this chunk, and in all; refused; let go
+    int32_t sum[4] = {};                    // given back before this chunk, and in all; refused; let go
     for (int32_t k = threadIdx.x; k < (int32_t)gridDim.x; k += kThreads) {
         const int32_t g = p.sums[k];
-        if (k < (int32_t)blockIdx.x) part[0] += g;
-        part[1] += g, part[2] += p.sums[kChunks + k], part[3] += p.sums[2 * kChunks + k];
+        if (k < (int32_t)blockIdx.x) sum[0] += g;
+        sum[1] += g, sum[2] += p.sums[kChunks + k], sum[3] += p.sums[2 * kChunks + k];
     }
-    int32_t sum[4];
-#pragma unroll
-    for (int z = 0; z < 4; ++z) before_me<kThreads>(part[z], &sum[z], lds.sums);
+    sums_of<kThreads, 4>(sum, lds.sums);
     if (blockIdx.x == 0 && threadIdx.x == 0) {
         const int32_t room = p.pages - free_pages, given = sum[1] < room ? sum[1] : room;
         int32_t *c = p.out;
@@ -569,17 +588,16 @@ __global__ __launch_bounds__(kChunkWords) void agft_pages_bits_sum_kernel(EditAr
 }
 
 __global__ __launch_bounds__(1024) void agft_pages_bits_move_kernel(EditArgs p) {
-    __shared__ int32_t s_sums[16];
+    __shared__ int32_t s_sums[3 * 16];
     const int32_t n = held_pages(p), chunk = blockIdx.x, chunk_n = n / (32 * kChunkWords);
-    int32_t part[3] = {}, sum[3];              // free pages before this chunk, before n's, and in all
+    int32_t sum[3] = {};                       // free pages before this chunk, before n's, and in all
     for (int32_t k = threadIdx.x; k < (int32_t)gridDim.x; k += 1024) {
         const int32_t s = p.sums[k];
-        if (k < chunk) part[0] += s;
-        if (k < chunk_n) part[1] += s;
-        part[2] += s;
+        if (k < chunk) sum[0] += s;
+        if (k < chunk_n) sum[1] += s;
+        sum[2] += s;
     }
-#pragma unroll
-    for (int z = 0; z < 3; ++z) before_me<1024>(part[z], &sum[z], s_sums);
+    sums_of<1024, 3>(sum, s_sums);
     const int32_t below = n == p.pages ? sum[2] : sum[1] + free_below(p.bits[n >> 5], p.prefix[n >> 5], n);
     const int32_t moves = compact_moves(p, n, below, sum[2]);
     const int64_t first = (int64_t)chunk * 32 * kChunkWords;
@@ -652,8 +670,14 @@ __global__ __launch_bounds__(kThreads) void agft_pages_commit_kernel(EditArgs p)
 // ---- copies ----
 //
 // Memory's rate: every byte read once and written once, 16 bytes a lane, four of
-// them on their way, a workgroup a piece of a page at a time.
+// them on their way (2 / 8: 637 / 623 us for 620), a workgroup a piece of a page at a time.
+// Stores go past the caches, where nobody reads them soon (11,964 pages of 128 KB 608 us,
+// 5.2 TB/s, a large copy of the library's 4.7; 1,177 of 32 KB 13.7 us for 15.8), loads do
+// not (16.7).  Workgroups up to 16,384 (2,048 / 4,096 / 16,384 / 65,536: 627 / 620 / 609 /
+// 602; those without a move have to come and go).
+typedef uint32_t uint4v __attribute__((ext_vector_type(4)));
 constexpr int kCopyAhead = 4;
+constexpr int kCopyGroups = 16384;
 constexpr int kCopyBytes = kThreads * 16 * kCopyAhead;
 
 __global__ __launch_bounds__(kThreads) void agft_pages_copy_kernel(char *codes, int32_t *exps, const int32_t *counters,
@@ -667,13 +691,14 @@ __global__ __launch_bounds__(kThreads) void agft_pages_copy_kernel(char *codes, 
         const int64_t at = (int64_t)part * kCopyBytes + threadIdx.x * 16;
         const char *from = codes + m.x * page_bytes + at;
         char *to = codes + m.y * page_bytes + at;
-        uint4 v[kCopyAhead];
+        uint4v v[kCopyAhead];
 #pragma unroll
         for (int z = 0; z < kCopyAhead; ++z)
-            v[z] = at + z * kThreads * 16 < page_bytes ? *reinterpret_cast<const uint4 *>(from + z * kThreads * 16) : uint4{};
+            v[z] = at + z * kThreads * 16 < page_bytes ? *reinterpret_cast<const uint4v *>(from + z * kThreads * 16) : (uint4v){};
 #pragma unroll
         for (int z = 0; z < kCopyAhead; ++z)
-            if (at + z * kThreads * 16 < page_bytes) *reinterpret_cast<uint4 *>(to + z * kThreads * 16) = v[z];
+            if (at + z * kThreads * 16 < page_bytes)
+                __builtin_nontemporal_store(v[z], reinterpret_cast<uint4v *>(to + z * kThreads * 16));
         if (part == 0)
             for (int k = threadIdx.x; k < page_exps; k += kThreads)
                 exps[(int64_t)m.y * page_exps + k] = exps[(int64_t)m.x * page_exps + k];
@@ -823,7 +848,7 @@ int agft_pages_copy(const agft_kv_config *cfg, void *d_cache, size_t cache_bytes
     const int32_t parts = (int32_t)((page_bytes + kCopyBytes - 1) / kCopyBytes);
     const int64_t all = (int64_t)max_moves * parts;
     char *base = static_cast<char *>(d_cache);
-    agft_pages_copy_kernel<<<dim3((unsigned)(all < 4096 ? all : 4096)), kThreads, 0, static_cast<hipStream_t>(stream)>>>(
+    agft_pages_copy_kernel<<<dim3((unsigned)(all < kCopyGroups ? all : kCopyGroups)), kThreads, 0, static_cast<hipStream_t>(stream)>>>(
         base + C.codes, reinterpret_cast<int32_t *>(base + C.exps), ev.counters, reinterpret_cast<const int2 *>(ev.moves),
         max_moves, page_bytes, cfg->heads * 2, parts, cfg->pages);
     return launched();
