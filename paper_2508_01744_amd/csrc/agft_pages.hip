@@ -670,11 +670,11 @@ __global__ __launch_bounds__(kThreads) void agft_pages_commit_kernel(EditArgs p)
 // ---- copies ----
 //
 // Memory's rate: every byte read once and written once, 16 bytes a lane, four of
-// them on their way (2 / 8: 637 / 623 us for 620), a workgroup a piece of a page at a time.
-// Stores go past the caches, where nobody reads them soon (11,964 pages of 128 KB 608 us,
-// 5.2 TB/s, a large copy of the library's 4.7; 1,177 of 32 KB 13.7 us for 15.8), loads do
-// not (16.7).  Workgroups up to 16,384 (2,048 / 4,096 / 16,384 / 65,536: 627 / 620 / 609 /
-// 602; those without a move have to come and go).
+// them on their way (2 / 8: 637 / 623 us for 620), a workgroup a piece of a page at a time:
+// 11,964 pages of 128 KB 609 us, 5.2 TB/s (a large copy of the library's 4.7), 1,177 of 32
+// KB 15.8 us.  Workgroups up to 16,384 (2,048 / 4,096 / 16,384 / 65,536: 627 / 620 / 609 /
+// 602; those without a move have to come and go).  Stores past the caches save 2 us of the
+// 15.8 and cost whoever reads the pages next 14.
 typedef uint32_t uint4v __attribute__((ext_vector_type(4)));
 constexpr int kCopyAhead = 4;
 constexpr int kCopyGroups = 16384;
@@ -698,7 +698,7 @@ __global__ __launch_bounds__(kThreads) void agft_pages_copy_kernel(char *codes, 
 #pragma unroll
         for (int z = 0; z < kCopyAhead; ++z)
             if (at + z * kThreads * 16 < page_bytes)
-                __builtin_nontemporal_store(v[z], reinterpret_cast<uint4v *>(to + z * kThreads * 16));
+                *reinterpret_cast<uint4v *>(to + z * kThreads * 16) = v[z];
         if (part == 0)
             for (int k = threadIdx.x; k < page_exps; k += kThreads)
                 exps[(int64_t)m.y * page_exps + k] = exps[(int64_t)m.x * page_exps + k];

@@ -134,7 +134,7 @@ class _OnStream:
         return self._empty(nbytes, dtype=torch.uint8)
 
     def _ints(self, t, shape, what):
-        if t.device != self.device or t.dtype != torch.int32 or not t.is_contiguous() or tuple(t.shape) != shape:
+        if t.get_device() != self._index or t.dtype != torch.int32 or t.shape != shape or not t.is_contiguous():
             raise ValueError(f"{what} must be a contiguous int32 tensor {list(shape)} on {self.device}")
 
 
@@ -326,12 +326,12 @@ class KvTables(_OnStream):
         """Plan an edit with room for `moves` moves."""
         if edit is None:
             edit = KvEdit(self.cfg, moves, self.device, self.stream)
-        elif edit.device != self.device or edit._shape is not self._shape:
+        elif edit._shape is not self._shape or edit.device != self.device:
             raise ValueError("edit of another device or configuration")
-        code = getattr(self._lib, "agft_pages_" + name)(self._cfg, self.ptr, self.nbytes, *args, edit.ptr, edit.nbytes,
+        code = getattr(self._lib, name)(self._cfg, self.ptr, self.nbytes, *args, edit.ptr, edit.nbytes,
                                                         edit.max_moves, self._s())
         if code != L.AGFT_OK:
-            L.check("agft_pages_" + name, code)
+            L.check(name, code)
         edit.planned, edit._by, edit._when = True, self, self._changes
         return edit
 
@@ -341,15 +341,17 @@ class KvTables(_OnStream):
         partly filled last one is copied (KvCache.copy).  dst[j] holds nothing and
         is named once; edit.granted[j] is 0 where that is not so, or no page is
         free.  edit: a KvEdit of max_moves n to write again."""
-        n = src.numel()
-        if src.dim() != 1 or not 1 <= n <= 65536:
+        shape = src.shape
+        n = shape[0] if len(shape) == 1 else 0
+        if not 1 <= n <= 65536:
             raise ValueError("src must name 1 to 65536 requests")
-        for t, what in ((src, "src"), (dst, "dst"), (tokens, "tokens")):
-            if t is not None:
-                self._ints(t, (n,), what)
+        self._ints(src, shape, "src")
+        self._ints(dst, shape, "dst")
+        if tokens is not None:
+            self._ints(tokens, shape, "tokens")
         if edit is not None and edit.max_moves != n:
             raise ValueError(f"edit is for {edit.max_moves} moves, not {n}")
-        return self._edit("fork", edit, n, src.data_ptr(), dst.data_ptr(), None if tokens is None else tokens.data_ptr(), n)
+        return self._edit("agft_pages_fork", edit, n, src.data_ptr(), dst.data_ptr(), None if tokens is None else tokens.data_ptr(), n)
 
     def trim(self, keep, edit=None):
         """Plan that request i keeps its first keep[i] tokens (int32 [R]; 0 ends it,
@@ -357,7 +359,7 @@ class KvTables(_OnStream):
         owner are free after the commit.  A request that would end inside a page
         with other owners stays as it is and counts as refused.  No pages to copy."""
         self._ints(keep, (self.cfg.requests,), "keep")
-        return self._edit("trim", edit, 1, keep.data_ptr())
+        return self._edit("agft_pages_trim", edit, 1, keep.data_ptr())
 
     def compact(self, edit=None):
         """Plan that the held pages go to the pool's lower end: afterwards the free
@@ -367,7 +369,7 @@ class KvTables(_OnStream):
         moves = max(1, self.cfg.pages // 2)
         if edit is not None and edit.max_moves != moves:
             raise ValueError(f"edit is for {edit.max_moves} moves, not {moves}")
-        return self._edit("compact", edit, moves)
+        return self._edit("agft_pages_compact", edit, moves)
 
     def _commit_edit(self, edit):
         self._fits(edit, "edit")
@@ -514,22 +516,28 @@ class KvCache(_OnStream):
         if lse is not None and (lse.device != self.device or lse.dtype != torch.float32 or
                                 lse.shape != (n, hq) or not lse.is_contiguous()):
             raise ValueError(f"lse must be a contiguous float32 tensor [{n}][{hq}] on {self.device}")
-        rows = lam.shape[0] if lam.dim() == 2 else n
-        if lam.get_device() != self._index or lam.dtype != torch.float32 or lam.shape[-1:] != (ho,) or rows < n or \
-                lam.dim() > 2:
+        shape = lam.shape
+        if shape == (ho,):
+            token, (head,) = 0, lam.stride()
+        elif len(shape) == 2 and shape[1] == ho and shape[0] >= n:
+            token, head = lam.stride()
+        else:
+            token = None
+        if token is None or lam.dtype != torch.float32 or lam.get_device() != self._index:
             raise ValueError(f"lam must be float32 [{ho}] or [{n} or more][{ho}] on {self.device}")
-        if weight is not None and (weight.get_device() != self._index or weight.dtype != torch.float32 or
-                                   weight.shape != (2 * c.dim,) or not weight.is_contiguous() or weight.data_ptr() & 15):
-            raise ValueError(f"weight must be a contiguous float32 tensor [{2 * c.dim}] on {self.device}, from a multiple of "
-                             "16 bytes on")
-        if torch.is_grad_enabled() and (lam.requires_grad or weight is not None and weight.requires_grad):
+        at = None
+        if weight is not None:
+            at = weight.data_ptr()
+            if weight.shape != (2 * c.dim,) or weight.dtype != torch.float32 or at & 15 or weight.get_device() != self._index \
+                    or not weight.is_contiguous():
+                raise ValueError(f"weight must be a contiguous float32 tensor [{2 * c.dim}] on {self.device}, from a multiple "
+                                 "of 16 bytes on")
+        if (lam.requires_grad or at is not None and weight.requires_grad) and torch.is_grad_enabled():
             raise ValueError("lam or weight asks for a gradient, and these calls have none: detach it, or call under "
                              "torch.no_grad()")
         d = self._diff
-        d.lambda_, d.lambda_head = lam.data_ptr(), lam.stride(-1)
-        d.lambda_token = lam.stride(0) if lam.dim() == 2 else 0
-        d.weight = None if weight is None else weight.data_ptr()
-        d.eps, d.gain = eps, gain
+        d.lambda_, d.lambda_token, d.lambda_head = lam.data_ptr(), token, head
+        d.weight, d.eps, d.gain = at, eps, gain
         work = step.diff_work(self)
         code = self._lib.agft_diff_attend(self._cfg, self.ptr, self.nbytes, tables.ptr, tables.nbytes, step.ptr,
                                           step.nbytes, n, step.max_new, self._b0, self._bdiff, self._b1,
