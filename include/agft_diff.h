@@ -25,7 +25,8 @@
  * Products and sums are kept in fp32, the sums of the probabilities and of y^2
  * too; probabilities meet the values in fp16, with the eleven bits and the range
  * that agft_kv_attend gives them, relative to the larger of a page's two value
- * scales.  The other head's values of that page keep all their bits while its scale
+ * scales (in requests of few rows and for fp16 outputs what that rounding leaves of
+ * each is summed as well).  The other head's values of that page keep all their bits while its scale
  * lies within 2^22 (e4m3) or 2^29 (int8) of the larger, fewer beyond, none below
  * 2^-33 (2^-30) of it.
  */

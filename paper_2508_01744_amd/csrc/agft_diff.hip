@@ -318,6 +318,9 @@ template <int FORM, int TYPE, int DIM>
 __device__ __forceinline__ void attend_few(const DiffArgs &p, FewLds<DIM> &lds, int block) {
     constexpr int DG = DIM / kBlockDims, C = FewLds<DIM>::C;
     constexpr int BLK = 2;                        // blocks of 16 tokens at a time
+    // Outputs of eleven bits: the probabilities' rounding, of a difference, is no less than
+    // theirs, so what is left of each goes through the second product as well.
+    constexpr bool FINE = TYPE == AGFT_KV_FP16;
     using H = Half<TYPE>;
     using F = Half<AGFT_KV_FP16>;
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
@@ -501,7 +504,7 @@ __device__ __forceinline__ void attend_few(const DiffArgs &p, FewLds<DIM> &lds, 
                     for (int c = 0; c < C; ++c) o[c] *= fall;
                 }
                 const float off = m == -INFINITY ? 0.0f : m;
-                fp16x4 pr[BLK];
+                fp16x8 pr, rest;
 #pragma unroll
                 for (int s = 0; s < BLK; ++s) {
                     float4v e;
@@ -509,13 +512,19 @@ __device__ __forceinline__ void attend_few(const DiffArgs &p, FewLds<DIM> &lds, 
                     for (int j = 0; j < 4; ++j) e[j] = __builtin_amdgcn_exp2f(t[s][j] - off);
                     l = fmaf((e[0] + e[1]) + (e[2] + e[3]), back[s], l);
 #pragma unroll
-                    for (int j = 0; j < 4; ++j) pr[s][j] = (_Float16)(e[j] * pow2(kRaise));
+                    for (int j = 0; j < 4; ++j) {
+                        const float x = e[j] * pow2(kRaise);
+                        pr[4 * s + j] = (_Float16)x;
+                        if constexpr (FINE) rest[4 * s + j] = (_Float16)(x - (float)pr[4 * s + j]);
+                    }
                 }
-                const fp16x8 pp = __builtin_shufflevector(pr[0], pr[1], 0, 1, 2, 3, 4, 5, 6, 7);
 #pragma unroll
-                for (int c = 0; c < C; ++c)
-                    o[c] = F::mfma(decode_scaled<FORM>(vc[0][c >> 2][c & 3], vc[1][c >> 2][c & 3], by[0][c / (C / 2)],
-                                                       by[1][c / (C / 2)]), pp, o[c]);
+                for (int c = 0; c < C; ++c) {
+                    const fp16x8 w = decode_scaled<FORM>(vc[0][c >> 2][c & 3], vc[1][c >> 2][c & 3], by[0][c / (C / 2)],
+                                                         by[1][c / (C / 2)]);
+                    o[c] = F::mfma(w, pr, o[c]);
+                    if constexpr (FINE) o[c] = F::mfma(w, rest, o[c]);
+                }
                 if (b + BLK < b1) fetch_values(b + BLK, vc);
             }
         }
