@@ -20,6 +20,9 @@ current when they are called; nothing here waits for the GPU except load().
 There is no backward pass: tensors that ask for a gradient are refused.
 Launches go to the calling thread's current device, which has to be the object's.
 Tensors of another stream are the caller's to order, as for any torch call.
+Windows and edits are planned one at a time, each committed before the next is
+planned; calls with a step or an edit of tables that have changed since are
+refused (a graph that replays them is not watched).
 """
 import contextlib
 import ctypes
@@ -227,7 +230,8 @@ class KvEdit(_OnStream):
         self.lengths = _view(self.buffer, v.lengths, torch.int32, (cfg.requests,))
         self.granted = _view(self.buffer, v.granted, torch.int32, (self.max_moves,))
         self.moves = _view(self.buffer, v.moves, torch.int32, (self.max_moves, 2))
-        self.planned, self._by, self._when = False, None, -1
+        # the tables that it was planned from, after how many of their changes, and whether it is one of them
+        self.planned, self._by, self._when, self._done = False, None, -1, False
 
 
 class KvTables(_OnStream):
@@ -332,7 +336,7 @@ class KvTables(_OnStream):
                                                         edit.max_moves, self._s())
         if code != L.AGFT_OK:
             L.check(name, code)
-        edit.planned, edit._by, edit._when = True, self, self._changes
+        edit.planned, edit._by, edit._when, edit._done = True, self, self._changes, False
         return edit
 
     def fork(self, src, dst, tokens=None, edit=None):
@@ -373,12 +377,13 @@ class KvTables(_OnStream):
 
     def _commit_edit(self, edit):
         self._fits(edit, "edit")
-        if edit._by is not self or edit._when != self._changes:
+        if edit._by is not self or edit._when != self._changes or edit._done:
             raise ValueError("the tables have changed since the edit was planned, or it is not theirs")
         L.check("agft_pages_commit", self._lib.agft_pages_commit(self._cfg, self.ptr, self.nbytes, edit.ptr, edit.nbytes,
                                                                  edit.max_moves, self._s()))
         self._changes += 1
         self._edits += 1
+        edit._when, edit._done = self._changes, True
 
 
 class KvCache(_OnStream):
@@ -549,8 +554,11 @@ class KvCache(_OnStream):
         return out
 
     def copy(self, edit):
-        """Copy the pages that a planned edit moves or fills."""
+        """Copy the pages that a planned edit moves or fills, before or after its commit,
+        but before the tables change again."""
         self._fits(edit, "edit")
+        if edit._when != edit._by._changes:
+            raise ValueError("the tables have changed since the edit was planned: its pages may be others' by now")
         code = self._lib.agft_pages_copy(self._cfg, self.ptr, self.nbytes, edit.ptr, edit.nbytes, edit.max_moves, self._s())
         if code != L.AGFT_OK:
             L.check("agft_pages_copy", code)

@@ -97,6 +97,14 @@ def test_an_edit_is_for_the_tables_that_it_was_planned_from(lib):
     again = t.compact(edit=second)
     t.reset()
     refused(lib, lambda: t.commit(again), "changed")
+    refused(lib, lambda: KvCache(t.cfg).copy(again), "changed")     # (its pages may be others' by now)
+    t.compact(edit=second)
+    cache = KvCache(t.cfg)
+    cache.copy(second)
+    t.commit(second)
+    cache.copy(second)                                              # (another layer)
+    t.commit(t.plan(ints(*[1] * 8), 8))
+    refused(lib, lambda: cache.copy(second), "changed")
     t.compact(edit=second)
     apart = KvTables(t.cfg)
     refused(lib, lambda: apart.commit(second), "not theirs")
