@@ -21,8 +21,8 @@ There is no backward pass: tensors that ask for a gradient are refused.
 Launches go to the calling thread's current device, which has to be the object's.
 Tensors of another stream are the caller's to order, as for any torch call.
 Windows and edits are planned one at a time, each committed before the next is
-planned; calls with a step or an edit of tables that have changed since are
-refused (a graph that replays them is not watched).
+planned.  A step of tables that an edit has changed since is refused, and an edit
+of tables that anything has changed since (a graph's replays are not watched).
 """
 import contextlib
 import ctypes
