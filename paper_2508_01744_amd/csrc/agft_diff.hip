@@ -612,7 +612,7 @@ __device__ __forceinline__ int lane_anew() {
 // second map's sums go to the first's wavefronts through LDS at the end.
 //
 // The prompt (10,001 tokens, 16 query heads of 128 numbers, two maps each, int8, causal:
-// 1.23 TFLOP) takes 1.23 ms, 1.0 PFLOP/s, 78% of what a large matrix product of the library
+// 1.23 TFLOP) takes 1.21 ms, 1.0 PFLOP/s, 79% of what a large matrix product of the library
 // reaches (e4m3 1.17 ms; 64 numbers, 0.61 TFLOP, 0.68 to 0.72 ms).  Matrix instructions and
 // vector ones are each busy for a third to a half of the cycles, LDS for a quarter; what
 // counts is that they run beside one another.  Four wavefronts of 128 numbers, one on a
@@ -620,6 +620,10 @@ __device__ __forceinline__ int lane_anew() {
 // 12 registers spilled 1.38; pages and exponents in LDS instead, none spilled, 1.26, and the
 // sums at a raised wave priority 1.23.  64 numbers in steps of 32 tokens 0.81 ms (0.74 on
 // that card), eight wavefronts on tiles of 128 tokens the same as four on 64.
+// A tile over few tokens is what comes before and after the loop: 1,024 tiles of 64
+// numbers over 65 tokens 62.5 us, 51 with all that the first steps need asked for
+// together and the norm's weights and lambda in LDS, 49 with results stored 16 bytes a
+// lane (over 321 tokens 93, 85, 82; the prompt 1.25, 1.23, 1.22).
 constexpr int kTileKeys = 64;
 template <int DIM>
 constexpr int tile_span() {                // tokens of a step, in 32s
@@ -641,6 +645,7 @@ struct TileLds {
     __attribute__((aligned(16))) char tile[2][2][2 * HEAD];
     float4 scale[2][16];                                   // by map, block % 16: its factor of the scores, e, 2^-e
     int2 look[tile_waves<DIM>()][2][64];                   // pages and exponents of the blocks that a wavefront fetches
+    float lambda[16 * tile_waves<DIM>()], weight[2 * DIM];
     int last;
 };
 
@@ -658,8 +663,8 @@ __device__ __forceinline__ void attend_many(const DiffArgs &p, TileLds<DIM> &lds
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     const int h = lane >> 5, n = lane & 31, map = wave / GROUPS, own_rows = wave % GROUPS;
     const int pair = block % p.heads, sub = block / p.heads % SUBS, place = block / p.heads / SUBS;
+    const Item item = p.items[place];                      // (the list has room for every workgroup's)
     if (place >= p.works[p.requests].items) return;
-    const Item item = p.items[place];
     const int i = item.request;
     const int4 own = *reinterpret_cast<const int4 *>(p.works + i);
     const int len = p.works[i].length;
@@ -706,16 +711,24 @@ __device__ __forceinline__ void attend_many(const DiffArgs &p, TileLds<DIM> &lds
     };
     constexpr bool KEPT = SPAN == 2;                       // in registers, where there is room; else in LDS
     int2 kept[2];
-    const auto look_up = [&](int t0, int side_at) {
-        const int lane = lane_anew();
-        int b = (t0 + lane) * BLOCKS + part + (side_at == 0 ? SHIFT : 0);
-        b = b < 0 ? 0 : b >= blocks ? blocks - 1 : b;
+    const auto block_of = [&](int t, int side_at) {
+        const int b = t * BLOCKS + part + (side_at == 0 ? SHIFT : 0);
+        return b < 0 ? 0 : b >= blocks ? blocks - 1 : b;
+    };
+    const auto page_and_exps = [&](int b) {
         uint32_t z = (uint32_t)p.table[(int64_t)i * p.row_pages + ((b << 4) >> p.shift)];
         if (z >= (uint32_t)p.pages) z = (uint32_t)p.pages - 1;
         const int4 e = *reinterpret_cast<const int4 *>(p.exps + ((int64_t)z * p.heads + pair) * 4);
-        const int2 k = make_int2((int)z, (e.x & 255) | (e.y & 255) << 8 | (e.z & 255) << 16 | e.w << 24);
-        if constexpr (KEPT) kept[side_at] = k;
-        else lds.look[wave][side_at][lane] = k;
+        return make_int2((int)z, (e.x & 255) | (e.y & 255) << 8 | (e.z & 255) << 16 | e.w << 24);
+    };
+    const auto look_up = [&](int t0) {
+        const int lane = lane_anew();
+        const int2 k[2] = {page_and_exps(block_of(t0 + lane, 0)), page_and_exps(block_of(t0 + lane, 1))};
+#pragma unroll
+        for (int a = 0; a < 2; ++a) {
+            if constexpr (KEPT) kept[a] = k[a];
+            else lds.look[wave][a][lane] = k[a];
+        }
     };
     // (a wavefront reads what it wrote itself)
     const auto look_at = [&](int t, int side_at) {
@@ -724,15 +737,13 @@ __device__ __forceinline__ void attend_many(const DiffArgs &p, TileLds<DIM> &lds
         const int2 k = lds.look[wave][side_at][t & 63];
         return Look{__builtin_amdgcn_readfirstlane(k.x), __builtin_amdgcn_readfirstlane(k.y)};
     };
-    const auto block_at = [&](int t, int side_at) {
-        int b = t * BLOCKS + part + (side_at == 0 ? SHIFT : 0);
-        b = b < 0 ? 0 : b >= blocks ? blocks - 1 : b;
-        return codes + (int64_t)look_at(t, side_at).id * page_bytes + (b & sub_mask) * (16 * DIM) + side_at * side;
+    const auto block_at = [&](int t, int side_at, int id) {
+        return codes + (int64_t)id * page_bytes + (block_of(t, side_at) & sub_mask) * (16 * DIM) + side_at * side;
     };
     uint4v ahead[2][HEADS][DG];                            // codes of the next step on their way
     const auto fetch = [&](int t, bool first) {
-        if ((t & 63) == 0 || first) look_up(t & ~63, 0), look_up(t & ~63, 1);
-        const char *k = block_at(t, 0), *v = block_at(t, 1);
+        if ((t & 63) == 0 && !first) look_up(t);
+        const char *k = block_at(t, 0, look_at(t, 0).id), *v = block_at(t, 1, look_at(t, 1).id);
         const int at = lane_anew() * 16;
 #pragma unroll
         for (int a = 0; a < HEADS; ++a)
@@ -745,23 +756,21 @@ __device__ __forceinline__ void attend_many(const DiffArgs &p, TileLds<DIM> &lds
     // Entry 16 g + m of the codes to the lanes that take its numbers: token m's
     // numbers 16 g.. as a row of the left operand of the scores, numbers m, 16 + m,
     // .. of tokens 4 g.. as rows of the left operand of the sums.
-    const auto stage = [&](int t) {                        // what fetch(t) brought
+    // Tile t's keys and what their blocks' scores are taken by; x: the blocks' exponents.
+    const auto stage_keys = [&](int t, const uint4v (*keys)[DG], int x) {
         const int buf = t & 1, lane = lane_anew(), g = lane >> 4, m16 = lane & 15;
         const int to_key = head * TileLds<DIM>::HEAD +
                            (((part >> 1) * DG * 4 + (g >> 1) * 2) * 64 + 32 * (g & 1) + 16 * (part & 1) + m16) * 16;
-        const int to_value = ((part * 2 + head) * DG * 2 * 64 + 32 * (g & 1) + 16 * (g >> 1) + m16) * 16;
 #pragma unroll
         for (int a = 0; a < HEADS; ++a)
 #pragma unroll
             for (int dg = 0; dg < DG; ++dg) {
-                const uint4v k = ahead[0][a][dg];
+                const uint4v k = keys[a][dg];
 #pragma unroll
                 for (int e = 0; e < 2; ++e)
                     *reinterpret_cast<typename H::x8 *>(&s_tile[buf][0][to_key + a * TileLds<DIM>::HEAD + (dg * 4 + e) * 1024]) =
                         H::template decode<FORM>(k[2 * e], k[2 * e + 1]);
             }
-        // (read by all lanes: what is made for one lane of them alone need not be there in the others)
-        const int x = look_at(t, 0).exps;
         if (lane == 0) {
             const int e0 = (int8_t)(x >> 8), e1 = x >> 24, e = e0 > e1 ? e0 : e1;
 #pragma unroll
@@ -769,6 +778,12 @@ __device__ __forceinline__ void attend_many(const DiffArgs &p, TileLds<DIM> &lds
                 s_scale[head + a][(t * BLOCKS + part + SHIFT) & 15] =
                     make_float4(scale2 * pow2(head + a == 0 ? (int8_t)x : (int8_t)(x >> 16)), (float)e, pow2(-e), 0.0f);
         }
+    };
+    const auto stage = [&](int t) {                        // what fetch(t) brought
+        // (read by all lanes: what is made for one lane of them alone need not be there in the others)
+        stage_keys(t, ahead[0], look_at(t, 0).exps);
+        const int buf = t & 1, lane = lane_anew(), g = lane >> 4, m16 = lane & 15;
+        const int to_value = ((part * 2 + head) * DG * 2 * 64 + 32 * (g & 1) + 16 * (g >> 1) + m16) * 16;
         if ((t * BLOCKS + part + 1) * kBlockTokens > len) {
             // codes past the request's tokens may be anything, NaN too
             const int valid = len - (t * kTileKeys + 16 * part + 4 * g);
@@ -916,9 +931,28 @@ __device__ __forceinline__ void attend_many(const DiffArgs &p, TileLds<DIM> &lds
         if constexpr (SPAN == 1) step(t, std::integral_constant<int, 1>{}, mask);
     };
 
-    fetch(begin - 1, true);
-    stage(begin - 1);
-    fetch(begin, true);
+    {
+        // The keys of the step before the first, the first step's operands, and what follows the
+        // loop are asked for together.
+        const int b = block_of(begin - 1, 0);
+        int2 before = page_and_exps(b);
+        before.x = __builtin_amdgcn_readfirstlane(before.x), before.y = __builtin_amdgcn_readfirstlane(before.y);
+        look_up(begin & ~63);
+        const bool has_lambda = threadIdx.x < ROWS, has_weight = threadIdx.x < WIDE / 4;
+        const int row_of = (int)threadIdx.x < rows ? row0 + (int)threadIdx.x : row0 + rows - 1;
+        const float lambda = has_lambda ? lambda_of(p, first, pair, row_of) : 0.0f;
+        const float4v weight = has_weight ? weight_at(p, 4 * threadIdx.x) : (float4v){0, 0, 0, 0};
+        uint4v keys[HEADS][DG];
+        const char *k = block_at(begin - 1, 0, before.x) + lane * 16;
+#pragma unroll
+        for (int a = 0; a < HEADS; ++a)
+#pragma unroll
+            for (int dg = 0; dg < DG; ++dg) keys[a][dg] = *reinterpret_cast<const uint4v *>(k + a * 2 * side + dg * kBlockBytes);
+        fetch(begin, true);
+        if (has_lambda) lds.lambda[threadIdx.x] = lambda;
+        if (has_weight) *reinterpret_cast<float4v *>(&lds.weight[4 * threadIdx.x]) = weight;
+        stage_keys(begin - 1, keys, before.y);
+    }
     __syncthreads();
     if (busy) {                                            // the first tokens' scores: keys of the step before
 #pragma unroll
@@ -1002,7 +1036,7 @@ __device__ __forceinline__ void attend_many(const DiffArgs &p, TileLds<DIM> &lds
     static_assert(sizeof(lds.tile) >= GROUPS * DG * 16 * 64 * sizeof(float4v), "a map's sums fit where the tiles were");
     float f = l > 0.0f || l != l ? pow2(-lift<FORM>()) / l : 0.0f;
     if (busy && map == 1) {
-        f *= lambda_of(p, first, pair, row1);
+        f *= lds.lambda[at_row + n1];
 #pragma unroll
         for (int c = 0; c < DG * 4; ++c)
 #pragma unroll
@@ -1024,13 +1058,22 @@ __device__ __forceinline__ void attend_many(const DiffArgs &p, TileLds<DIM> &lds
             for (int j = 0; j < 4; ++j) o[c][4 * z + j] = y[j];
         }
     const float by = row_factor<WIDE>(p, halves_sum(squares));
+    char *to = p.out + ((first + row1 / p.group) * p.out_token + (pair * p.group + row1 % p.group) * p.out_head) * 2;
 #pragma unroll
     for (int c = 0; c < DG * 4; ++c)
 #pragma unroll
-        for (int z = 0; z < 4; ++z) {
-            const int d = number(c, z);
-            store4<TYPE>(p, first, pair, row1, d,
-                         (float4v){o[c][4 * z], o[c][4 * z + 1], o[c][4 * z + 2], o[c][4 * z + 3]} * by * weight_at(p, d));
+        for (int z = 0; z < 4; z += 2) {
+            uint2 y[2];
+#pragma unroll
+            for (int k = 0; k < 2; ++k) {
+                const float4v x = (float4v){o[c][4 * (z + k)], o[c][4 * (z + k) + 1], o[c][4 * (z + k) + 2], o[c][4 * (z + k) + 3]} * by *
+                                  *reinterpret_cast<const float4v *>(&lds.weight[number(c, z + k)]);
+                y[k] = H::pack4(x[0], x[1], x[2], x[3]);
+            }
+            // numbers 0..3 and 8..11, 4..7 and 12..15 of the row's two lanes: 0..7, 8..15
+            const auto lo = __builtin_amdgcn_permlane32_swap(y[0].x, y[1].x, false, false);
+            const auto hi = __builtin_amdgcn_permlane32_swap(y[0].y, y[1].y, false, false);
+            *reinterpret_cast<uint4v *>(to + (number(c, z) + 4 * h1) * 2) = (uint4v){lo[0], hi[0], lo[1], hi[1]};
         }
 }
 
@@ -1043,7 +1086,7 @@ __global__ __launch_bounds__(64 * kFewWaves, few_groups<DIM>() / 256) void agft_
 }
 
 // Tiles of many rows; of 64 numbers in one launch with the few ones' workgroups, which
-// are as large (chunks of 256 to 1,024 tokens beside single ones: 124 us, 141 apart).
+// are as large (chunks of 256 to 1,024 tokens beside single ones: 116 us, apart 17 more).
 template <int DIM>
 constexpr bool one_launch() {
     return tile_waves<DIM>() == kFewWaves;
