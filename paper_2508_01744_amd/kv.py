@@ -22,7 +22,8 @@ Launches go to the calling thread's current device, which has to be the object's
 Tensors of another stream are the caller's to order, as for any torch call.
 Windows and edits are planned one at a time, each committed before the next is
 planned.  A step of tables that an edit has changed since is refused, and an edit
-of tables that anything has changed since (a graph's replays are not watched).
+of tables that anything has changed since.  A graph's replays are not watched: a
+step that a graph plans is taken as the caller says it is.
 """
 import contextlib
 import ctypes
@@ -61,6 +62,8 @@ try:
 except AttributeError:
     _current_device = torch.cuda.current_device
 
+_recording = torch.cuda.is_current_stream_capturing
+
 
 _one = {}       # devices and configurations' tuples, one object each: compared at every call
 
@@ -97,10 +100,11 @@ class _OnStream:
                              f"{other._shape}, not {self._shape}")
         if not other.planned:
             raise ValueError(f"the {what} has not been planned: its memory holds nothing yet")
-        if other._of is not None and other._of._edits != other._at:
+        if other._of is not None and other._of._edits != other._at and not other._recorded:
             raise ValueError(f"the tables have been edited since the {what} was planned")
 
     _of = None      # steps: the tables that they were planned from, when those had been edited _at times
+    _recorded = False   # and whether a graph plans them, whose replays nobody here sees
 
     def set_stream(self, stream):
         """Enqueue on `stream` from now on (None: on the stream current at each call)."""
@@ -314,6 +318,8 @@ class KvTables(_OnStream):
                                       step.max_tokens, self._s())
         if code != L.AGFT_OK:
             L.check("agft_kv_plan", code)
+        if self.device.type == "cuda" and _recording():
+            step._recorded = True
         step.planned, step._of, step._at = True, self, self._edits
         return step
 
