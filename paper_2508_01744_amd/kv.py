@@ -21,9 +21,13 @@ There is no backward pass: tensors that ask for a gradient are refused.
 Launches go to the calling thread's current device, which has to be the object's.
 Tensors of another stream are the caller's to order, as for any torch call.
 Windows and edits are planned one at a time, each committed before the next is
-planned.  A step of tables that an edit has changed since is refused, and an edit
-of tables that anything has changed since.  A graph's replays are not watched: a
-step that a graph plans is taken as the caller says it is.
+planned: plans write into the tables' rows and ring, where a later one writes over
+an earlier one.  So what was planned before the latest plan is not committed any
+more (plan it again), and nor do layers take an edit or store tokens of a window
+then, unless that had been committed; steps and edits of tables that were edited,
+loaded or reset since are refused too, and those of other tables.  (Of two windows
+the older one's step still attends, to the pages that the rows name now.)  A graph's replays are not
+watched: a step that a graph plans is taken as the caller says it is.
 """
 import contextlib
 import ctypes
@@ -100,11 +104,24 @@ class _OnStream:
                              f"{other._shape}, not {self._shape}")
         if not other.planned:
             raise ValueError(f"the {what} has not been planned: its memory holds nothing yet")
-        if other._of is not None and other._of._edits != other._at and not other._recorded:
-            raise ValueError(f"the tables have been edited since the {what} was planned")
 
-    _of = None      # steps: the tables that they were planned from, when those had been edited _at times
-    _recorded = False   # and whether a graph plans them, whose replays nobody here sees
+    def _fits_step(self, step):
+        """And steps whose slots and lengths are of tables that were edited, loaded or reset since."""
+        self._fits(step, "step")
+        if step._number <= step._of._void and not step._recorded:
+            raise ValueError("the tables have been edited, loaded or reset since the step was planned")
+
+    def _fits_window(self, tables, step):
+        """What attends: the step, and its tables as no edit's plan has written into them."""
+        self._fits_step(step)
+        self._fits(tables, "tables")
+        if step._recorded:
+            return
+        if step._of is not tables:
+            raise ValueError("the step was planned from other tables")
+        if step._number < tables._edit_number and not step._done:
+            raise ValueError("an edit has been planned since the step, which was not committed: its rows may be the "
+                             "edit's by now")
 
     def set_stream(self, stream):
         """Enqueue on `stream` from now on (None: on the stream current at each call)."""
@@ -181,7 +198,9 @@ class KvStep(_OnStream):
         self.slots = _view(self.buffer, v.slots, torch.int64, (self.max_tokens,))
         self._works, self._work_dim = [], 0
         self._diff_works, self._diff_dim = [], 0
-        self.planned = False
+        # the tables that it was planned from, by which of their plans, and whether that was committed (of a step
+        # that a graph plans all that is as the caller says: nobody here sees its replays)
+        self.planned, self._of, self._number, self._done, self._recorded = False, None, 0, False, False
 
     def set_max_new(self, max_new):
         """No request brings more new tokens than this (None: max_tokens); rows
@@ -234,8 +253,9 @@ class KvEdit(_OnStream):
         self.lengths = _view(self.buffer, v.lengths, torch.int32, (cfg.requests,))
         self.granted = _view(self.buffer, v.granted, torch.int32, (self.max_moves,))
         self.moves = _view(self.buffer, v.moves, torch.int32, (self.max_moves, 2))
-        # the tables that it was planned from, after how many of their changes, and whether it is one of them
-        self.planned, self._by, self._when, self._done = False, None, -1, False
+        # the tables that it was planned from, by which of their plans, after how many of their changes, and whether
+        # it is one of them
+        self.planned, self._of, self._number, self._when, self._done = False, None, 0, -1, False
 
 
 class KvTables(_OnStream):
@@ -260,14 +280,16 @@ class KvTables(_OnStream):
         L.check("agft_pages_owners_at", self._lib.agft_pages_owners_at(self._cfg, self.ptr, self.nbytes,
                                                                        ctypes.byref(owners)))
         self.owners = _view(self.buffer, owners.value, torch.int32, (cfg.pages,))
-        # changes of the tables, and edits among them: plans hold for the tables that they were made from
-        self._changes = self._edits = 0
+        # Changes of the tables; the latest plan's number, the latest windows' and edits' ones, and the last one that
+        # an edit, a load or a reset has left behind: plans hold for the tables that they were made from.
+        self._changes = self._number = self._step_number = self._edit_number = self._void = 0
         self.reset()
 
     def reset(self):
         """No request holds a token, every page is free."""
         L.check("agft_kv_reset", self._lib.agft_kv_reset(self._cfg, self.ptr, self.nbytes, self._s()))
         self._changes += 1
+        self._void = self._number
 
     def load(self, lengths, table, free, shared=False):
         """Take over the tables of a running node: lengths [R], table
@@ -300,6 +322,7 @@ class KvTables(_OnStream):
             self.ring[:free.numel()].copy_(free)
             self.counters.copy_(counters)
         self._changes += 1
+        self._void = self._number
 
     def plan(self, add, max_tokens, max_new=None, step=None):
         """Plan a window: add [R] int32 new tokens per request (0: none, < 0: it
@@ -320,17 +343,25 @@ class KvTables(_OnStream):
             L.check("agft_kv_plan", code)
         if self.device.type == "cuda" and _recording():
             step._recorded = True
-        step.planned, step._of, step._at = True, self, self._edits
+        else:
+            self._number += 1
+            self._step_number = self._number
+        step.planned, step._of, step._number, step._done = True, self, self._number, False
         return step
 
     def commit(self, step):
         """The planned window's lengths and free pages, or the planned edit, become the tables'."""
         if isinstance(step, KvEdit):
             return self._commit_edit(step)
-        self._fits(step, "step")
+        self._fits_step(step)
+        if step._of is not self and not step._recorded:
+            raise ValueError("the step was planned from other tables")
+        if step._number != self._number and not step._recorded:
+            raise ValueError("another window or an edit has been planned since the step: it may have written over its pages")
         L.check("agft_kv_commit", self._lib.agft_kv_commit(self._cfg, self.ptr, self.nbytes, step.ptr, step.nbytes,
                                                            step.max_tokens, self._s()))
         self._changes += 1
+        step._done = True
 
     def _edit(self, name, edit, moves, *args):
         """Plan an edit with room for `moves` moves."""
@@ -342,7 +373,9 @@ class KvTables(_OnStream):
                                                         edit.max_moves, self._s())
         if code != L.AGFT_OK:
             L.check(name, code)
-        edit.planned, edit._by, edit._when, edit._done = True, self, self._changes, False
+        self._number += 1
+        self._edit_number = self._number
+        edit.planned, edit._of, edit._number, edit._when, edit._done = True, self, self._number, self._changes, False
         return edit
 
     def fork(self, src, dst, tokens=None, edit=None):
@@ -383,12 +416,15 @@ class KvTables(_OnStream):
 
     def _commit_edit(self, edit):
         self._fits(edit, "edit")
-        if edit._by is not self or edit._when != self._changes or edit._done:
+        if edit._of is not self or edit._when != self._changes or edit._done:
             raise ValueError("the tables have changed since the edit was planned, or it is not theirs")
+        if edit._number != self._number:
+            raise ValueError("a window or another edit has been planned since the edit: it may have written over its "
+                             "rows and free pages")
         L.check("agft_pages_commit", self._lib.agft_pages_commit(self._cfg, self.ptr, self.nbytes, edit.ptr, edit.nbytes,
                                                                  edit.max_moves, self._s()))
         self._changes += 1
-        self._edits += 1
+        self._void = self._number
         edit._when, edit._done = self._changes, True
 
 
@@ -464,7 +500,10 @@ class KvCache(_OnStream):
         """Store the window's keys and values, [max_tokens][heads][dim] each
         (bf16, fp16 or fp32), rows as in step.starts."""
         H, n = self.cfg.heads, step.max_tokens
-        self._fits(step, "step")
+        self._fits_step(step)
+        if step._number < step._of._step_number and not (step._done or step._recorded):
+            raise ValueError("another window has been planned since the step, which was not committed: its slots may be "
+                             "that one's by now")
         if k.dtype != v.dtype:
             raise ValueError("k and v must have one type")
         self._dense(self._d0, k, H, n, "k")
@@ -483,8 +522,7 @@ class KvCache(_OnStream):
         scale: 1 / sqrt(dim) if None."""
         c, n = self.cfg, step.max_tokens
         hq = c.heads * c.group
-        self._fits(step, "step")
-        self._fits(tables, "tables")
+        self._fits_window(tables, step)
         if out is None:
             out = self._empty(n, hq, c.dim, dtype=q.dtype)
         elif out.dtype != q.dtype:
@@ -514,8 +552,7 @@ class KvCache(_OnStream):
         tokens as in attend."""
         c, n = self.cfg, step.max_tokens
         hq, ho = c.heads * c.group, c.heads // 2 * c.group
-        self._fits(step, "step")
-        self._fits(tables, "tables")
+        self._fits_window(tables, step)
         if c.heads % 2 or c.dim not in (64, 128):
             raise ValueError(f"differential attention is of pairs of heads of 64 or 128 numbers, not {c.heads} of {c.dim}")
         if out is None:
@@ -563,8 +600,9 @@ class KvCache(_OnStream):
         """Copy the pages that a planned edit moves or fills, before or after its commit,
         but before the tables change again."""
         self._fits(edit, "edit")
-        if edit._when != edit._by._changes:
-            raise ValueError("the tables have changed since the edit was planned: its pages may be others' by now")
+        if edit._when != edit._of._changes or edit._number != edit._of._number and not edit._done:
+            raise ValueError("the tables have changed since the edit was planned, or something else has been: its pages "
+                             "may be others' by now")
         code = self._lib.agft_pages_copy(self._cfg, self.ptr, self.nbytes, edit.ptr, edit.nbytes, edit.max_moves, self._s())
         if code != L.AGFT_OK:
             L.check("agft_pages_copy", code)
