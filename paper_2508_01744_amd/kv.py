@@ -283,6 +283,7 @@ class KvTables(_OnStream):
         # Changes of the tables; the latest plan's number, the latest windows' and edits' ones, and the last one that
         # an edit, a load or a reset has left behind: plans hold for the tables that they were made from.
         self._changes = self._number = self._step_number = self._edit_number = self._void = 0
+        self._token = object()      # what layers know them by
         self.reset()
 
     def reset(self):
@@ -438,6 +439,9 @@ class KvCache(_OnStream):
         self._b0, self._b1 = ctypes.byref(self._d0), ctypes.byref(self._d1)
         self._diff = L.agft_diff_args()
         self._bdiff = ctypes.byref(self._diff)
+        # the latest window appended and edit copied here, by their plans' numbers and their tables: what an edit's
+        # plan found in its pages is there from the windows before it until the copy, and from the copy on
+        self._appended, self._appended_of, self._copied, self._copied_of = 0, None, 0, None
         self.nbytes = self._lib.agft_kv_cache_bytes(self._cfg)
         self.buffer = self._buffer(self.nbytes, "cache")
         self.ptr = self.buffer.data_ptr()
@@ -504,6 +508,9 @@ class KvCache(_OnStream):
         if step._number < step._of._step_number and not (step._done or step._recorded):
             raise ValueError("another window has been planned since the step, which was not committed: its slots may be "
                              "that one's by now")
+        if self._copied > step._number and self._copied_of is step._of._token and not step._recorded:
+            raise ValueError("the pages of a later edit have been copied in this layer: append a window before that, or "
+                             "plan it after the edit's commit")
         if k.dtype != v.dtype:
             raise ValueError("k and v must have one type")
         self._dense(self._d0, k, H, n, "k")
@@ -512,6 +519,8 @@ class KvCache(_OnStream):
                                         self._s())
         if code != L.AGFT_OK:
             L.check("agft_kv_append", code)
+        if not step._recorded:
+            self._appended, self._appended_of = step._number, step._of._token
 
     def attend(self, tables, step, q, out=None, lse=None, scale=None):
         """softmax(scale q K^T) V of the window's tokens over their requests'
@@ -598,14 +607,18 @@ class KvCache(_OnStream):
 
     def copy(self, edit):
         """Copy the pages that a planned edit moves or fills, before or after its commit,
-        but before the tables change again."""
+        but before the tables change again, behind the windows planned before it and
+        ahead of this layer's tokens of later ones."""
         self._fits(edit, "edit")
         if edit._when != edit._of._changes or edit._number != edit._of._number and not edit._done:
             raise ValueError("the tables have changed since the edit was planned, or something else has been: its pages "
                              "may be others' by now")
+        if self._appended > edit._number and self._appended_of is edit._of._token:
+            raise ValueError("a later window's tokens are in this layer already: the edit's pages may be theirs")
         code = self._lib.agft_pages_copy(self._cfg, self.ptr, self.nbytes, edit.ptr, edit.nbytes, edit.max_moves, self._s())
         if code != L.AGFT_OK:
             L.check("agft_pages_copy", code)
+        self._copied, self._copied_of = edit._number, edit._of._token
 
     def export(self, slots, dtype=torch.bfloat16):
         """Keys and values of the slots [n] (int64; -1 gives zeros) as two

@@ -148,3 +148,42 @@ def test_graphs_whose_plans_are_recorded(lib, monkeypatch):
         cache.append(step, K, K)
         cache.attend(t, step, Q)
         t.commit(step)
+
+
+def test_a_layers_copies_come_before_its_tokens_of_later_windows(lib):
+    """The copy would write over a token in a fork's last page, or copy a page that was filled anew."""
+    t, cache = node()
+    late = KvCache(t.cfg)
+    edit = t.fork(ints(0, 1), ints(5, 6))
+    t.commit(edit)
+    step = t.plan(ADD, 8)
+    cache.copy(edit)                                    # (a plan writes to no layer)
+    for layer in (cache, late):
+        layer.append(step, K, K)
+    refused(lib, lambda: late.copy(edit), "already")
+    refused(lib, lambda: cache.copy(edit), "already")
+    KvCache(t.cfg).copy(edit)
+    other = KvTables(t.cfg)                             # (other tables' windows say nothing of these)
+    for _ in range(3):
+        other.commit(other.plan(ADD, 8))
+    step = other.plan(ADD, 8)
+    free = KvCache(t.cfg)
+    free.append(step, K, K)
+    free.copy(edit)
+
+
+def test_a_layers_tokens_of_earlier_windows_come_before_its_copies(lib):
+    """A fork's last page would lack them, and a moved page too."""
+    t, cache = node()
+    step = t.plan(ADD, 8)
+    t.commit(step)
+    for plan in (t.compact, lambda: t.fork(ints(0), ints(1))):
+        edit = plan()
+        late = KvCache(t.cfg)
+        late.append(step, K, K)
+        late.copy(edit)
+        refused(lib, lambda: late.append(step, K, K), "copied in this layer")
+    t.commit(edit)
+    step = t.plan(ADD, 8)
+    late.append(step, K, K)
+    t.commit(step)
