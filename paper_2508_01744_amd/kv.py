@@ -294,7 +294,8 @@ class KvTables(_OnStream):
 
     def load(self, lengths, table, free, shared=False):
         """Take over the tables of a running node: lengths [R], table
-        [R][row_pages] and the free pages in the order of their use (int32).
+        [R][row_pages] and the free pages in the order of their use (int32), which
+        no request holds and of which none is named twice.
         shared: requests may have pages in common, whose owners are counted.
         Set-up: checks the values, which waits for the GPU."""
         cfg = self.cfg
@@ -308,12 +309,18 @@ class KvTables(_OnStream):
         for wrong, what in zip(torch.stack(bad).tolist(), ("lengths", "table", "free")):
             if wrong:
                 raise ValueError(f"{what} out of range")
+        used = torch.arange(cfg.row_pages, device=table.device) < ((lengths + (cfg.page - 1)) // cfg.page)[:, None]
+        holders = torch.bincount(table[used], minlength=cfg.pages)
+        listed = torch.bincount(free, minlength=cfg.pages)
+        twice, held = torch.stack([(listed > 1).any(), ((listed > 0) & (holders > 0)).any()]).tolist()
+        if twice:
+            raise ValueError("free lists a page twice")
+        if held:
+            raise ValueError("free lists a page that a request holds")
         counters = torch.tensor([0, free.numel(), 0, 0, 0, 0, 0, 0], dtype=torch.int32)
         owners = None
         if shared:
-            cols = torch.arange(cfg.row_pages, device=table.device)
-            used = cols < ((lengths + (cfg.page - 1)) // cfg.page)[:, None]
-            owners = (torch.bincount(table[used], minlength=cfg.pages) - 1).clamp_(min=0)
+            owners = (holders - 1).clamp_(min=0)
             counters[2] = owners.sum()
         with self._settled():
             self.owners.zero_() if owners is None else self.owners.copy_(owners)

@@ -1,0 +1,42 @@
+"""Which tables KvTables.load takes over (CPU: calls that would launch are noted by
+kv_stub.py instead)."""
+import contextlib
+
+import pytest
+import torch
+
+import kv_stub
+from paper_2508_01744_amd import KvTables, kv_config
+
+PAGES = 40
+
+
+@pytest.fixture
+def tables(monkeypatch):
+    kv_stub.install(monkeypatch)
+    t = KvTables(kv_config(requests=3, row_tokens=64, pages=PAGES, page=16, heads=2, group=1, dim=64))
+    t._settled = contextlib.nullcontext
+    return t
+
+
+def ints(*x):
+    return torch.tensor(x, dtype=torch.int32)
+
+
+LENGTHS = ints(48, 33, 0)
+TABLE = ints(5, 6, 7, 30, 8, 9, 10, 31, 5, 5, 5, 5).view(3, 4)     # (behind the tokens: what earlier ones left)
+
+
+@pytest.mark.parametrize("shared", [False, True])
+def test_free_pages_that_are_not(tables, shared):
+    before = tables.buffer.clone()
+    for free, match in ((ints(1, 2, 1), "twice"), (ints(39, 39), "twice"), (ints(1, 7), "holds"), (ints(10), "holds"),
+                        (ints(5, 0), "holds")):
+        with pytest.raises(ValueError, match=match):
+            tables.load(LENGTHS, TABLE, free, shared=shared)
+        assert torch.equal(tables.buffer, before)
+    for free in (ints(1, 2, 3), ints(30, 31), ints(), ints(*[p for p in range(PAGES) if p not in (5, 6, 7, 8, 9, 10)])):
+        tables.load(LENGTHS, TABLE, free, shared=shared)
+        assert tables.counters.tolist()[:2] == [0, free.numel()] and tables.ring.tolist()[:free.numel()] == free.tolist()
+        assert torch.equal(tables.lengths, LENGTHS) and torch.equal(tables.table, TABLE)
+    tables.load(ints(0, 0, 0), TABLE, torch.arange(PAGES, dtype=torch.int32), shared=shared)
