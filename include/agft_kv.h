@@ -21,7 +21,7 @@
  *
  * Lengths.  Request i holds L_i tokens (0 at the start).  A window asks for
  * add_i more: > 0 new tokens, 0 none, < 0 the request ends (refused while pages
- * have several owners, agft_pages.h).  With
+ * have several owners, counted or not, agft_pages.h).  With
  * pages(n) = ceil(n / page), a_i = add_i where 0 < add_i and L_i + add_i <=
  * row_pages * page and else 0, need_i = pages(L_i + a_i) - pages(L_i):
  *
@@ -98,7 +98,8 @@ typedef struct agft_kv_config {
 
 /* Where the tables' and a step's parts lie in their buffers. */
 typedef struct agft_kv_tables_view {
-    int32_t *counters; /* [8]: ring's head, free pages, owners of pages beyond the first (agft_pages.h), and zeros */
+    int32_t *counters; /* [8]: ring's head, free pages, owners of pages beyond the first, 1 where there are some
+                          that nobody counted (agft_pages.h), and zeros */
     int32_t *lengths;  /* [requests] */
     int32_t *table;    /* [requests][row_pages] pages of a request's tokens, in order */
     int32_t *ring;     /* [pages] free pages from the ring's head on */

@@ -21,7 +21,9 @@
  * Only pages whose tokens are all there are shared, so no write meets a shared
  * page.  While counters[2] is not 0, requests end by agft_pages_trim: agft_kv_plan
  * refuses an end (add < 0) then, leaves the request as it is and counts it among
- * the refused ones.
+ * the refused ones.  Whoever fills the tables with pages in common and does not count
+ * their owners sets counters[3] to 1: trims refuse every request then as well, since no
+ * page could be told to be free.
  *
  * Fork.  For j = 0 .. n - 1 request dst_j gets the first t_j = min(tokens_j,
  * L(src_j)) tokens of request src_j.  It is asked for if src_j and dst_j are
@@ -37,7 +39,8 @@
  *
  * Trim.  Request i keeps keep_i tokens, if 0 <= keep_i < L_i (else all of them; 0
  * ends it).  One that would end inside a page with further owners is refused: its
- * next tokens would be written there (fork what it is to keep, and end it).  Pages
+ * next tokens would be written there (fork what it is to keep, and end it); all are while
+ * owners are not counted.  Pages
  * go back behind the ring's tail when their last owner lets them go, in the order
  * of the requests and of their pages, a page that several let go in the place of
  * the last.
@@ -78,7 +81,7 @@ size_t agft_pages_edit_bytes(const agft_kv_config *cfg, int32_t max_moves);
 int agft_pages_edit_at(const agft_kv_config *cfg, int32_t max_moves, void *d_edit, size_t nbytes, agft_pages_view *out);
 
 /* Owners beyond the first, int32 [pages], in the tables' buffer (agft_kv_reset sets them to 0; whoever fills the tables
-   otherwise fills these, and counters[2], too). */
+   otherwise fills these and counters[2], or sets counters[3], too). */
 int agft_pages_owners_at(const agft_kv_config *cfg, void *d_tables, size_t nbytes, int32_t **out);
 
 /*

@@ -51,7 +51,9 @@ struct Ask {
     bool wants, ends;
 };
 
-// (No request ends here while pages have several owners: agft_pages.h.)
+// Whether pages have several owners, counted or not: no request ends here then (agft_pages.h).
+__device__ __forceinline__ bool pages_shared(const PlanArgs &p) { return (p.counters[2] | p.counters[3]) != 0; }
+
 __device__ __forceinline__ Ask ask_of(const PlanArgs &p, int32_t past, int32_t add, bool shared) {
     Ask a;
     const int32_t cap = p.row_pages << p.shift;
@@ -152,7 +154,7 @@ __device__ __forceinline__ void plan_chunk(const PlanArgs &p, int r0, uint32_t n
     const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
     const int i0 = r0 + threadIdx.x * PER;
     Ask a[PER];
-    const bool shared = p.counters[2] != 0;
+    const bool shared = pages_shared(p);
     uint32_t need = 0, tok = 0, mid = 0;
 #pragma unroll
     for (int j = 0; j < PER; ++j) {
@@ -499,7 +501,7 @@ __global__ __launch_bounds__(kPlanThreads) void agft_kv_plan_slots_kernel(PlanAr
         const int i = r0 + lane;
         const bool live = lane < 16 && i < p.requests;
         if (live) p.works[i].few += s_off[1][i / kPlanChunk];
-        const bool ends = live && p.add[i] < 0 && p.counters[2] == 0;
+        const bool ends = live && p.add[i] < 0 && !pages_shared(p);
         const Ask a = ask_of(p, ends ? p.lengths[i] : 0, 0, false);
         plan_give_back(p, ends, i, a.held, ends ? p.back[i] + s_off[3][i / kPlanChunk] : 0, head, free_pages);
     }

@@ -23,6 +23,8 @@ constexpr int kNearPages = 1 << 18;    // pages whose free bits a workgroup keep
 constexpr int kChunkWords = 1024;      // words of 32 free bits whose prefix sums one workgroup makes
 
 enum { kHead, kFree, kExtra, kRefused, kTaken, kGiven, kEntries, kKind };
+// of the tables' counters, behind the first three: pages have owners that nobody counted
+constexpr int kUncounted = 3;
 // what the commit needs beside: owners beyond the first before the edit; held pages and moves of a compaction
 enum { kExtraBefore, kHeld, kMoves };
 
@@ -358,12 +360,14 @@ __device__ __forceinline__ void trim_chunk(const EditArgs &p, bool extra, TrimLd
         const bool here = lane < p.per && i < p.requests;
         int32_t past = 0, to = 0;
         bool refused = false;
+        const bool uncounted = PLAN && p.counters[kUncounted] != 0;
         if (here) {
             if constexpr (PLAN) {
                 past = held_to(p, p.lengths[i]);
                 const int32_t k = p.keep[i];
                 to = k >= 0 && k < past ? k : past;
-                if (extra && to < past && (to & (p.page - 1)) != 0)
+                if (uncounted) refused = to < past;
+                else if (extra && to < past && (to & (p.page - 1)) != 0)
                     refused = p.owners[page_at(p, p.table[(int64_t)i * p.row_pages + (to >> p.shift)])] > 0;
                 if (refused) to = past;
             } else {

@@ -262,7 +262,8 @@ class KvTables(_OnStream):
     """Block tables, lengths and the ring of free pages of a node's requests:
     counters [8], lengths [R], table [R][row_pages], ring [pages], owners [pages]
     beyond a page's first (int32).  While a page has several owners, counters[2] is
-    not 0, and requests end by trim: a plan refuses to end them."""
+    not 0, and requests end by trim: a plan refuses to end them.  Where owners were not
+    counted (load), counters[3] is 1, and trims are refused too."""
     planned = True      # (as a step's: their memory holds something from the start)
 
     def __init__(self, cfg, device="cuda", stream=None):
@@ -297,6 +298,8 @@ class KvTables(_OnStream):
         [R][row_pages] and the free pages in the order of their use (int32), which
         no request holds and of which none is named twice.
         shared: requests may have pages in common, whose owners are counted.
+        Without it pages in common stay whole: no request ends or is trimmed (both
+        count as refused), and such a page that is filled in part is refused.
         Set-up: checks the values, which waits for the GPU."""
         cfg = self.cfg
         self._ints(lengths, (cfg.requests,), "lengths")
@@ -317,7 +320,12 @@ class KvTables(_OnStream):
             raise ValueError("free lists a page twice")
         if held:
             raise ValueError("free lists a page that a request holds")
-        counters = torch.tensor([0, free.numel(), 0, 0, 0, 0, 0, 0], dtype=torch.int32)
+        # (of requests whose last page is filled in part: whether others hold that page)
+        last = table.gather(1, (lengths // cfg.page).clamp(max=cfg.row_pages - 1).long()[:, None])[:, 0].long()
+        common, partly = torch.stack([(holders > 1).any(), ((lengths % cfg.page != 0) & (holders[last] > 1)).any()]).tolist()
+        if partly and not shared:
+            raise ValueError("a page that its request fills in part is another's too: without shared both would write there")
+        counters = torch.tensor([0, free.numel(), 0, int(common and not shared), 0, 0, 0, 0], dtype=torch.int32)
         owners = None
         if shared:
             owners = (holders - 1).clamp_(min=0)

@@ -40,3 +40,21 @@ def test_free_pages_that_are_not(tables, shared):
         assert tables.counters.tolist()[:2] == [0, free.numel()] and tables.ring.tolist()[:free.numel()] == free.tolist()
         assert torch.equal(tables.lengths, LENGTHS) and torch.equal(tables.table, TABLE)
     tables.load(ints(0, 0, 0), TABLE, torch.arange(PAGES, dtype=torch.int32), shared=shared)
+
+
+COMMON = ints(5, 6, 7, 9, 5, 6, 8, 0, 5, 9, 9, 9).view(3, 4)
+
+
+def test_pages_in_common_that_nobody_counts(tables):
+    """They stay whole: counters[3] tells the kernels that no page can be given back."""
+    tables.load(ints(48, 33, 16), COMMON, ints(1, 2, 3))
+    assert tables.counters.tolist() == [0, 3, 0, 1, 0, 0, 0, 0] and not tables.owners.any()
+    tables.load(ints(48, 33, 16), COMMON, ints(1, 2, 3), shared=True)
+    assert tables.counters.tolist() == [0, 3, 3, 0, 0, 0, 0, 0] and tables.owners.tolist()[5:7] == [2, 1]
+    tables.load(LENGTHS, TABLE, ints(1, 2, 3))
+    assert tables.counters.tolist() == [0, 3, 0, 0, 0, 0, 0, 0]
+    before = tables.buffer.clone()
+    for lengths in (ints(20, 33, 16), ints(48, 32, 1), ints(17, 17, 0)):
+        with pytest.raises(ValueError, match="in part"):
+            tables.load(lengths, COMMON, ints(1, 2, 3))
+        assert torch.equal(tables.buffer, before)
