@@ -19,7 +19,7 @@
  * Owners.  A page may be held by several requests: owners counts those beyond the
  * first, and the tables' counters[2] is the sum over all pages (less than 2^31).
  * Only pages whose tokens are all there are shared, so no write meets a shared
- * page.  While counters[2] is not 0, requests end by agft_pages_trim: agft_kv_plan
+ * page (whoever fills the tables otherwise sees to that).  While counters[2] is not 0, requests end by agft_pages_trim: agft_kv_plan
  * refuses an end (add < 0) then, leaves the request as it is and counts it among
  * the refused ones.  Whoever fills the tables with pages in common and does not count
  * their owners sets counters[3] to 1: trims refuse every request then as well, since no

@@ -292,12 +292,15 @@ class KvTables(_OnStream):
         L.check("agft_kv_reset", self._lib.agft_kv_reset(self._cfg, self.ptr, self.nbytes, self._s()))
         self._changes += 1
         self._void = self._number
+        self._partly = False
 
     def load(self, lengths, table, free, shared=False):
         """Take over the tables of a running node: lengths [R], table
         [R][row_pages] and the free pages in the order of their use (int32), which
         no request holds and of which none is named twice.
-        shared: requests may have pages in common, whose owners are counted.
+        shared: requests may have pages in common, whose owners are counted.  While
+        one of them is a request's last, filled in part, windows that bring that
+        request tokens are refused, and plans wait for the GPU to see whether they do.
         Without it pages in common stay whole: no request ends or is trimmed (both
         count as refused), and such a page that is filled in part is refused.
         Set-up: checks the values, which waits for the GPU."""
@@ -337,6 +340,7 @@ class KvTables(_OnStream):
             self.ring.zero_()
             self.ring[:free.numel()].copy_(free)
             self.counters.copy_(counters)
+        self._partly = partly
         self._changes += 1
         self._void = self._number
 
@@ -353,6 +357,8 @@ class KvTables(_OnStream):
             if step.max_tokens != max_tokens:
                 raise ValueError(f"step is for {step.max_tokens} tokens, not {max_tokens}")
             step.set_max_new(max_new)
+        if self._partly:
+            self._look_for_writes(add)
         code = self._lib.agft_kv_plan(self._cfg, self.ptr, self.nbytes, add.data_ptr(), step.ptr, step.nbytes,
                                       step.max_tokens, self._s())
         if code != L.AGFT_OK:
@@ -364,6 +370,20 @@ class KvTables(_OnStream):
             self._step_number = self._number
         step.planned, step._of, step._number, step._done = True, self, self._number, False
         return step
+
+    def _look_for_writes(self, add):
+        """Tables that were loaded with a partly filled page in common: whether this
+        window would write into one, until there is none any more."""
+        if self.device.type == "cuda" and _recording():
+            raise ValueError("tables with a partly filled page in common: windows can be recorded once it has one owner")
+        with self._settled():
+            inside = self.lengths % self.cfg.page
+            last = self.table.gather(1, (self.lengths // self.cfg.page).clamp(max=self.cfg.row_pages - 1).long()[:, None])
+            partly = (inside != 0) & (self.owners[last[:, 0].long()] > 0)
+            partly, meets = torch.stack([partly.any(), (partly & (add > 0)).any()]).tolist()
+        if meets:
+            raise ValueError("new tokens of a request whose last page, filled in part, is another's too: end one of them")
+        self._partly = partly
 
     def commit(self, step):
         """The planned window's lengths and free pages, or the planned edit, become the tables'."""

@@ -58,3 +58,25 @@ def test_pages_in_common_that_nobody_counts(tables):
         with pytest.raises(ValueError, match="in part"):
             tables.load(lengths, COMMON, ints(1, 2, 3))
         assert torch.equal(tables.buffer, before)
+
+
+def test_no_new_tokens_in_a_page_that_others_hold(tables):
+    """Both would write there; once one of them is gone the other gets tokens again."""
+    t = tables
+    t.load(ints(20, 27, 16), COMMON, ints(1, 2, 3), shared=True)
+    for add in (ints(1, 0, 0), ints(0, 5, 1), ints(1, 1, 1)):
+        with pytest.raises(ValueError, match="in part"):
+            t.plan(add, 8)
+    for add in (ints(0, 0, 1), ints(-1, 0, 0)):
+        t.plan(add, 8)
+    with pytest.raises(ValueError, match="in part"):
+        t.plan(ints(0, 1, 0), 8)
+    t.owners[6] = 0                                     # (the kernels are not run here)
+    t.lengths[0] = 0
+    t.plan(ints(0, 1, 0), 8)
+    assert not t._partly
+    for again in (lambda: t.load(ints(48, 33, 16), COMMON, ints(1, 2, 3), shared=True), t.reset):
+        t.load(ints(20, 27, 16), COMMON, ints(1, 2, 3), shared=True)
+        assert t._partly
+        again()
+        t.plan(ints(1, 1, 1), 8)
