@@ -371,7 +371,8 @@ __device__ __forceinline__ void trim_chunk(const EditArgs &p, bool extra, TrimLd
                     refused = p.owners[page_at(p, p.table[(int64_t)i * p.row_pages + (to >> p.shift)])] > 0;
                 if (refused) to = past;
             } else {
-                past = p.past[i], to = p.out_lengths[i];
+                past = held_to(p, p.past[i]), to = held_to(p, p.out_lengths[i]);
+                if (to > past) to = past;
             }
         }
         const int32_t first = pages_of(p, to), gone = pages_of(p, past) - first, end = up_to(gone);
@@ -615,6 +616,8 @@ __global__ __launch_bounds__(1024) void agft_pages_bits_move_kernel(EditArgs p) 
 }
 
 // ---- commits ----
+//
+// What a commit takes from the edit's memory as a place is held to what it is a place of.
 
 // Workgroups (blockIdx.y) that share a chunk's entries.
 constexpr int kCommitParts = 4;
@@ -625,11 +628,13 @@ __global__ __launch_bounds__(kThreads) void agft_pages_commit_kernel(EditArgs p)
     const int32_t thread = group * kThreads + threadIdx.x, threads = groups * kThreads;
     if (thread < 3) p.counters[thread] = p.out[thread];
     if (kind == AGFT_PAGES_FORK) {
-        const int32_t n = p.out[kEntries] < p.max_moves ? p.out[kEntries] : p.max_moves;
+        const int32_t most = p.max_moves < kMaxRequests ? p.max_moves : kMaxRequests;
+        const int32_t n = p.out[kEntries] < most ? p.out[kEntries] : most;
         for (int32_t j = group; j < n; j += groups) {
             const int4 r = p.rows[j];
-            const int32_t *row = p.table + (int64_t)r.y * p.row_pages;
-            for (int32_t c = threadIdx.x; c < r.z; c += kThreads) atomicAdd(&p.owners[page_at(p, row[c])], 1);
+            if ((uint32_t)r.y >= (uint32_t)p.requests) continue;
+            const int32_t *row = p.table + (int64_t)r.y * p.row_pages, full = r.z < p.row_pages ? r.z : p.row_pages;
+            for (int32_t c = threadIdx.x; c < full; c += kThreads) atomicAdd(&p.owners[page_at(p, row[c])], 1);
         }
     } else if (kind == AGFT_PAGES_TRIM) {
         if (p.info[kExtraBefore] != 0) {
@@ -643,7 +648,8 @@ __global__ __launch_bounds__(kThreads) void agft_pages_commit_kernel(EditArgs p)
             }
         }
     } else if (kind == AGFT_PAGES_COMPACT) {
-        const int32_t n = p.info[kHeld], moves = p.info[kMoves];
+        const int32_t n = p.info[kHeld];
+        const int32_t moves = (uint32_t)n < (uint32_t)p.pages ? p.info[kMoves] < p.max_moves ? p.info[kMoves] : p.max_moves : 0;
         const int32_t below = moves > 0 ? free_below(p.bits[n >> 5], p.before[n >> 5], n) : 0;
         for (int32_t k = thread; k < moves; k += threads) {
             const int2 m = p.moves[k];
@@ -653,7 +659,7 @@ __global__ __launch_bounds__(kThreads) void agft_pages_commit_kernel(EditArgs p)
         // every entry in use
         if (threadIdx.x < 64) {
             const int32_t lane = threadIdx.x, i = blockIdx.x * p.per + lane;
-            const int32_t held = lane < p.per && i < p.requests ? pages_of(p, p.past[i]) : 0, end = up_to(held);
+            const int32_t held = lane < p.per && i < p.requests ? pages_of(p, held_to(p, p.past[i])) : 0, end = up_to(held);
             lds.first[lane] = 0, lds.at[lane + 1] = end;
             if (lane == 0) lds.at[0] = 0;
         }
@@ -665,7 +671,7 @@ __global__ __launch_bounds__(kThreads) void agft_pages_commit_kernel(EditArgs p)
             const int32_t id = p.table[idx];
             if ((uint32_t)id >= (uint32_t)p.pages || id < n) continue;
             const int32_t rank = (id - free_below(p.bits[id >> 5], p.before[id >> 5], id)) - (n - below);
-            if (rank < moves) p.table[idx] = p.moves[rank].y;
+            if ((uint32_t)rank < (uint32_t)moves) p.table[idx] = p.moves[rank].y;
         }
     }
     for (int32_t i = thread; i < p.requests; i += threads) p.lengths[i] = p.out_lengths[i];
