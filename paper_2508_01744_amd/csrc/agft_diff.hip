@@ -883,8 +883,10 @@ __device__ __forceinline__ void attend_many(const DiffArgs &p, TileLds<DIM> &lds
         if constexpr (EARLY > 2) score(2);
         __builtin_amdgcn_sched_barrier(0);
         // the maximum that the sums are relative to follows the real one at some distance
-        if (__builtin_expect(__any(top > (float)kRaise || m == -INFINITY), 0)) {
-            const float m1 = (fmaxf(m, off + top) - (float)kTileRaise) + (float)kTileRaise;
+        // (a row's own: another row that grows, or is NaN and never begins, changes none of its bits)
+        const bool grows = top > (float)kRaise || m == -INFINITY;
+        if (__builtin_expect(__any(grows), 0)) {
+            const float m1 = grows ? (fmaxf(m, off + top) - (float)kTileRaise) + (float)kTileRaise : m;
             float fall = m == -INFINITY ? 0.0f : exp2f(m - m1), shift = m1 == -INFINITY ? 0.0f : off - (m1 - (float)kTileRaise);
             m = m1;
             // (keeps the compiler from multiplying ahead of the branch, which is rarely taken)
