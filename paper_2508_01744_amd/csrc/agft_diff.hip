@@ -93,7 +93,8 @@ __device__ __forceinline__ void store4(const DiffArgs &p, int first, int pair, i
 __device__ __forceinline__ void store_lse(const DiffArgs &p, int first, int pair, int map, int r, float m, float l) {
     if (p.lse == nullptr) return;
     const int t = first + r / p.group, hq = (2 * pair + map) * p.group + r % p.group;
-    p.lse[(int64_t)t * p.heads * 2 * p.group + hq] = m == -INFINITY ? -INFINITY : (m + __log2f(l)) * kLn2;
+    // (no keys: m is -infinity and l 0; scores that are all NaN leave m there too, and l tells them)
+    p.lse[(int64_t)t * p.heads * 2 * p.group + hq] = (m + __log2f(l)) * kLn2;
 }
 
 __device__ __forceinline__ float lambda_of(const DiffArgs &p, int first, int pair, int r) {

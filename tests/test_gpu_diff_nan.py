@@ -33,3 +33,10 @@ def test_other_rows_keep_their_bits(past, add, dim):
     (out, lse), (got, got_lse), rows, maps = results(past, add, dim)
     assert bool(out.isfinite().all()) and bool(lse.isfinite().all()) and bool(got[rows].isnan().all())
     assert torch.equal(got[~rows], out[~rows]) and torch.equal(got_lse[~maps], lse[~maps])
+
+
+@pytest.mark.parametrize("past,add,dim", SHAPES)
+def test_log_sums_of_such_queries_are_nan(past, add, dim):
+    """And not -infinity, which says that a row saw no keys."""
+    _, (_, lse), _, maps = results(past, add, dim)
+    assert bool(lse[maps].isnan().all())
