@@ -5,7 +5,9 @@
  * The cache's heads go in pairs: heads 2 p and 2 p + 1 hold the keys of pair p's
  * two maps, and their values, side by side, are the 2 dim numbers that both maps
  * weigh.  For every token of the window and each g < group, with query heads
- * group (2 p + a) + g, a = 0, 1, as agft_kv_attend has them:
+ * group (2 p + a) + g, a = 0, 1, as agft_kv_attend has them (so the two that make
+ * one output lie group heads apart; a projection that puts them side by side has its
+ * rows in another order when group > 1, and no strides of q can tell):
  *
  *   A_a = softmax(scale q_a K_{2p+a}^T)          over the request's tokens up to this one
  *   y   = A_0 V - lambda A_1 V,                  V = [V_{2p} V_{2p+1}]
@@ -25,10 +27,14 @@
  * Products and sums are kept in fp32, the sums of the probabilities and of y^2
  * too; probabilities meet the values in fp16, with the eleven bits and the range
  * that agft_kv_attend gives them, relative to the larger of a page's two value
- * scales (in requests of few rows and for fp16 outputs what that rounding leaves of
- * each is summed as well).  The other head's values of that page keep all their bits while its scale
- * lies within 2^22 (e4m3) or 2^29 (int8) of the larger, fewer beyond, none below
- * 2^-33 (2^-30) of it.
+ * scales.  Where outputs are fp16 and a request brings few rows (tokens x group up
+ * to 16, or to 64 while such requests are little work), what that rounding leaves of
+ * each probability is summed as well: the error is that of 32-bit probabilities.  In
+ * tiles of more rows it is not: fp16 outputs are off by 1.2 to 1.4 times as much there,
+ * bf16 ones by 1.01 times.  The other head's values of that page keep all their bits while
+ * its scale lies within 2^22 (e4m3) or 2^29 (int8) of the larger.  Beyond, e4m3 values
+ * lose them by and by, from the smallest codes on, until 2^41 leaves none; int8 ones
+ * count for nothing.
  */
 #ifndef AGFT_DIFF_H
 #define AGFT_DIFF_H

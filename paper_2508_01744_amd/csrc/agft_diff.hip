@@ -27,7 +27,8 @@ constexpr int kRaise = 15;
 // Two halves of a value row meet the same probabilities, and each page has a scale
 // for either.  The larger one, 2^e, goes into the probabilities' exponent as the
 // one scale of agft_kv_attend does; a half's codes come to fp16 times 2^(ev - e +
-// lift), lift being what fp16's range leaves above the largest code.
+// lift), lift being what fp16's range leaves above the largest code.  They are whole
+// there while their smallest step (2^-9; 1) comes to fp16's, 2^-24, or more.
 template <int FORM>
 constexpr int lift() {
     return FORM == AGFT_KV_E4M3 ? 7 : 5;   // 448 * 2^7; 1152 * 2^5 (the integers' offset below)
@@ -613,10 +614,15 @@ __device__ __forceinline__ int lane_anew() {
 // second map's sums go to the first's wavefronts through LDS at the end.
 //
 // The prompt (10,001 tokens, 16 query heads of 128 numbers, two maps each, int8, causal:
-// 1.23 TFLOP) takes 1.21 ms, 1.0 PFLOP/s, 79% of what a large matrix product of the library
-// reaches (e4m3 1.17 ms; 64 numbers, 0.61 TFLOP, 0.68 to 0.72 ms).  Matrix instructions and
-// vector ones are each busy for a third to a half of the cycles, LDS for a quarter; what
-// counts is that they run beside one another.  Four wavefronts of 128 numbers, one on a
+// 1.23 TFLOP) takes 1.21 to 1.24 ms by card, 1.0 PFLOP/s, 77 to 79% of what a large matrix
+// product of the library reaches, and 1.30 called again and again without a pause (e4m3 1.17
+// to 1.20 ms; 64 numbers, 0.61 TFLOP, 0.73 to 0.76 ms, half as many numbers for each
+// exponential).  Of the cycles matrix instructions are busy for 45% (64 numbers 36%), vector
+// ones for 46% (56%), LDS for 36% (39%), without a bank conflict; what counts is that they
+// run beside one another.  What fp16 leaves of a probability is not summed here, as it is
+// for few rows: it makes fp16 outputs' error 1.00 times that of 32-bit probabilities for 1.22
+// to 1.39, and takes 1.73 ms for 1.20 (64 numbers 1.05 for 0.77), far more than 8-bit codes
+// are worth.  Four wavefronts of 128 numbers, one on a
 // SIMD, 1.89 ms; eight without the scores ahead 1.47; with three operands on their way and
 // 12 registers spilled 1.38; pages and exponents in LDS instead, none spilled, 1.26, and the
 // sums at a raised wave priority 1.23.  64 numbers in steps of 32 tokens 0.81 ms (0.74 on

@@ -590,7 +590,9 @@ class KvCache(_OnStream):
         """Differential attention (agft_diff.h): heads 2 p and 2 p + 1 are a pair,
         y = (softmax(scale q_0 K_0^T) - lam softmax(scale q_1 K_1^T)) [V_0 V_1], and out
         is gain y, or with a weight (float32 [2 dim]) gain weight y / sqrt(mean(y^2) +
-        eps).  q [max_tokens][heads * group][dim], as for attend; lam float32
+        eps).  q [max_tokens][heads * group][dim], as for attend (q_0 and q_1 lie group
+        heads apart: a projection that puts them side by side needs its rows permuted
+        when group > 1); lam float32
         [heads / 2 * group], or [max_tokens][heads / 2 * group] with any strides; out
         [max_tokens][heads / 2 * group][2 * dim]; lse, scale and rows past the window's
         tokens as in attend."""
